@@ -21,6 +21,7 @@
  *             index must be issued in order on one stream (or be ordered by the caller): most
  *             use scratch in its workspace, also where they leave the index as it is.  Only
  *             ice_attend_tokens does not touch the workspace and may overlap with other calls.
+ *             (The 4-bit cache has no index and no state: its calls say which arrays they use.)
  *   Errors    Every call returns an ice_status_t and never throws or aborts.  All errors are
  *             detected on the host from the arguments and host-side counters BEFORE anything is
  *             enqueued; ice_last_error() returns a thread-local description of the last failure.
@@ -284,6 +285,97 @@ typedef struct {
 } ice_geometry_view_t;
 ice_status_t ice_set_geometry(ice_index_t *idx, int32_t geometry);
 ice_status_t ice_export_geometry(ice_index_t *idx, ice_geometry_view_t *view);
+
+/* A cache in 4 bits for the layers that the index does not serve: those that attend to every token (App. A keeps the first layers
+ * dense) and those that reuse an anchor layer's selection (App. B).  One ice_cache_t describes one layer's pool of blocks of
+ * block_size tokens; requests of any length share it through a block table.  Nothing here needs an index.
+ *
+ *   data  ice_cache_bytes() bytes of device memory, 128-byte aligned: [n_blocks][n_kv_heads][block_size / 16] tiles of 2176 bytes.
+ *         A tile holds 16 consecutive tokens of one KV head: 1024 bytes of key codes (64 per token, dimension 2i in the low half of
+ *         byte i), 1024 bytes of value codes, 64 key scales, 64 value scales; the scale of token t's block j of 32 dimensions is
+ *         byte 16 (t mod 4) + 4 j + t / 4.
+ *   Codes  of 32 dimensions share a scale 2^(b - 127), b its byte (b = 255: the values are NaN); a code's low three bits stand for
+ *         0, 0.5, 1, 1.5, 2, 3, 4, 6, its high bit for the sign (the OCP microscaling format MXFP4).
+ *   Slots  token p of request s lies in block block_table[s][p / block_size] at p mod block_size; its slot is
+ *         block * block_size + p mod block_size.  One block table serves the caches of all layers of a model.
+ *
+ * Table entries, slots, lengths and positions are device values, so they are not checked on the host: what names a block or
+ * a token that does not exist is left out (not written, not attended to, read as 0) and nothing outside the arrays is touched.
+ * These calls touch only the arrays that they are given: calls on different streams may overlap where they share no array that
+ * one of them writes.  The current device must be the one that holds the arrays.  Every call is made of kernels alone and can be captured
+ * into a graph. */
+typedef struct {
+    void *data;
+    int32_t n_blocks;    /* >= 1; n_blocks * n_kv_heads * block_size < 2^31                       */
+    int32_t n_kv_heads;  /* >= 1                                                                   */
+    int32_t head_dim;    /* 128 only                                                               */
+    int32_t block_size;  /* 16, 32 or 64 tokens                                                    */
+} ice_cache_t;
+
+/* Bytes of a cache of this shape (data is not looked at).  0 on invalid arguments. */
+size_t ice_cache_bytes(const ice_cache_t *cache);
+
+/* Block tables, lengths and slots of a step, from how many tokens each request gains (new_len > 0) or gives back (new_len < 0:
+ * rejected drafts; -cached_len or less: the request has ended).
+ *   new_len, cached_len int32 [n_requests] -> seq_len int32 [n_requests] = max(cached_len + new_len, 0).
+ *   block_table int32 [n_requests][max_blocks]: of a row only the entries of blocks taken in this call are written.
+ *   free_ids int32 [n_blocks], n_free int32 [1]: a stack of free block ids, its top at free_ids[n_free - 1].  First the blocks
+ *     given back are pushed (by request, then by place in the row), then those taken are popped in the same order; n_free_left
+ *     int32 [1] = its height afterwards.
+ *   query_start int32 [n_requests + 1]: where each request's new tokens begin among the step's tokens, and their number.
+ *   slots int32 [n_slots]: of each new token; -1 behind the last one.
+ *   info int32 [4] = new tokens, blocks taken, blocks given back, and 0 or why the step was refused: 1 the stack is too short,
+ *     2 a request would outgrow its row, 4 more new tokens than n_slots, 8 cached_len or n_free out of range (or a sum of these).  A refused
+ *     step changes no block: seq_len = cached_len, n_free_left = n_free, query_start 0, slots -1.
+ * seq_len may be cached_len and n_free_left may be n_free, so that a captured step can be replayed; other arrays must not overlap.
+ * SHAPE for sizes below 1, n_requests > 65535, n_slots > 2^30, n_blocks * block_size >= 2^31 or max_blocks * block_size >= 2^31. */
+ice_status_t ice_plan_blocks(int32_t n_requests, int32_t block_size, int32_t max_blocks, int32_t n_blocks, const int32_t *new_len,
+                             const int32_t *cached_len, int32_t *seq_len, int32_t *block_table, int32_t *free_ids,
+                             const int32_t *n_free, int32_t *n_free_left, int32_t *query_start, int32_t *slots, int32_t n_slots,
+                             int32_t *info, void *stream);
+
+/* Writes n_tokens tokens' keys and values into their slots (a slot outside the pool is skipped; slots must be distinct).
+ *   k, v: bf16, row t at k + t * k_stride elements, [n_kv_heads][128] contiguous within it; strides are multiples of 8 and may be
+ *   those of a fused projection's output.
+ * A block of 32 values with the largest magnitude a, 2^e <= a < 2^(e+1), gets the scale 2^(e-2), twice that if a > 1.75 * 2^e, at least 2^-100
+ * and at most 2^125, and every value the nearest code to value / scale, the even one on a tie.  A block with an infinity or a NaN is held as
+ * NaN. */
+ice_status_t ice_cache_write(const ice_cache_t *cache, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                             const int32_t *slots, int32_t n_tokens, void *stream);
+
+/* Reads n_rows tokens of every request, from position first[s] on (NULL: from 0), exactly as they are held:
+ *   K, V: bf16 [n_requests, n_kv_heads, n_rows, 128], the layout that ice_build_index and ice_attend_tokens take; rows at
+ *   positions outside [0, seq_len[s]) are 0. */
+ice_status_t ice_cache_read(const ice_cache_t *cache, int32_t n_requests, const int32_t *seq_len, const int32_t *block_table,
+                            int32_t max_blocks, const int32_t *first_or_null, int32_t n_rows, void *K, void *V, void *stream);
+
+/* Causal attention of a step's queries over their requests' cached tokens (Eq. 1, softmax(q . k / sqrt(d)) . v, fp32 accumulation):
+ * query j of request s, row query_start[s] + j of q, stands at position seq_len[s] - (number of s's queries) + j and sees the
+ * positions up to its own, with window > 0 only the last `window` of these.  The step's tokens are written before.
+ *   q: bf16, row t at q + t * q_stride elements (a multiple of 8), [n_kv_heads * group_size][128] within it; group_size 1 to 16, query
+ *     head h reads KV head h / group_size.
+ *   query_start int32 [n_requests + 1], ascending from 0, at most n_tokens (the rows of q and out).  max_query: no request has more queries
+ *     (those beyond are left out).  max_keys: about the longest seq_len, a hint for how the work is cut, not a limit.
+ *   out: fp32 or bf16 [n_tokens][n_kv_heads * group_size][128]; lse_or_null fp32 [n_tokens][n_kv_heads * group_size], the natural logarithm of the
+ *     softmax's sum.  A query that sees nothing (or only scores of -inf) gets 0 and -inf.  Rows behind query_start[n_requests] are left as they were.
+ *   workspace: ice_cache_attend_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0). */
+enum { ICE_OUT_F32 = 0, ICE_OUT_BF16 = 1 };
+size_t ice_cache_attend_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t max_query, int32_t max_keys);
+ice_status_t ice_cache_attend(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,
+                              const int32_t *query_start, int32_t n_tokens, int32_t max_query, const int32_t *seq_len,
+                              int32_t max_keys, const int32_t *block_table, int32_t max_blocks, int32_t window, void *out,
+                              int32_t out_type, float *lse_or_null, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of one query per request over listed positions (App. B: a layer that reuses the selection of its anchor layer): the form
+ * of ice_attend_tokens for this cache.
+ *   token_pos int32 [n_requests, n_kv_heads, max_tok], n_tok int32 [n_requests, n_kv_heads], as ice_selected_tokens writes them; the
+ *     first n_tok entries are used, one outside [0, seq_len[s]) is left out, one that is listed twice counts twice.
+ *   q: bf16, n_requests rows; out, lse as above with n_requests rows; a list without tokens gives 0 and -inf.
+ *   workspace: ice_cache_attend_bytes(cache, group_size, n_requests, 1, max_tok) bytes. */
+ice_status_t ice_cache_attend_tokens(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,
+                                     const int32_t *seq_len, const int32_t *block_table, int32_t max_blocks, const int32_t *token_pos,
+                                     const int32_t *n_tok, int32_t max_tok, void *out, int32_t out_type, float *lse_or_null,
+                                     void *workspace, size_t workspace_bytes, void *stream);
 
 /* Test and snapshot surface.  Export fills `view` with pointers INTO the workspace (no copy).
  * Import copies caller arrays (device pointers, same layout; the export-only fields are

@@ -6,6 +6,7 @@ stream.  There is no fallback: if libicecache.so is missing, loading fails loudl
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -18,7 +19,9 @@ STATUS_NAMES = ["ICE_OK", "ICE_ERR_INVALID_ARG", "ICE_ERR_SHAPE", "ICE_ERR_STATE
                 "ICE_ERR_UNSUPPORTED", "ICE_ERR_DEVICE"]
 SYMBOLS = ["ice_workspace_bytes", "ice_create", "ice_destroy", "ice_build_index", "ice_insert", "ice_insert_batch", "ice_select",
            "ice_attend", "ice_attend_noalloc", "ice_select_attend", "ice_attend_resident", "ice_select_attend_resident", "ice_selected_tokens", "ice_attend_tokens", "ice_select_hier", "ice_select_hier3", "ice_build_top_level", "ice_export_top_level", "ice_set_geometry", "ice_export_geometry", "ice_export_index", "ice_import_index", "ice_debug_assign", "ice_debug_rerun_stage", "ice_debug_build_plan", "ice_debug_near_bounds", "ice_debug_select_fault",
-           "ice_debug_peak_read", "ice_debug_peak_mfma", "ice_last_error"]
+           "ice_debug_peak_read", "ice_debug_peak_mfma", "ice_last_error",
+           "ice_cache_bytes", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
+           "ice_cache_attend_tokens"]
 
 
 class IceConfig(C.Structure):
@@ -35,6 +38,11 @@ class IceIndexView(C.Structure):
                                           "assign", "assign_centroid_bf16", "init_idx")]
 
 
+class IceCacheDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n_blocks", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("block_size", C.c_int32)]
+
+
 class IceTopView(C.Structure):
     _fields_ = [("n_top", C.c_int32), ("n_top_max", C.c_int32), ("top_centroid", C.c_void_p), ("top_centroid_bf16", C.c_void_p),
                 ("top_of", C.c_void_p), ("top_count", C.c_void_p), ("top_init", C.c_void_p)]
@@ -47,6 +55,7 @@ class IceGeometryView(C.Structure):
 
 
 ICE_GEOMETRY_RAW, ICE_GEOMETRY_TRANSFORMED = 0, 1
+ICE_OUT_F32, ICE_OUT_BF16 = 0, 1
 
 
 class IceError(RuntimeError):
@@ -105,8 +114,17 @@ def lib() -> C.CDLL:
                                              C.c_int32, C.c_void_p]
         L.ice_debug_peak_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.ice_debug_peak_mfma.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_double), C.c_void_p]
+        i32, i64, ptr, desc = C.c_int32, C.c_int64, C.c_void_p, C.POINTER(IceCacheDesc)
+        L.ice_cache_bytes.restype = L.ice_cache_attend_bytes.restype = C.c_size_t
+        L.ice_cache_bytes.argtypes = [desc]
+        L.ice_plan_blocks.argtypes = [i32] * 4 + [ptr] * 9 + [i32, ptr, ptr]
+        L.ice_cache_write.argtypes = [desc, ptr, ptr, i64, i64, ptr, i32, ptr]
+        L.ice_cache_read.argtypes = [desc, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, ptr]
+        L.ice_cache_attend_bytes.argtypes = [desc, i32, i32, i32, i32]
+        L.ice_cache_attend.argtypes = [desc, ptr, i64, i32, i32, ptr, i32, i32, ptr, i32, ptr, i32, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
+        L.ice_cache_attend_tokens.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         for name in SYMBOLS:
-            if name not in ("ice_last_error", "ice_workspace_bytes"):
+            if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -301,6 +319,61 @@ def ice_debug_peak_mfma(sink, iters, stream=None) -> float:
     flops = C.c_double(0.0)
     _check(lib().ice_debug_peak_mfma(_ptr(sink), iters, C.byref(flops), _stream(stream)))
     return flops.value
+
+
+def make_cache_desc(data, n_blocks, n_kv_heads, block_size, head_dim=128) -> IceCacheDesc:
+    return IceCacheDesc(_ptr(data), n_blocks, n_kv_heads, head_dim, block_size)
+
+
+def ice_cache_bytes(cache: IceCacheDesc) -> int:
+    return lib().ice_cache_bytes(C.byref(cache))
+
+
+def ice_plan_blocks(new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots, info, block_size,
+                    stream=None) -> None:
+    """int32 device tensors as in the header; block_table [n_requests, max_blocks], free_ids [n_blocks]."""
+    n, n_blocks, n_slots = new_len.numel(), free_ids.numel(), slots.numel()
+    for name, t, size in (("new_len", new_len, n), ("cached_len", cached_len, n), ("seq_len", seq_len, n), ("n_free", n_free, 1),
+                          ("n_free_left", n_free_left, 1), ("query_start", query_start, n + 1), ("info", info, 4),
+                          ("free_ids", free_ids, n_blocks), ("slots", slots, n_slots)):
+        if t.dtype is not torch.int32 or t.numel() != size or not t.is_contiguous() or t.device != block_table.device:
+            raise IceError(ICE_ERR_SHAPE, "%s: contiguous int32 of %d entries on the block table's device" % (name, size))
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or block_table.shape[0] != n or not block_table.is_contiguous():
+        raise IceError(ICE_ERR_SHAPE, "block_table: contiguous int32 [%d, max_blocks]" % n)
+    if not block_table.is_cuda:
+        raise IceError(ICE_ERR_INVALID_ARG, "the arrays must be on a GPU")
+    _check(lib().ice_plan_blocks(n, block_size, block_table.shape[1], n_blocks, _ptr(new_len), _ptr(cached_len), _ptr(seq_len),
+                                 _ptr(block_table), _ptr(free_ids), _ptr(n_free), _ptr(n_free_left), _ptr(query_start), _ptr(slots), n_slots,
+                                 _ptr(info), _stream(stream)))
+
+
+def ice_cache_write(cache: IceCacheDesc, k, v, k_stride, v_stride, slots, n_tokens, stream=None) -> None:
+    """k, v: addresses (rows need not be contiguous with each other)."""
+    _check(lib().ice_cache_write(C.byref(cache), k, v, k_stride, v_stride, _ptr(slots), n_tokens, _stream(stream)))
+
+
+def ice_cache_read(cache: IceCacheDesc, n_requests, seq_len, block_table, max_blocks, first, n_rows, K, V, stream=None) -> None:
+    _check(lib().ice_cache_read(C.byref(cache), n_requests, _ptr(seq_len), _ptr(block_table), max_blocks, _ptr(first), n_rows, _ptr(K),
+                                _ptr(V), _stream(stream)))
+
+
+def ice_cache_attend_bytes(cache: IceCacheDesc, group_size, n_requests, max_query, max_keys) -> int:
+    return lib().ice_cache_attend_bytes(C.byref(cache), group_size, n_requests, max_query, max_keys)
+
+
+def ice_cache_attend(cache: IceCacheDesc, q, q_stride, group_size, n_requests, query_start, n_tokens, max_query, seq_len, max_keys,
+                     block_table, max_blocks, window, out, out_type, lse, workspace, workspace_bytes, stream=None) -> None:
+    """q: an address (its rows need not be contiguous with each other)."""
+    _check(lib().ice_cache_attend(C.byref(cache), q, q_stride, group_size, n_requests, _ptr(query_start), n_tokens, max_query, _ptr(seq_len),
+                                  max_keys, _ptr(block_table), max_blocks, window, _ptr(out), out_type, _ptr(lse), _ptr(workspace),
+                                  workspace_bytes, _stream(stream)))
+
+
+def ice_cache_attend_tokens(cache: IceCacheDesc, q, q_stride, group_size, n_requests, seq_len, block_table, max_blocks, token_pos, n_tok,
+                            max_tok, out, out_type, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().ice_cache_attend_tokens(C.byref(cache), q, q_stride, group_size, n_requests, _ptr(seq_len), _ptr(block_table), max_blocks,
+                                         _ptr(token_pos), _ptr(n_tok), max_tok, _ptr(out), out_type, _ptr(lse), _ptr(workspace),
+                                         workspace_bytes, _stream(stream)))
 
 
 # ------------------------------------------------------------------------------------------------
@@ -536,3 +609,172 @@ class IceIndex:
         best = torch.empty((self.U, n), dtype=torch.float32, device=self.device) if with_best else None
         ice_debug_assign(self.handle, K, n, centroids_bf16, Cn, a, best, stream)
         return a, best
+
+
+def _on_stream(call):
+    """A method whose launches and allocations belong to the `stream` it is given (a torch stream or a raw address), on the device that
+    holds the object's arrays, whichever device and stream are current."""
+    @functools.wraps(call)
+    def method(self, *args, stream=None, **more):
+        if stream is None and torch.cuda.current_device() == self._index:
+            return call(self, *args, **more)
+        with torch.cuda.device(self._index):
+            if stream is None:
+                return call(self, *args, **more)
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=self.device)
+            with torch.cuda.stream(stream):
+                return call(self, *args, **more)
+    return method
+
+
+def _want(ok, text):
+    if not ok:
+        raise IceError(ICE_ERR_SHAPE, text)
+
+
+class IceBlocks:
+    """The block tables of a batch of requests that share a pool of blocks, kept on the GPU.  One serves the caches of all layers.
+
+    block_table [max_requests, max_blocks], seq_len [max_requests], free_ids [n_blocks] and n_free [1] are the state;
+    plan() moves it on by a step without waiting for the GPU."""
+
+    def __init__(self, n_blocks, block_size, max_requests, max_len, device="cuda"):
+        self.block_size, self.n_blocks, self.max_requests = block_size, n_blocks, max_requests
+        self.device = torch.device(device)
+        if block_size not in (16, 32, 64) or n_blocks < 1 or max_requests < 1 or max_len < 1:
+            raise IceError(ICE_ERR_SHAPE, "block_size 16, 32 or 64; n_blocks, max_requests and max_len at least 1")
+        if self.device.type != "cuda":
+            raise IceError(ICE_ERR_INVALID_ARG, "the arrays must be on a GPU")
+        e = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.block_table = e(max_requests, -(-max_len // block_size)).fill_(-1)
+        self.seq_len, self.info, self.query_start = e(max_requests), e(4), e(max_requests + 1)
+        self.free_ids = torch.arange(n_blocks - 1, -1, -1, dtype=torch.int32, device=self.device)  # (block 0 goes out first)
+        self.n_free = e(1).fill_(n_blocks)
+        self._index = self.block_table.device.index
+
+    @_on_stream
+    def plan(self, new_len, n_slots, slots=None):
+        """new_len int32 [max_requests] on the GPU: tokens a request gains (> 0) or gives back (< 0; its length or more: it has
+        ended).  n_slots: room for so many new tokens.  -> (query_start [max_requests + 1], slots [n_slots], info [4]).
+        query_start and info are this object's own and change with the next call."""
+        if slots is None:
+            slots = torch.empty(n_slots, dtype=torch.int32, device=self.device)
+        _want(slots.numel() == n_slots, "slots: %d entries" % n_slots)
+        _want(new_len.numel() == self.max_requests, "new_len: %d entries" % self.max_requests)
+        ice_plan_blocks(new_len, self.seq_len, self.seq_len, self.block_table, self.free_ids, self.n_free, self.n_free, self.query_start,
+                        slots, self.info, self.block_size)
+        return self.query_start, slots, self.info
+
+
+@functools.lru_cache(maxsize=4096)
+def _attend_bytes(n_blocks, n_kv_heads, block_size, group_size, n_requests, max_query, max_keys):
+    return ice_cache_attend_bytes(make_cache_desc(None, n_blocks, n_kv_heads, block_size), group_size, n_requests, max_query, max_keys)
+
+
+class IceCache:
+    """One layer's KV cache in 4 bits (see ice_cache_t in the header).  bf16 tensors may be torch.bfloat16 or int16 bit
+    patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous."""
+
+    def __init__(self, n_blocks, n_kv_heads, block_size=64, device="cuda", data=None):
+        self.n_blocks, self.n_kv_heads, self.block_size = n_blocks, n_kv_heads, block_size
+        if ice_cache_bytes(make_cache_desc(None, n_blocks, n_kv_heads, block_size)) == 0:
+            raise IceError(ICE_ERR_SHAPE, ice_last_error())
+        shape = (n_blocks, n_kv_heads, block_size // 16, 2176)
+        if data is None:
+            data = torch.empty(shape, dtype=torch.uint8, device=device)
+        _want(tuple(data.shape) == shape and data.dtype is torch.uint8 and data.is_contiguous() and data.is_cuda,
+              "data: contiguous uint8 %s on a GPU" % (shape,))
+        self.data, self.device, self._index = data, data.device, data.device.index
+        self._desc = make_cache_desc(data, n_blocks, n_kv_heads, block_size)
+
+    def _rows(self, x, name, heads=None):
+        _want(x.dim() == 3 and x.shape[2] == 128 and (heads is None or x.shape[1] == heads) and x.stride(2) == 1 and
+              (x.stride(1) == 128 or x.shape[1] == 1) and x.element_size() == 2 and not x.dtype.is_complex and x.dtype is not torch.float16 and
+              x.device == self.device, "%s: bf16 [tokens, %s, 128] on the cache's device, heads and values side by side" % (name, heads or "heads"))
+        return x.data_ptr(), x.stride(0)
+
+    def _ints(self, t, name, *shape):
+        _want(t.dtype is torch.int32 and tuple(t.shape) == shape and t.device == self.device and t.is_contiguous(),
+              "%s: contiguous int32 %s on the cache's device" % (name, list(shape)))
+        return t.data_ptr()
+
+    def _table(self, seq_len, block_table):
+        n = seq_len.shape[0]
+        _want(block_table.dim() == 2, "block_table: [requests, max_blocks]")
+        return n, self._ints(seq_len, "seq_len", n), self._ints(block_table, "block_table", n, block_table.shape[1]), block_table.shape[1]
+
+    @_on_stream
+    def write(self, k, v, slots):
+        """k, v [tokens, n_kv_heads, 128] into their slots [tokens]; -1 is left out."""
+        kp, ks = self._rows(k, "k", self.n_kv_heads)
+        vp, vs = self._rows(v, "v", self.n_kv_heads)
+        _want(k.shape[0] == v.shape[0], "k and v: as many tokens")
+        ice_cache_write(self._desc, kp, vp, ks, vs, self._ints(slots, "slots", k.shape[0]), k.shape[0])
+
+    @_on_stream
+    def read(self, block_table, seq_len, n_rows, first=None, out=None):
+        """(K, V) bf16 [requests, n_kv_heads, n_rows, 128]: the tokens from position first[s] on, as they are held."""
+        n, sp, tp, width = self._table(seq_len, block_table)
+        if first is not None:
+            first = self._ints(first, "first", n)
+        if out is None:
+            out = tuple(torch.empty((n, self.n_kv_heads, n_rows, 128), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        K, V = out
+        for x in out:
+            _want(tuple(x.shape) == (n, self.n_kv_heads, n_rows, 128) and x.element_size() == 2 and x.is_contiguous() and x.device == self.device,
+                  "out: two contiguous bf16 tensors [requests, n_kv_heads, n_rows, 128]")
+        ice_cache_read(self._desc, n, sp, tp, width, first, n_rows, K, V)
+        return K, V
+
+    def _outputs(self, q, out, out_dtype, lse, with_lse):
+        shape = q.shape
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype, device=self.device)
+        _want(out.shape == shape and out.is_contiguous() and out.device == self.device and out.dtype in (torch.float32, torch.bfloat16),
+              "out: contiguous float32 or bfloat16 %s" % (tuple(shape),))
+        if lse is None and with_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+        if lse is not None:
+            _want(lse.shape == shape[:2] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.device == self.device,
+                  "lse: contiguous float32 %s" % (tuple(shape[:2]),))
+        return out, lse, ICE_OUT_F32 if out.dtype is torch.float32 else ICE_OUT_BF16
+
+    def _group(self, q):
+        qp, qs = self._rows(q, "q")
+        _want(q.shape[1] % self.n_kv_heads == 0, "q: a multiple of %d heads" % self.n_kv_heads)
+        return qp, qs, q.shape[1] // self.n_kv_heads
+
+    @_on_stream
+    def attend(self, q, query_start, seq_len, block_table, max_query=None, max_len=None, window=0, out=None, out_dtype=torch.float32,
+               lse=None, with_lse=False):
+        """Causal attention of a step's queries q [tokens, heads, 128] over their requests' cached tokens.  max_query, max_len: what the host
+        knows of the most queries of a request (none has more) and the longest length (a hint).  -> out, or (out, lse) when lse is
+        given or with_lse is true.  Rows of q behind query_start[-1] are left out and their outputs left as they were."""
+        qp, qs, group = self._group(q)
+        n, sp, tp, width = self._table(seq_len, block_table)
+        tokens = q.shape[0]
+        out, lse, out_type = self._outputs(q, out, out_dtype, lse, with_lse)
+        if tokens:
+            max_query = tokens if max_query is None else min(max_query, tokens)
+            max_len = width * self.block_size if max_len is None else max_len
+            nbytes = _attend_bytes(self.n_blocks, self.n_kv_heads, self.block_size, group, n, max_query, max_len)
+            work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+            ice_cache_attend(self._desc, qp, qs, group, n, self._ints(query_start, "query_start", n + 1), tokens, max_query, sp, max_len, tp,
+                             width, window, out, out_type, lse, work, nbytes)
+        return out if lse is None else (out, lse)
+
+    @_on_stream
+    def attend_tokens(self, q, seq_len, block_table, token_pos, n_tok, out=None, out_dtype=torch.float32, lse=None, with_lse=False):
+        """Attention of one query per request, q [requests, heads, 128], over positions token_pos[..., :n_tok] of its tokens, both as
+        IceIndex.selected_tokens gives them."""
+        qp, qs, group = self._group(q)
+        n, sp, tp, width = self._table(seq_len, block_table)
+        _want(q.shape[0] == n, "q: one row per request")
+        most = token_pos.shape[-1]
+        pp, np_ = self._ints(token_pos, "token_pos", n, self.n_kv_heads, most), self._ints(n_tok, "n_tok", n, self.n_kv_heads)
+        out, lse, out_type = self._outputs(q, out, out_dtype, lse, with_lse)
+        nbytes = _attend_bytes(self.n_blocks, self.n_kv_heads, self.block_size, group, n, 1, most)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+        ice_cache_attend_tokens(self._desc, qp, qs, group, n, sp, tp, width, pp, np_, most, out, out_type, lse, work, nbytes)
+        return out if lse is None else (out, lse)

@@ -8,6 +8,7 @@
 #include <new>
 #include <unordered_map>
 
+#include "ice_cache.h"
 #include "ice_internal.h"
 
 struct ice_index : ice::Host {};
@@ -387,6 +388,177 @@ ice_status_t ice_attend_tokens(ice_index_t *ix, const void *q, const void *K, co
     const Resident res = {static_cast<const bf16_t *>(K), static_cast<const bf16_t *>(V), max_tok, pos, n_tok, n_rows};
     launch_attend(ix->dev, static_cast<const bf16_t *>(q), nullptr, nullptr, 1, res, out, static_cast<hipStream_t>(stream));
     return device_status("ice_attend_tokens");
+}
+
+// ---- the 4-bit sequence cache
+
+static ice_status_t check_cache(const ice_cache_t *c) {
+    if (!c) return fail(ICE_ERR_INVALID_ARG, "cache is null");
+    if (c->head_dim != kD) return fail(ICE_ERR_UNSUPPORTED, "head_dim %d: only 128 is supported", c->head_dim);
+    if (c->block_size != 16 && c->block_size != 32 && c->block_size != 64)
+        return fail(ICE_ERR_UNSUPPORTED, "block_size %d: only 16, 32, 64 are supported", c->block_size);
+    if (c->n_blocks < 1 || c->n_kv_heads < 1) return fail(ICE_ERR_SHAPE, "n_blocks and n_kv_heads must be >= 1");
+    if ((double)c->n_blocks * c->n_kv_heads * c->block_size >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d blocks of %d tokens for %d KV heads: 2^31 rows or more", c->n_blocks, c->block_size, c->n_kv_heads);
+    return ICE_OK;
+}
+
+static ice_status_t check_cache_data(const ice_cache_t *c) {
+    if (ice_status_t st = check_cache(c)) return st;
+    if (!c->data || (reinterpret_cast<uintptr_t>(c->data) & 127u))
+        return fail(ICE_ERR_INVALID_ARG, "the cache's data is null or not 128-byte aligned");
+    return ICE_OK;
+}
+
+static CacheDims cache_dims(const ice_cache_t *c) {
+    return {static_cast<uint8_t *>(c->data), c->n_blocks, c->n_kv_heads, c->block_size == 64 ? 2 : c->block_size == 32 ? 1 : 0};
+}
+
+static ice_status_t check_table(const ice_cache_t *c, int32_t n_requests, const int32_t *seq_len, const int32_t *table, int32_t max_blocks) {
+    if (!seq_len || !table) return fail(ICE_ERR_INVALID_ARG, "seq_len or block_table is null");
+    if (n_requests < 1 || n_requests > 65535) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, 65535]", n_requests);
+    if (max_blocks < 1 || (long long)max_blocks * c->block_size >= 2147483648ll)
+        return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, and fewer than 2^31 tokens", max_blocks);
+    return ICE_OK;
+}
+
+size_t ice_cache_bytes(const ice_cache_t *c) {
+    if (check_cache(c) != ICE_OK) return 0;
+    return (size_t)c->n_blocks * c->n_kv_heads * (c->block_size / kCacheTile) * kCacheTileBytes;
+}
+
+ice_status_t ice_plan_blocks(int32_t n_requests, int32_t block_size, int32_t max_blocks, int32_t n_blocks, const int32_t *new_len,
+                             const int32_t *cached_len, int32_t *seq_len, int32_t *table, int32_t *free_ids, const int32_t *n_free,
+                             int32_t *n_free_left, int32_t *query_start, int32_t *slots, int32_t n_slots, int32_t *info, void *stream) {
+    if (!new_len || !cached_len || !seq_len || !table || !free_ids || !n_free || !n_free_left || !query_start || !slots || !info)
+        return fail(ICE_ERR_INVALID_ARG, "a pointer is null");
+    if (block_size != 16 && block_size != 32 && block_size != 64)
+        return fail(ICE_ERR_UNSUPPORTED, "block_size %d: only 16, 32, 64 are supported", block_size);
+    if (n_requests < 1 || n_requests > 65535) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, 65535]", n_requests);
+    if (n_slots < 1 || n_slots > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_slots %d is outside [1, 2^30]", n_slots);
+    if (n_blocks < 1 || (long long)n_blocks * block_size >= 2147483648ll)
+        return fail(ICE_ERR_SHAPE, "n_blocks %d: at least 1, and fewer than 2^31 slots", n_blocks);
+    if (max_blocks < 1 || (long long)max_blocks * block_size >= 2147483648ll)
+        return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, and fewer than 2^31 tokens", max_blocks);
+    launch_cache_plan({n_requests, block_size == 64 ? 6 : block_size == 32 ? 5 : 4, max_blocks, n_blocks, new_len, cached_len, seq_len, table,
+                       free_ids, n_free, n_free_left, query_start, slots, n_slots, info},
+                      static_cast<hipStream_t>(stream));
+    return device_status("ice_plan_blocks");
+}
+
+ice_status_t ice_cache_write(const ice_cache_t *c, const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slots,
+                             int32_t n_tokens, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (n_tokens < 0) return fail(ICE_ERR_SHAPE, "n_tokens must be >= 0");
+    if (n_tokens == 0) return ICE_OK;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(ICE_ERR_INVALID_ARG, "k or v is null or misaligned");
+    if (!slots) return fail(ICE_ERR_INVALID_ARG, "slots is null");
+    const int64_t row = (int64_t)c->n_kv_heads * kD;
+    if ((k_stride & 7) || (v_stride & 7) || (n_tokens > 1 && (k_stride < row || v_stride < row)))
+        return fail(ICE_ERR_SHAPE, "strides must be multiples of 8 and at least n_kv_heads * 128");
+    if ((double)((n_tokens + 15ll) / 16) * c->n_kv_heads > 1e7) return fail(ICE_ERR_UNSUPPORTED, "too many rows for one call");
+    launch_cache_write(cache_dims(c), static_cast<const bf16_t *>(k), static_cast<const bf16_t *>(v), k_stride, v_stride, slots, n_tokens,
+                       static_cast<hipStream_t>(stream));
+    return device_status("ice_cache_write");
+}
+
+ice_status_t ice_cache_read(const ice_cache_t *c, int32_t n_requests, const int32_t *seq_len, const int32_t *table, int32_t max_blocks,
+                            const int32_t *first, int32_t n_rows, void *K, void *V, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
+    if (n_rows < 0) return fail(ICE_ERR_SHAPE, "n_rows must be >= 0");
+    if (n_rows == 0) return ICE_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V)) return fail(ICE_ERR_INVALID_ARG, "K or V is null or misaligned");
+    if ((double)((n_rows + 15ll) / 16) * n_requests * c->n_kv_heads > 1e7) return fail(ICE_ERR_UNSUPPORTED, "too many rows for one call");
+    launch_cache_read(cache_dims(c), n_requests, seq_len, table, max_blocks, first, n_rows, static_cast<bf16_t *>(K), static_cast<bf16_t *>(V),
+                      static_cast<hipStream_t>(stream));
+    return device_status("ice_cache_read");
+}
+
+// the sizes that say how an attention call is cut
+static ice_status_t plan_attend(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_query, int32_t max_keys, CacheAttend &a,
+                                size_t *bytes) {
+    if (ice_status_t st = check_cache(c)) return st;
+    if (G < 1 || G > 16) return fail(ICE_ERR_UNSUPPORTED, "group_size %d: only 1 to 16 are supported", G);
+    if (n_requests < 1 || n_requests > 65535) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, 65535]", n_requests);
+    if (max_query < 1 || max_query > (1 << 24)) return fail(ICE_ERR_SHAPE, "max_query %d is outside [1, 2^24]", max_query);
+    if (max_keys < 1 || max_keys > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_keys or max_tok %d is outside [1, 2^30]", max_keys);
+    a.c = cache_dims(c);
+    a.S = n_requests;
+    a.G = G;
+    a.max_query = max_query;
+    a.max_keys = max_keys;
+    a.scale_log2 = 0.12751743f;  // log2(e) / sqrt(128)
+    *bytes = plan_cache_attend(a);
+    if (a.S * (double)a.c.H * a.row_tiles * a.n_chunks >= 8e6)
+        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %d queries of %d heads: too many for one call", a.S, a.c.H, max_query, G);
+    return ICE_OK;
+}
+
+size_t ice_cache_attend_bytes(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_query, int32_t max_keys) {
+    CacheAttend a{};
+    size_t bytes = 0;
+    return plan_attend(c, G, n_requests, max_query, max_keys, a, &bytes) == ICE_OK ? bytes : 0;
+}
+
+static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
+                                 float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
+    if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
+    if ((q_stride & 7) || (a.T > 1 && q_stride < (int64_t)c->n_kv_heads * a.G * kD))
+        return fail(ICE_ERR_SHAPE, "q's stride must be a multiple of 8 and at least n_kv_heads * group_size * 128");
+    if (!out || !aligned16(out)) return fail(ICE_ERR_INVALID_ARG, "out is null or misaligned");
+    if (out_type != ICE_OUT_F32 && out_type != ICE_OUT_BF16) return fail(ICE_ERR_INVALID_ARG, "out_type %d: ICE_OUT_F32 or ICE_OUT_BF16", out_type);
+    if (need && (!ws || !aligned16(ws))) return fail(ICE_ERR_INVALID_ARG, "workspace is null or misaligned");
+    if (need > ws_bytes) return fail(ICE_ERR_CAPACITY, "workspace of %zu bytes, %zu are needed", ws_bytes, need);
+    a.q = static_cast<const bf16_t *>(q);
+    a.q_stride = q_stride;
+    a.out = out;
+    a.out_bf16 = out_type == ICE_OUT_BF16;
+    a.lse = lse;
+    a.part = static_cast<float *>(ws);
+    launch_cache_attend(a, static_cast<hipStream_t>(stream));
+    return device_status(who);
+}
+
+ice_status_t ice_cache_attend(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t G, int32_t n_requests, const int32_t *query_start,
+                              int32_t n_tokens, int32_t max_query, const int32_t *seq_len, int32_t max_keys, const int32_t *table,
+                              int32_t max_blocks, int32_t window, void *out, int32_t out_type, float *lse, void *ws, size_t ws_bytes,
+                              void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
+    if (!query_start) return fail(ICE_ERR_INVALID_ARG, "query_start is null");
+    if (n_tokens < 0) return fail(ICE_ERR_SHAPE, "n_tokens must be >= 0");
+    if (window < 0) return fail(ICE_ERR_SHAPE, "window must be >= 0 (0: no window)");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, a, &need)) return st;
+    if (n_tokens == 0) return ICE_OK;
+    a.T = n_tokens;
+    a.query_start = query_start;
+    a.seq_len = seq_len;
+    a.table = table;
+    a.max_blocks = max_blocks;
+    a.window = window;
+    return cache_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need, stream, "ice_cache_attend");
+}
+
+ice_status_t ice_cache_attend_tokens(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t G, int32_t n_requests,
+                                     const int32_t *seq_len, const int32_t *table, int32_t max_blocks, const int32_t *pos,
+                                     const int32_t *n_tok, int32_t max_tok, void *out, int32_t out_type, float *lse, void *ws,
+                                     size_t ws_bytes, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
+    if (!pos || !n_tok) return fail(ICE_ERR_INVALID_ARG, "token_pos or n_tok is null");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_attend(c, G, n_requests, 1, max_tok, a, &need)) return st;
+    a.T = n_requests;
+    a.seq_len = seq_len;
+    a.table = table;
+    a.max_blocks = max_blocks;
+    a.pos = pos;
+    a.n_tok = n_tok;
+    return cache_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need, stream, "ice_cache_attend_tokens");
 }
 
 static ice_status_t select_hier_common(ice_index_t *ix, const void *q, int32_t budget, int32_t n_top, int32_t n_probe_top,
