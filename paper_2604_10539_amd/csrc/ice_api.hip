@@ -490,8 +490,6 @@ static ice_status_t plan_attend(const ice_cache_t *c, int32_t G, int32_t n_reque
     a.max_keys = max_keys;
     a.scale_log2 = 0.12751743f;  // log2(e) / sqrt(128)
     *bytes = plan_cache_attend(a);
-    if (a.S * (double)a.c.H * a.row_tiles * a.n_chunks >= 8e6)
-        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %d queries of %d heads: too many for one call", a.S, a.c.H, max_query, G);
     return ICE_OK;
 }
 
@@ -504,6 +502,10 @@ size_t ice_cache_attend_bytes(const ice_cache_t *c, int32_t G, int32_t n_request
 static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
                                  float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
     if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
+    // (the sum of a launch's pieces of 128 keys is counted in 31 bits)
+    const double keys = a.pos ? a.max_keys : (double)a.max_blocks * c->block_size, rows = a.pos ? 1 : a.max_query * (double)a.G;
+    if ((keys / 128 + 3) * (rows / 192 + 2) * (a.S < 1024 ? a.S : 1024) * c->n_kv_heads >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %.0f keys x %.0f query rows: too many for one call", a.S, c->n_kv_heads, keys, rows);
     if ((q_stride & 7) || (a.T > 1 && q_stride < (int64_t)c->n_kv_heads * a.G * kD))
         return fail(ICE_ERR_SHAPE, "q's stride must be a multiple of 8 and at least n_kv_heads * group_size * 128");
     if (!out || !aligned16(out)) return fail(ICE_ERR_INVALID_ARG, "out is null or misaligned");

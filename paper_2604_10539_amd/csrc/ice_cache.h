@@ -43,13 +43,17 @@ struct CacheAttend {
     const int *pos, *n_tok;  // listed tokens (then one query per request), or null
     void *out;
     float *lse, *part;
+    int4 *notes;
     int S, T, G, max_query, max_blocks, max_keys, window;
-    int chunk, n_chunks, row_tiles;  // keys per share, shares, tiles of 16 query rows per (request, KV head)
+    int rows;                     // query rows (query, head of the group) that a record has room for
+    int few_groups, many_groups;  // workgroups of the kernel for few queries a request, of the one for many
+    bool many;                    // some request may have more query rows than the first one takes
+    int first, n_here;  // the launch's requests
     float scale_log2;
     bool out_bf16;
 };
-// How a call is cut: fills chunk, n_chunks and row_tiles from the sizes; returns the bytes of workspace.
+// How a call is cut, from the sizes: fills few_groups, many_groups and many; returns the bytes of workspace.
 size_t plan_cache_attend(CacheAttend &a);
-void launch_cache_attend(const CacheAttend &a, hipStream_t stream);
+void launch_cache_attend(CacheAttend a, hipStream_t stream);
 
 }  // namespace ice

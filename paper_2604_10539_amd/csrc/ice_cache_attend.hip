@@ -1,5 +1,6 @@
 // Attention over the 4-bit sequence cache.
 #include <algorithm>
+#include <type_traits>
 
 #include "ice_cache.h"
 
@@ -12,10 +13,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 8;      // of a workgroup
+constexpr int kWaves = 4;      // of a workgroup
 constexpr int kStep = 32;      // keys per step of a wave
-constexpr int kRows = 16;      // query rows (token, head of the group) of a workgroup
-constexpr int kRecord = 132;   // floats per row of a share's partial result: 128 sums, maximum, denominator
+constexpr int kQuantum = kWaves * kStep;
+constexpr int kRows = 16;      // columns of a tile of query rows
+constexpr int kRecord = 132;   // floats per row of a partial result: 128 sums, maximum, denominator
+constexpr int kEntries = 1024; // requests of one launch at most
 constexpr float kNoMax = -3.402823466e38f;  // maximum of a row that has seen no key: below every finite score
 constexpr float kSlack = 8.f;  // a row's reference may lie this far (in powers of two) below its maximum before sums are rescaled
 
@@ -32,386 +35,924 @@ __device__ inline uint32_t pack2(float a, float b) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
+// Scale i of a dword of scale bytes.  The conversion takes the exponent field of its scale operand and nothing else of it.
+__device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }
+__device__ inline float cut(float v, uint32_t mask) { return v - __uint_as_float(__float_as_uint(v) & mask); }
 
-// Where a request's queries and keys lie.
-struct Span {
-    int row0, n_query, len;  // first query row, queries, cached tokens
-    __device__ Span(const CacheAttend &a, int s) {
-        row0 = min(max(a.query_start[s], 0), a.T);
-        n_query = min(max(a.query_start[s + 1], row0), a.T) - row0;
-        len = max(a.seq_len[s], 0);
-        len = (int)min((long long)len, (long long)a.max_blocks << (a.c.tile_shift + 4));
+// A request's query rows and the keys they see; for listed tokens, those of one KV head.
+template <bool LIST>
+struct Unit {
+    int row0, n_query, len;  // first query row, queries, cached tokens (listed: entries of the list)
+    int tokens;              // cached tokens
+    __device__ Unit(const CacheAttend &a, int s, int h) {
+        tokens = max(a.seq_len[s], 0);
+        tokens = (int)min((long long)tokens, (long long)a.max_blocks << (a.c.tile_shift + 4));
+        if constexpr (LIST) {
+            row0 = s;
+            n_query = 1;
+            len = min(max(a.n_tok[s * a.c.H + h], 0), a.max_keys);
+        } else {
+            row0 = min(max(a.query_start[s], 0), a.T);
+            n_query = min(max(a.query_start[s + 1], row0), a.T) - row0;
+            len = tokens;
+        }
     }
+    __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
     // keys [low, high) that query t sees
-    __device__ int high(int t) const { return max(len - n_query + t + 1, 0); }
-    __device__ int low(const CacheAttend &a, int t) const { return a.window > 0 ? max(high(t) - a.window, 0) : 0; }
+    __device__ int high(int t) const { return LIST ? len : max(len - n_query + t + 1, 0); }
+    __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(high(t) - a.window, 0) : 0; }
 };
 
+// Writes four dims of a row from its sums relative to 2^top, and the logarithm of its denominator.
+__device__ inline void put_row(const CacheAttend &a, size_t row, int d0, f32x4 sum, float top, float total) {
+    const bool none = total == 0.f;  // no key at all: the largest of any weights is 2^-kSlack or more
+    sum = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total);
+    if (a.out_bf16) *(uint2 *)((bf16_t *)a.out + row * kD + d0) = make_uint2(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]));
+    else *(f32x4 *)((float *)a.out + row * kD + d0) = sum;
+    if (a.lse && d0 == 0) a.lse[row] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+}
+
+// ------------------------------------------------------------------------------------------------------------- few queries
 // What a wave holds of 32 keys: two tiles of 16.  Key codes: lane (g, c) has dims [32 g, 32 g + 32) of the token that is
 // row c of the product's left operand.  Value codes: lane (g, c) has dims [8 c, 8 c + 8) of tokens g, 4 + g, 8 + g, 12 + g.
 struct Keys {
     u32x4 k[2], v[2];
     uint32_t ks[2], vs[2];
+    uint32_t bad;  // tokens that do not exist, one bit each
 };
 
-// One workgroup: 16 query rows of one (request, KV head) against one share of its keys.
-//
-// S^T = K Q^T puts a row's scores on one lane (g, c): head row c, tokens 4 i + g of each tile; these registers are the
-// right operand of O^T = V^T P^T as they are (contraction slot 8 g + 4 tile + i), and a row's sums come out on the lanes that hold its
-// softmax, so that neither the weights nor the rescaling cross lanes.  Codes become bf16 in registers, without rounding (three
-// significant bits at most).  The weights are split into TERMS bf16 terms whose products add up in fp32: three carry all of a float32
-// weight (float32 outputs), two 16 bits of it.
-template <int TERMS, bool LIST>
-__global__ __launch_bounds__(kWaves * 64) void cache_attend_kernel(CacheAttend a) {
-    __shared__ float s_acc[kWaves][kRows][kRecord];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-    unsigned at = blockIdx.x;
-    const int share = (int)(at % (unsigned)a.n_chunks);
-    at /= (unsigned)a.n_chunks;
-    const int rt = (int)(at % (unsigned)a.row_tiles);
-    at /= (unsigned)a.row_tiles;
-    const int h = (int)(at % (unsigned)a.c.H), s = (int)(at / (unsigned)a.c.H);
+// The part of the flat work that a workgroup does.
+struct Pieces {
+    unsigned total, groups, base, rest;
+    __device__ Pieces(unsigned total_, unsigned most) : total(total_) {
+        groups = min(most, max(total, 1u));
+        base = total / groups;
+        rest = total - base * groups;  // the first `rest` pieces are one longer
+    }
+    __device__ unsigned begin(unsigned i) const { return i * base + min(i, rest); }
+    __device__ unsigned owner(unsigned x) const {
+        const unsigned longer = rest * (base + 1);
+        return x < longer ? x / (base + 1) : rest + (x - longer) / base;
+    }
+};
 
-    // rows of this workgroup and the keys they see
-    int row0, n_rows, low, high, len;  // low, high: of this lane's row c
-    int from, to;                      // keys that any row sees, inside this share
-    int all_low, all_high;             // keys that every row sees
-    if constexpr (LIST) {
-        row0 = s;
-        n_rows = a.G;
-        len = min(max(a.seq_len[s], 0), (int)min((long long)a.max_blocks << (a.c.tile_shift + 4), 0x7FFFFFFFll));
-        low = 0;
-        high = min(max(a.n_tok[s * a.c.H + h], 0), a.max_keys);
-        from = all_low = 0;
-        to = all_high = high;
-    } else {
-        const Span span(a, s);
-        const int total = min(span.n_query, a.max_query) * a.G;
-        n_rows = min(total - kRows * rt, kRows);
-        if (n_rows <= 0) return;
-        row0 = span.row0;
-        len = span.len;
-        const int t_first = kRows * rt / a.G, t_last = (kRows * rt + n_rows - 1) / a.G, t = (kRows * rt + min(c, n_rows - 1)) / a.G;
-        low = span.low(a, t);
-        high = span.high(t);
-        from = span.low(a, t_first);
-        to = span.high(t_last);
-        all_low = span.low(a, t_last);
-        all_high = span.high(t_first);
+// One step of a row's softmax: p, scores of eight keys, become weights relative to 2^m; the sums so far follow when m moves.
+__device__ inline void softmax(float (&p)[8], float scale_log2, float &m, float &l, f32x4 (&acc)[8]) {
+    float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7]))) * scale_log2;
+    if (__any(top > m + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] *= alpha;
     }
-    const bool whole = a.n_chunks == 1;
-    {
-        const int begin = share * a.chunk;
-        const bool last = share == a.n_chunks - 1;
-        from = max(from, begin);
-        if (!last) to = min(to, begin + a.chunk);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], scale_log2, -m));
+        l += p[e];
     }
-    if (from >= to && !whole) return;  // (the merge knows which shares are empty)
-
-    // query rows: right operand of step j holds dims 32 g + 8 j .. + 8 of row c
-    u32x4 qv[4];
-    {
-        const int row = kRows * rt + min(c, n_rows - 1), t = row / a.G;
-        const bf16_t *p = a.q + (long long)(row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
+}
+// The upper halves of eight floats: bf16, cut off.
+__device__ inline u32x4 tops(const float (&p)[8]) {
+    u32x4 w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) qv[j] = *(const u32x4 *)(p + 8 * j);
+    for (int e = 0; e < 8; e += 2) w[e >> 1] = __builtin_amdgcn_perm(__float_as_uint(p[e + 1]), __float_as_uint(p[e]), 0x07060302u);
+    return w;
+}
+// Left operands of the value product for dims 8 c + 2 J and 8 c + 2 J + 1, from codes of four tokens at a time: pairs of dims of a
+// token become pairs of tokens of a dim.
+template <int J> __device__ inline void half_values(const u32x4 &codes, const float *scale, uint32_t *v0, uint32_t *v1) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint32_t r0 = two<J>(codes[i], scale[i]), r1 = two<J>(codes[i + 1], scale[i + 1]);
+        v0[i >> 1] = __builtin_amdgcn_perm(r1, r0, 0x05040100u);
+        v1[i >> 1] = __builtin_amdgcn_perm(r1, r0, 0x07060302u);
     }
-    const int tiles_mask = (1 << a.c.tile_shift) - 1;
-    const int step0 = from / kStep, steps = (to + kStep - 1) / kStep;  // steps of 32 keys: [step0, steps)
-    const int k_row = 4 * (c & 3) + (c >> 2);                          // token that is row c of the key operand: row 4 g + i is token 4 i + g
-    const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
-    const uint32_t v_at = kCacheV + 64 * g + 4 * c, vs_at = kCacheVS + 16 * g + 4 * (c >> 2);
-    const int *table = a.table + (size_t)s * a.max_blocks;
-    const int *list = LIST ? a.pos + ((size_t)s * a.c.H + h) * a.max_keys : nullptr;
-
-    // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n0 + l / 2, in units of tiles of the pool.  Listed:
-    // index of key l & 31 of step n0 + l / 32, in units of rows of the pool.  -1: no such place.
-    auto places = [&](int n0) -> int {
-        if constexpr (LIST) {
-            const long long e = (long long)(step0 + wave + kWaves * (n0 + (lane >> 5))) * kStep + (lane & 31);
-            if (e >= to) return -1;
-            const int p = list[e];
-            if (p < 0 || p >= len) return -1;
-            const int id = table[p >> (a.c.tile_shift + 4)];
-            if (id < 0 || id >= a.c.n_blocks) return -1;
-            return (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15));
-        } else {
-            const int tile = (step0 + wave + kWaves * (n0 + (lane >> 1))) * 2 + (lane & 1);
-            if (tile * 16 >= to) return -1;
-            const int id = table[tile >> a.c.tile_shift];
-            if (id < 0 || id >= a.c.n_blocks) return -1;
-            return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask));
+}
+template <int J> __device__ inline void values(const Keys &y, const float (&scale)[8], u32x4 &v0, u32x4 &v1) {
+    uint32_t a[4], b[4];
+    half_values<J>(y.v[0], scale, a, b);
+    half_values<J>(y.v[1], scale + 4, a + 2, b + 2);
+    v0 = u32x4{a[0], a[1], a[2], a[3]};
+    v1 = u32x4{b[0], b[1], b[2], b[3]};
+}
+// A value block that is held as NaN makes the outputs of the rows that see it NaN, and of no other row: its weight of 0 in the others
+// would.  So where a step's keys are not seen by all rows, such blocks are taken out of the product (take_nan says whether there were any)
+// and looked for again, key by key: nan[x] becomes NaN on the lanes whose dims and row x are hit.  Rare.
+__device__ inline bool take_nan(Keys &y) {
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (((y.vs[e >> 2] >> (8 * (e & 3))) & 0xFF) == 0xFF) {
+            any = true;
+            y.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
         }
-    };
-    constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
-    // requests step n (of this wave); bad: tokens of the step that do not exist, one bit each
-    auto request = [&](int held, int n, Keys &x, uint32_t &bad) {
-        bad = 0;
-        if constexpr (LIST) {
-            bad = (uint32_t)(__ballot(held == -1) >> (32 * (n & 1)));
+    return __any(any);
+}
+template <int NT>
+__device__ inline void find_nan(const CacheAttend &a, const int *table, int h, int key0, int from, int to, int g, const int (&low)[NT],
+                                const int (&high)[NT], float (&nan)[NT]) {
+    for (int key = max(key0, from); key < min(key0 + kStep, to); ++key) {
+        const int id = table[key >> (a.c.tile_shift + 4)];
+        if (id < 0 || id >= a.c.n_blocks) continue;
+        const size_t tile = (((size_t)id * a.c.H + h) << a.c.tile_shift) + ((key >> 4) & ((1 << a.c.tile_shift) - 1));
+        if (a.c.data[tile * kCacheTileBytes + kCacheVS + cache_scale_byte(key & 15, g)] != 255) continue;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const uint32_t kr = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + k_row), 0);
-                const uint8_t *kt = a.c.data + (size_t)(kr >> 4) * kCacheTileBytes;
-                x.k[b] = *(const u32x4 *)(kt + 64 * (kr & 15) + 16 * g);
-                x.ks[b] = kt[kCacheKS + cache_scale_byte(kr & 15, g)];
-                uint32_t sc = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t vr = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + 4 * i + g), 0);
-                    const uint8_t *vt = a.c.data + (size_t)(vr >> 4) * kCacheTileBytes;
-                    x.v[b][i] = *(const uint32_t *)(vt + kCacheV + 64 * (vr & 15) + 4 * c);
-                    sc |= (uint32_t)vt[kCacheVS + cache_scale_byte(vr & 15, c >> 2)] << (8 * i);
-                }
-                x.vs[b] = sc;
-            }
-        } else {
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int id = __builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b);
-                if (id < 0) bad |= 0xFFFFu << (16 * b);
-                const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
-                x.k[b] = __builtin_nontemporal_load((const u32x4 *)(t + k_at));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[b][i] = __builtin_nontemporal_load((const uint32_t *)(t + v_at + 256 * i));
-                x.ks[b] = t[ks_at];
-                x.vs[b] = *(const uint32_t *)(t + vs_at);
-            }
-        }
-    };
-
-    f32x4 acc[8];  // acc[j][i]: dim 32 g + 8 i + j of row c
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = kNoMax, l = 0.f;
-    const int n_mine = steps - step0 - wave > 0 ? (steps - step0 - wave + kWaves - 1) / kWaves : 0;
-    int held = n_mine > 0 ? places(0) : -1;
-    Keys x, y;
-    uint32_t bad_x = 0, bad_y = 0;
-    if (n_mine > 0) request(held, 0, x, bad_x);
-    for (int n = 0; n < n_mine; ++n) {
-        if (n + 1 < n_mine) {
-            if ((n + 1) % kAhead == 0) held = places(n + 1);
-            request(held, n + 1, y, bad_y);
-        }
-        const int key0 = (step0 + wave + kWaves * n) * kStep;
-        f32x4 d[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const float sc = __uint_as_float(x.ks[b] << 23);
-            d[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) d[b] = mfma(eight(x.k[b][j], sc), qv[j], d[b]);
-        }
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = d[e >> 2][e & 3] * a.scale_log2;
-        const bool edge = key0 < max(all_low, from) || key0 + kStep > min(all_high, to) || bad_x != 0;
-        if (edge) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int in = 16 * (e >> 2) + 4 * (e & 3) + g, key = key0 + in;
-                const bool gone = (bad_x >> in) & 1;
-                if (gone || key < max(low, from) || key >= min(high, to)) p[e] = -INFINITY;
-                // what no row sees may hold anything: its value scale must not turn a weight of 0 into NaN
-                if (gone || key < from || key >= to) x.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-            }
-        }
-        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-        if (__any(top > m + kSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float mn = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= alpha;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] *= alpha;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(p[e] - m);
-            l += p[e];
-        }
-        if (!LIST && edge) {
-            // A value block that is held as NaN makes the outputs of the rows that see it NaN, and of no other row: its weight
-            // of 0 in the others would.  Rare: found by a scan of the step's scales, taken out of the product.
-            bool nan = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) nan |= ((x.vs[e >> 2] >> (8 * (e & 3))) & 0xFF) == 0xFF;
-            if (__any(nan)) {
-                for (int in = 0; in < kStep; ++in) {
-                    const int key = key0 + in;
-                    const int blk = table[key >> (a.c.tile_shift + 4)];
-                    if (key >= min(high, to) || key < max(low, from) || blk < 0 || blk >= a.c.n_blocks) continue;
-                    const uint8_t *t = a.c.data + (((((size_t)blk * a.c.H + h) << a.c.tile_shift) + ((key >> 4) & tiles_mask))) * kCacheTileBytes;
-                    if (t[kCacheVS + cache_scale_byte(key & 15, g)] == 255)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) acc[j] += __builtin_nanf("");
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (((x.vs[e >> 2] >> (8 * (e & 3))) & 0xFF) == 0xFF) x.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-            }
-        }
-        // weights in terms
-        u32x4 w[TERMS];
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const uint32_t two = pack2(p[e], p[e + 1]);
-                w[t][e >> 1] = two;
-                if (t + 1 < TERMS) {
-                    p[e] -= bf16_lo(two);
-                    p[e + 1] -= bf16_hi(two);
-                }
-            }
-        // values: pairs of dims of a token, then pairs of tokens of a dim
-        u32x4 va[8];
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const int b = e >> 2, i = e & 3;
-            const float s0 = __uint_as_float(((x.vs[b] >> (8 * i)) & 0xFF) << 23), s1 = __uint_as_float(((x.vs[b] >> (8 * i + 8)) & 0xFF) << 23);
-            const u32x4 r0 = eight(x.v[b][i], s0), r1 = eight(x.v[b][i + 1], s1);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                va[2 * j][e >> 1] = __builtin_amdgcn_perm(r1[j], r0[j], 0x05040100u);
-                va[2 * j + 1][e >> 1] = __builtin_amdgcn_perm(r1[j], r0[j], 0x07060302u);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = mfma(va[j], w[t], acc[j]);
-        x = y;
-        bad_x = bad_y;
+        for (int x = 0; x < NT; ++x)
+            if (key >= low[x] && key < high[x]) nan[x] = __builtin_nanf("");
     }
-
-    // the waves' sums meet in LDS
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (c < n_rows) {
-        float *r = s_acc[wave][c];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *(f32x4 *)(r + 32 * g + 8 * i) = f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
-            *(f32x4 *)(r + 32 * g + 8 * i + 4) = f32x4{acc[4][i], acc[5][i], acc[6][i], acc[7][i]};
-        }
-        if (g == 0) {
-            r[kD] = m;
-            r[kD + 1] = l;
-        }
-    }
-    __syncthreads();
-    const int row = tid >> 5, d0 = 4 * (tid & 31);  // 32 threads to a row, four dims each
-    if (row >= n_rows) return;
-    float top = kNoMax;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_acc[w][row][kD]);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_acc[w][row][kD] - top);
-        sum += *(const f32x4 *)(s_acc[w][row] + d0) * f;
-        total += s_acc[w][row][kD + 1] * f;
-    }
-    if (!whole) {
-        float *r = a.part + ((((size_t)(s * a.c.H + h) * a.row_tiles + rt) * a.n_chunks + share) * kRows + row) * kRecord;
-        *(f32x4 *)(r + d0) = sum;
-        if (d0 == 0) {
-            r[kD] = top;
-            r[kD + 1] = total;
-        }
-        return;
-    }
-    const int t_r = LIST ? 0 : (kRows * rt + row) / a.G;
-    const int head = h * a.G + (kRows * rt + row) % a.G;
-    const size_t o = ((size_t)(row0 + t_r) * a.c.H * a.G + head);
-    const bool none = total == 0.f;  // no key at all: the largest of any weights is 1 or more
-    sum = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total);
-    if (a.out_bf16) {
-        uint2 w = {pack2(sum[0], sum[1]), pack2(sum[2], sum[3])};
-        *(uint2 *)((bf16_t *)a.out + o * kD + d0) = w;
-    } else {
-        *(f32x4 *)((float *)a.out + o * kD + d0) = sum;
-    }
-    if (a.lse && d0 == 0) a.lse[o] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
-// Joins the shares of a call that was cut along the keys: 32 threads to a row.
-template <bool LIST>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttend a) {
-    const int row = threadIdx.x >> 5, d0 = 4 * (threadIdx.x & 31);
-    unsigned at = blockIdx.x;
-    const int half = (int)(at & 1);
-    at >>= 1;
-    const int rt = (int)(at % (unsigned)a.row_tiles);
-    at /= (unsigned)a.row_tiles;
-    const int h = (int)(at % (unsigned)a.c.H), s = (int)(at / (unsigned)a.c.H);
-    const int r = 8 * half + row, in = kRows * rt + r;
-    int row0, t, from, to;
+// Attention of few query rows (queries times heads of a group: at most 16 NT) of every request over its keys.
+//
+// S^T = K Q^T puts a row's scores on one lane (g, c): column c, tokens 4 i + g of each tile; these registers are the
+// right operand of O^T = V^T P^T as they are (contraction slot 8 g + 4 tile + i), and a row's sums come out on the lanes that hold its
+// softmax, so that neither the weights nor the rescaling cross lanes.  Codes become bf16 in registers, without rounding (three
+// significant bits at most).
+//
+// A weight enters the second product as bf16 terms whose products add up in fp32, cut off and not rounded, so that three terms are the
+// float32 weight and two are 16 bits of it.  Few rows leave columns free: with PACK = 3 (up to 5 rows) or 2 (up to 8) the terms of a row stand in
+// columns c, c + R, c + 2 R, whose lanes all compute the row's scores, and one set of products carries them; further terms take a set of
+// their own.  PACK, SETS = 3, 1; 2, 2; 1, 3: three terms, float32 outputs; 3, 1; 2, 1; 1, 2: bf16 outputs; 1, 1: bf16 outputs
+// of more than 16 rows, weights rounded to bf16 (their errors of half a step average out over the keys).
+//
+// The work is flat: the requests' keys in units of 128, KV head behind KV head, cut into equal pieces, one per workgroup, wherever the
+// cuts fall.  Lengths are device values and ragged; so no workgroup is idle while another has more to read.  Every workgroup finds its
+// piece from the lengths.  The part of a (request, KV head) that does not span it leaves its sums in a record; the workgroup
+// whose piece holds the end of one that was cut notes it for the merge.
+template <int PACK, int NT, int SETS, bool LIST>
+__global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
+    static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
+    constexpr int R = kRows / PACK;  // rows in a tile of columns
+    __shared__ float s_acc[kWaves][kRows][kRecord];
+    __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of 128 keys before each request
+    __shared__ unsigned s_wave[kWaves];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+    const int term = PACK == 1 ? 0 : c / R, col_row = PACK == 1 ? c : c % R;
+
+    unsigned total = 0;
+    const unsigned per_list = (unsigned)(a.max_keys + kQuantum - 1) / kQuantum;
     if constexpr (LIST) {
-        if (r >= a.G) return;
-        row0 = s;
-        t = 0;
-        from = 0;
-        to = min(max(a.n_tok[s * a.c.H + h], 0), a.max_keys);
+        total = (unsigned)a.n_here * a.c.H * per_list;
     } else {
-        const Span span(a, s);
-        const int total = min(span.n_query, a.max_query) * a.G, n_rows = min(total - kRows * rt, kRows);
-        if (r >= n_rows) return;
-        row0 = span.row0;
-        t = in / a.G;
-        from = span.low(a, kRows * rt / a.G);
-        to = span.high((kRows * rt + n_rows - 1) / a.G);
+        for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
+            const int e = e0 + tid;
+            unsigned n = 0;
+            if (e < a.n_here) {
+                const Unit<LIST> u(a, a.first + e, 0);
+                const int q = u.queries(a);
+                // at least one where there are rows, which want their outputs; none where the other kernel does the request
+                if (q > 0 && q * a.G <= NT * R)
+                    n = (unsigned)max((u.high(q - 1) + kQuantum - 1) / kQuantum - u.low(a, 0) / kQuantum, 1) * (unsigned)a.c.H;
+            }
+            const unsigned incl = (unsigned)wave_scan_add((int)n);
+            if (lane == 63) s_wave[wave] = incl;
+            __syncthreads();
+            unsigned before = total;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (w < wave) before += s_wave[w];
+                total += s_wave[w];
+            }
+            if (e < a.n_here) s_before[e] = before + incl - n;
+            __syncthreads();
+        }
+        if (tid == 0) s_before[a.n_here] = total;
+        __syncthreads();
     }
-    const float *p = a.part + (((size_t)(s * a.c.H + h) * a.row_tiles + rt) * a.n_chunks * kRows + r) * kRecord;
-    const int c0 = min(from / a.chunk, a.n_chunks - 1), c1 = from < to ? min((to + a.chunk - 1) / a.chunk, a.n_chunks) : 0;
+    const Pieces pieces(total, gridDim.x);
+    if (blockIdx.x >= pieces.groups || total == 0) {
+        if (tid == 0) a.notes[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        return;
+    }
+    const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
+    int4 note = make_int4(-1, 0, 0, 0);
+    int entry = 0;
+    if constexpr (!LIST) {  // the last request that begins at or before the piece (of those, the one that is not empty)
+        for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
+            if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
+    }
+    const int tiles_mask = (1 << a.c.tile_shift) - 1;
+    const int k_row = 4 * (c & 3) + (c >> 2);  // token that is row c of the key operand: row 4 g + i is token 4 i + g
+    const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
+    const uint32_t v_at = kCacheV + 64 * g + 4 * c, vs_at = kCacheVS + 16 * g + 4 * (c >> 2);
+
+    for (unsigned now = begin; now < end;) {
+        int s, h;
+        unsigned u0, u1;
+        if constexpr (LIST) {
+            const unsigned u = now / per_list;
+            s = (int)(u / (unsigned)a.c.H);
+            h = (int)(u % (unsigned)a.c.H);
+            u0 = u * per_list;
+            u1 = u0 + per_list;
+        } else {
+            while (s_before[entry + 1] <= now) ++entry;
+            const unsigned first = s_before[entry], per = (s_before[entry + 1] - first) / (unsigned)a.c.H;
+            s = entry;
+            h = (int)((now - first) / per);
+            u0 = first + (unsigned)h * per;
+            u1 = u0 + per;
+        }
+        s = __builtin_amdgcn_readfirstlane(s) + a.first;
+        h = __builtin_amdgcn_readfirstlane(h);
+        const unsigned stop = min(u1, end);
+        const Unit<LIST> unit(a, s, h);
+        const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
+        // keys of this part that any row sees, that every row sees, that this lane's rows see
+        const int q0 = unit.low(a, 0) / kQuantum;
+        const int from = max(unit.low(a, 0), (q0 + (int)(now - u0)) * kQuantum);
+        const int to = min(unit.high(t_last), (q0 + (int)(stop - u0)) * kQuantum);
+        const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(0), to);
+        int low[NT], high[NT];
+        u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int row = min(R * x + col_row, n_rows - 1), t = row / a.G;
+            low[x] = max(unit.low(a, t), from);
+            high[x] = min(unit.high(t), to);
+            const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
+        }
+        const int step0 = (q0 + (int)(now - u0)) * kWaves;  // the wave's steps: step0 + wave + kWaves n
+        const int n_mine = to > from ? max((to - kStep * (step0 + wave) + kQuantum - 1) / kQuantum, 0) : 0;
+        const int *table = a.table + (size_t)s * a.max_blocks;
+        const int *list = LIST ? a.pos + ((size_t)s * a.c.H + h) * a.max_keys : nullptr;
+
+        // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n0 + l / 2, in units of tiles of the pool.  Listed:
+        // index of key l & 31 of step n0 + l / 32, in units of rows of the pool.  -1: no such place.
+        auto places = [&](int n0) __attribute__((always_inline)) -> int {
+            if constexpr (LIST) {
+                const long long e = (long long)(step0 + wave + kWaves * (n0 + (lane >> 5))) * kStep + (lane & 31);
+                if (e >= to) return -1;
+                const int p = list[e];
+                if (p < 0 || p >= unit.tokens) return -1;
+                const int id = table[p >> (a.c.tile_shift + 4)];
+                if (id < 0 || id >= a.c.n_blocks) return -1;
+                return (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15));
+            } else {
+                const int tile = (step0 + wave + kWaves * (n0 + (lane >> 1))) * 2 + (lane & 1);
+                if ((long long)tile * 16 >= to) return -1;
+                const int id = table[tile >> a.c.tile_shift];
+                if (id < 0 || id >= a.c.n_blocks) return -1;
+                return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask));
+            }
+        };
+        constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
+        // step n of this wave: key codes, value codes
+        auto request_keys = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
+            x.bad = 0;
+            if constexpr (LIST) x.bad = (uint32_t)(__ballot(held == -1) >> (32 * (n & 1)));
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                if constexpr (LIST) {
+                    const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + k_row), 0);
+                    const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
+                    x.k[b] = *(const u32x4 *)(t + 64 * (row & 15) + 16 * g);
+                    x.ks[b] = t[kCacheKS + cache_scale_byte(row & 15, g)];
+                } else {
+                    const int id = __builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b);
+                    if (id < 0) x.bad |= 0xFFFFu << (16 * b);
+                    const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
+                    x.k[b] = __builtin_nontemporal_load((const u32x4 *)(t + k_at));
+                    x.ks[b] = t[ks_at];
+                }
+            }
+        };
+        auto request_values = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                if constexpr (LIST) {
+                    uint32_t scales = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + 4 * i + g), 0);
+                        const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
+                        x.v[b][i] = *(const uint32_t *)(t + kCacheV + 64 * (row & 15) + 4 * c);
+                        scales |= (uint32_t)t[kCacheVS + cache_scale_byte(row & 15, c >> 2)] << (8 * i);
+                    }
+                    x.vs[b] = scales;
+                } else {
+                    const uint8_t *t = a.c.data + (size_t)max(__builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b), 0) * kCacheTileBytes;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x.v[b][i] = __builtin_nontemporal_load((const uint32_t *)(t + v_at + 256 * i));
+                    x.vs[b] = *(const uint32_t *)(t + vs_at);
+                }
+            }
+        };
+
+        f32x4 acc[NT][8];  // acc[x][j][i]: dim 32 g + 8 i + j of column c of tile x
+        float m[NT], l[NT];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            m[x] = kNoMax;
+            l[x] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const uint32_t cut1 = PACK > 1 && term >= 1 ? 0xFFFF0000u : 0u, cut2 = PACK > 2 && term >= 2 ? 0xFFFF0000u : 0u;
+        // Step n; between(): what is to be requested once the key codes have been used.
+        auto attend = [&](int n, Keys &y, auto between) __attribute__((always_inline)) {
+            const int key0 = (step0 + wave + kWaves * n) * kStep;
+            f32x4 d[NT][2];
+#pragma unroll
+            for (int x = 0; x < NT; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const float sc = __uint_as_float(y.ks[b] << 23);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x4 k = eight(y.k[b][j], sc);
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                }
+            }
+            const uint32_t bad = y.bad;
+            between();
+            if (key0 < all_low || key0 + kStep > all_high || bad != 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int in = 16 * (e >> 2) + 4 * (e & 3) + g, key = key0 + in;
+                    const bool gone = (bad >> in) & 1;
+#pragma unroll
+                    for (int x = 0; x < NT; ++x)
+                        if (gone || key < low[x] || key >= high[x]) d[x][e >> 2][e & 3] = -INFINITY;
+                    // what no row sees may hold anything: its value scale must not turn a weight of 0 into NaN
+                    if (gone || key < from || key >= to) y.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+                }
+                if (!LIST && take_nan(y)) {
+                    float nan[NT] = {};
+                    find_nan<NT>(a, table, h, key0, from, to, g, low, high, nan);
+#pragma unroll
+                    for (int x = 0; x < NT; ++x)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
+                }
+            }
+            u32x4 w[NT][SETS];  // the weights' terms
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
+                softmax(p, a.scale_log2, m[x], l[x], acc[x]);
+                if constexpr (PACK == 2 && SETS == 2) {  // first and second term in the first set; the third one on the first's lanes
+                    float third[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float second = cut(p[e], 0xFFFF0000u);
+                        third[e] = term == 0 ? cut(second, 0xFFFF0000u) : 0.f;
+                        p[e] = term == 0 ? p[e] : second;
+                    }
+                    w[x][0] = tops(p);
+                    w[x][1] = tops(third);
+                } else if constexpr (PACK == 1 && SETS == 1) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) w[x][0][e >> 1] = pack2(p[e], p[e + 1]);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < SETS; ++t) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (t > 0) p[e] = cut(p[e], 0xFFFF0000u);
+                            if (PACK > 1) p[e] = cut(p[e], cut1);
+                            if (PACK > 2) p[e] = cut(p[e], cut2);
+                        }
+                        w[x][t] = tops(p);
+                    }
+                }
+            }
+            float vsc[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vsc[e] = scale_of(y.vs[e >> 2], e & 3);
+            auto dims = [&](auto sel) __attribute__((always_inline)) {
+                constexpr int j = decltype(sel)::value;
+                u32x4 v0, v1;
+                values<j>(y, vsc, v0, v1);
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int t = 0; t < SETS; ++t) {
+                        acc[x][2 * j] = mfma(v0, w[x][t], acc[x][2 * j]);
+                        acc[x][2 * j + 1] = mfma(v1, w[x][t], acc[x][2 * j + 1]);
+                    }
+            };
+            dims(std::integral_constant<int, 0>());
+            dims(std::integral_constant<int, 1>());
+            dims(std::integral_constant<int, 2>());
+            dims(std::integral_constant<int, 3>());
+        };
+
+        if (n_mine > 0) {
+            int held = places(0);
+            if constexpr (NT == 1) {  // two steps in registers: one worked on, one on its way
+                Keys x, y;
+                auto request = [&](int n, Keys &z) __attribute__((always_inline)) {
+                    if (n >= n_mine) return;
+                    if (n % kAhead == 0 && n) held = places(n);
+                    request_keys(held, n, z);
+                    request_values(held, n, z);
+                };
+                request(0, x);
+                for (int n = 0; n < n_mine; n += 2) {
+                    request(n + 1, y);
+                    attend(n, x, [] {});
+                    if (n + 1 >= n_mine) break;
+                    request(n + 2, x);
+                    attend(n + 1, y, [] {});
+                }
+            } else {  // no room for a second one: codes are requested as soon as the last ones have been used
+                Keys x;
+                request_keys(held, 0, x);
+                request_values(held, 0, x);
+                for (int n = 0; n < n_mine; ++n) {
+                    const bool more = n + 1 < n_mine;
+                    attend(n, x, [&]() __attribute__((always_inline)) {
+                        if (!more) return;
+                        if ((n + 1) % kAhead == 0) held = places(n + 1);
+                        request_keys(held, n + 1, x);
+                    });
+                    if (more) request_values(held, n + 1, x);
+                }
+            }
+        }
+
+        // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
+        const bool whole = now == u0 && stop == u1;
+        float *record = a.part + ((size_t)blockIdx.x * 2 + (now > u0 ? 0 : 1)) * a.rows * kRecord;
+        const int d0 = 4 * (tid & 31);
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            if (x > 0 && R * x >= n_rows) break;
+            l[x] += __shfl_xor(l[x], 16);
+            l[x] += __shfl_xor(l[x], 32);
+            if (R * x + col_row < n_rows && term < PACK) {
+                float *r = s_acc[wave][c];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    *(f32x4 *)(r + 32 * g + 8 * i) = f32x4{acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+                    *(f32x4 *)(r + 32 * g + 8 * i + 4) = f32x4{acc[x][4][i], acc[x][5][i], acc[x][6][i], acc[x][7][i]};
+                }
+                if (g == 0) {
+                    r[kD] = m[x];
+                    r[kD + 1] = l[x];
+                }
+            }
+            __syncthreads();
+            for (int in = tid >> 5; in < min(R, n_rows - R * x); in += kWaves * 2) {
+                const int row = R * x + in;
+                float top = kNoMax;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_acc[w][in][kD]);
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                float all = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(s_acc[w][in][kD] - top);
+                    f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
+#pragma unroll
+                    for (int t = 1; t < PACK; ++t) v += *(const f32x4 *)(s_acc[w][in + t * R] + d0);
+                    sum += v * f;
+                    all += s_acc[w][in][kD + 1] * f;
+                }
+                if (whole) {
+                    put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, top, all);
+                } else {
+                    float *r = record + (size_t)row * kRecord;
+                    *(f32x4 *)(r + d0) = sum;
+                    if (d0 == 0) {
+                        r[kD] = top;
+                        r[kD + 1] = all;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (now > u0 && stop == u1) note = make_int4(s, h, (int)pieces.owner(u0), 0);
+        now = stop;
+    }
+    if (tid == 0) a.notes[blockIdx.x] = note;
+}
+
+// ------------------------------------------------------------------------------------------------------------ many queries
+// Attention of many query rows of a (request, KV head): 192 at a time, tiles of 16 dealt to the four waves, three each.
+//
+// Bound by the matrix unit, so the codes are converted once per workgroup and not once per wave: of a round of 64 keys a wave converts 16, as
+// the few-query kernel does in registers, and leaves the operands in LDS as they are (a KiB each, 16 bytes a lane), from where all waves take
+// them.  Two buffers of 32 KiB: one barrier per round, and a wave may run a round ahead.  The next round's codes are on their way
+// meanwhile.  Outputs in bf16: weights rounded to bf16, one set of products; float32: three terms, cut off (three sets).
+//
+// The work is flat as above.  A causal row tile sees the more keys the later it stands; so the tiles of a (request, KV head) are taken
+// in pairs, the last and the first, the last but one and the second, which cost the same together, and a pair's place in the flat
+// work is found by a division.
+constexpr int kTiles = 3;                            // tiles of 16 rows per wave
+constexpr int kChunkRows = kWaves * kTiles * kRows;  // rows of a workgroup
+constexpr int kRound = kWaves * 16;                  // keys of a round
+
+struct Chunks {  // how a request's row tiles lie in the flat work of one KV head
+    int tiles;
+    unsigned pair, single, per_head;  // quanta of a pair, of the middle tile of an odd number, of all
+    template <typename U> __device__ static int quanta(const CacheAttend &a, const U &u, int n_rows, int tile) {
+        const int t0 = kChunkRows * tile / a.G, t1 = (min(kChunkRows * (tile + 1), n_rows) - 1) / a.G;
+        return max((u.high(t1) + kQuantum - 1) / kQuantum - u.low(a, t0) / kQuantum, 1);
+    }
+    template <typename U> __device__ Chunks(const CacheAttend &a, const U &u) {
+        const int n_rows = u.queries(a) * a.G;
+        tiles = 0;
+        pair = single = per_head = 0;
+        if (n_rows <= kRows) return;  // (the few-query kernel's, which takes that many where there are requests with more than kFewRows)
+        tiles = (n_rows + kChunkRows - 1) / kChunkRows;
+        const int middle = quanta(a, u, n_rows, (tiles - 1) / 2);
+        // an estimate for the pairs (a line, or with a window concave: the middle is the most); a pair's second tile takes what is left of it
+        if (tiles > 1) pair = (unsigned)max(2 * middle + 2, quanta(a, u, n_rows, tiles - 1) + 1);
+        if (tiles & 1) single = (unsigned)middle;
+        per_head = (unsigned)(tiles / 2) * pair + single;
+    }
+};
+
+template <int SETS>
+__global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend a) {
+    __shared__ u32x4 s_k[2][kWaves][4][64], s_v[2][kRound / kStep][8][64];
+    __shared__ unsigned s_before[kEntries + 1], s_wave[kWaves];
+    __shared__ uint32_t s_flags[2][kWaves];  // of a tile of keys: bit 0: in no block, bit 1: values held as NaN were taken out
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+    unsigned total = 0;
+    for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
+        const int e = e0 + tid;
+        const unsigned n = e < a.n_here ? Chunks(a, Unit<false>(a, a.first + e, 0)).per_head * (unsigned)a.c.H : 0u;
+        const unsigned incl = (unsigned)wave_scan_add((int)n);
+        if (lane == 63) s_wave[wave] = incl;
+        __syncthreads();
+        unsigned before = total;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += s_wave[w];
+            total += s_wave[w];
+        }
+        if (e < a.n_here) s_before[e] = before + incl - n;
+        __syncthreads();
+    }
+    if (tid == 0) s_before[a.n_here] = total;
+    __syncthreads();
+    const Pieces pieces(total, gridDim.x);
+    if (blockIdx.x >= pieces.groups || total == 0) {
+        if (tid == 0) a.notes[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        return;
+    }
+    const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
+    int4 note = make_int4(-1, 0, 0, 0);
+    int entry = 0;
+    for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
+        if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
+    const int tiles_mask = (1 << a.c.tile_shift) - 1;
+    const int k_row = 4 * (c & 3) + (c >> 2);
+    const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
+    const uint32_t v_at = kCacheV + 64 * g + 4 * c, vs_at = kCacheVS + 16 * g + 4 * (c >> 2);
+
+    for (unsigned now = begin; now < end;) {
+        while (s_before[entry + 1] <= now) ++entry;
+        const int s = __builtin_amdgcn_readfirstlane(entry) + a.first;
+        const Unit<false> unit(a, s, 0);
+        const Chunks ch(a, unit);
+        const unsigned first = s_before[entry];
+        const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
+        const unsigned head0 = first + (unsigned)h * ch.per_head, off = now - head0;
+        const int all_rows = unit.queries(a) * a.G;
+        int tile;
+        unsigned u0, u1;
+        if (off < (unsigned)(ch.tiles / 2) * ch.pair) {
+            const int p = (int)(off / ch.pair);
+            const unsigned p0 = head0 + (unsigned)p * ch.pair, split = p0 + (unsigned)Chunks::quanta(a, unit, all_rows, ch.tiles - 1 - p);
+            const bool second = now >= split;
+            tile = second ? p : ch.tiles - 1 - p;
+            u0 = second ? split : p0;
+            u1 = second ? p0 + ch.pair : split;
+        } else {
+            tile = ch.tiles / 2;
+            u0 = head0 + (unsigned)(ch.tiles / 2) * ch.pair;
+            u1 = u0 + ch.single;
+        }
+        tile = __builtin_amdgcn_readfirstlane(tile);
+        const unsigned stop = min(u1, end);
+        const int base = kChunkRows * tile, n_rows = min(all_rows - base, kChunkRows);
+        const int t_first = base / a.G, t_last = (base + n_rows - 1) / a.G;
+        const int q0 = unit.low(a, t_first) / kQuantum + (int)(now - u0);
+        const int from = max(unit.low(a, t_first), q0 * kQuantum);
+        // (the unit's last part takes its keys to the end, whatever was estimated for it)
+        const int to = stop == u1 ? unit.high(t_last) : min(unit.high(t_last), (q0 + (int)(stop - now)) * kQuantum);
+        const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(t_first), to);
+        const int key_at = q0 * kQuantum;  // of the first round
+        const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
+        // this lane's rows: columns of tiles wave + 4 x
+        int low[kTiles], high[kTiles], wave_low = 0, wave_high = to;
+        u32x4 qv[kTiles][4];
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) {
+            const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1), t = row / a.G;
+            low[x] = max(unit.low(a, t), from);
+            high[x] = min(unit.high(t), to);
+            const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
+        }
+        {  // keys that all rows of this wave see
+            const int r0 = min(kRows * wave, n_rows - 1), r1 = min(kRows * (kWaves * (kTiles - 1) + wave) + kRows - 1, n_rows - 1);
+            wave_low = max(unit.low(a, (base + r1) / a.G), from);
+            wave_high = min(unit.high((base + r0) / a.G), to);
+        }
+        const int *table = a.table + (size_t)s * a.max_blocks;
+        auto places = [&](int n0) __attribute__((always_inline)) -> int {  // this wave's tile of round n0 + l
+            const long long t = (long long)(key_at >> 4) + (long long)(n0 + lane) * kWaves + wave;
+            if (t * 16 >= to) return -1;
+            const int id = table[t >> a.c.tile_shift];
+            if (id < 0 || id >= a.c.n_blocks) return -1;
+            return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((int)t & tiles_mask));
+        };
+        u32x4 kc, vc;  // this wave's codes of the next round
+        uint32_t ksc, vsc;
+        bool gone;
+        auto request = [&](int held, int n) __attribute__((always_inline)) {
+            const int id = __builtin_amdgcn_readlane(held, n & 63);
+            gone = id < 0;
+            const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
+            kc = *(const u32x4 *)(t + k_at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vc[i] = *(const uint32_t *)(t + v_at + 256 * i);
+            ksc = t[ks_at];
+            vsc = *(const uint32_t *)(t + vs_at);
+        };
+        f32x4 acc[kTiles][8];
+        float m[kTiles], l[kTiles];
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) {
+            m[x] = kNoMax;
+            l[x] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int n_tiles = (n_rows - kRows * wave + kRows * kWaves - 1) / (kRows * kWaves);  // of this wave (may be 0 or less)
+        int held = rounds > 0 ? places(0) : -1;
+        if (rounds > 0) request(held, 0);
+        // the rounds of a wave with NX tiles of rows, without a branch on the tile between the products
+        auto run = [&](auto count) __attribute__((always_inline)) {
+        for (int n = 0; n < rounds; ++n) {
+            const int buf = n & 1;
+            {  // this wave's keys of the round become operands
+                const int key0 = key_at + n * kRound + 16 * wave;
+                bool nan = false;
+                if (key0 < all_low || key0 + 16 > all_high || gone) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = key0 + 4 * i + g;
+                        const uint32_t byte = 0xFFu << (8 * i);
+                        if (gone || key < from || key >= to) vsc &= ~byte;  // (what no row sees may hold anything)
+                        if ((vsc & byte) == byte) {
+                            nan = true;
+                            vsc &= ~byte;
+                        }
+                    }
+                    nan = __any(nan);
+                }
+                if (lane == 0) s_flags[buf][wave] = (gone ? 1u : 0u) | (nan ? 2u : 0u);
+                const float sc = __uint_as_float(ksc << 23);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s_k[buf][wave][j][lane] = eight(kc[j], sc);
+                float vf[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vf[i] = scale_of(vsc, i);
+                auto dims = [&](auto sel) __attribute__((always_inline)) {
+                    constexpr int j = decltype(sel)::value;
+                    uint32_t v0[2], v1[2];
+                    half_values<j>(vc, vf, v0, v1);
+                    uint2 *at = (uint2 *)&s_v[buf][wave >> 1][2 * j][lane] + (wave & 1);
+                    at[0] = make_uint2(v0[0], v0[1]);
+                    at[2 * 64] = make_uint2(v1[0], v1[1]);
+                };
+                dims(std::integral_constant<int, 0>());
+                dims(std::integral_constant<int, 1>());
+                dims(std::integral_constant<int, 2>());
+                dims(std::integral_constant<int, 3>());
+            }
+            if (n + 1 < rounds) {
+                if (((n + 1) & 63) == 0) held = places(n + 1);
+                request(held, n + 1);
+            }
+            lds_barrier();
+            const int n_steps = min(kRound / kStep, (to - key_at - n * kRound + kStep - 1) / kStep);
+            auto steps = [&](auto tiles) __attribute__((always_inline)) {
+                constexpr int NX = decltype(tiles)::value;
+#pragma unroll 1
+                for (int step = 0; step < n_steps; ++step) {
+                    const int key0 = key_at + n * kRound + step * kStep;
+                    f32x4 d[NX][2];
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const u32x4 k = s_k[buf][2 * step + b][j][lane];
+#pragma unroll
+                            for (int x = 0; x < NX; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                        }
+                    const uint32_t flags = (uint32_t)__builtin_amdgcn_readfirstlane((int)(s_flags[buf][2 * step] | s_flags[buf][2 * step + 1] << 2));
+                    if (key0 < wave_low || key0 + kStep > wave_high || flags != 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int key = key0 + 16 * (e >> 2) + 4 * (e & 3) + g;
+                            const bool none = (flags >> (2 * (e >> 2))) & 1;
+#pragma unroll
+                            for (int x = 0; x < NX; ++x)
+                                if (none || key < low[x] || key >= high[x]) d[x][e >> 2][e & 3] = -INFINITY;
+                        }
+                        if (flags & 10u) {
+                            float nan[kTiles] = {};
+                            find_nan<kTiles>(a, table, h, key0, from, to, g, low, high, nan);
+#pragma unroll
+                            for (int x = 0; x < NX; ++x)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
+                        }
+                    }
+                    if constexpr (SETS == 1) {
+                        u32x4 w[NX];
+#pragma unroll
+                        for (int x = 0; x < NX; ++x) {
+                            float p[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
+                            softmax(p, a.scale_log2, m[x], l[x], acc[x]);
+#pragma unroll
+                            for (int e = 0; e < 8; e += 2) w[x][e >> 1] = pack2(p[e], p[e + 1]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const u32x4 v = s_v[buf][step][j][lane];
+#pragma unroll
+                            for (int x = 0; x < NX; ++x) acc[x][j] = mfma(v, w[x], acc[x][j]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < NX; ++x) {
+                            float p[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
+                            softmax(p, a.scale_log2, m[x], l[x], acc[x]);
+                            u32x4 w[SETS];
+#pragma unroll
+                            for (int t = 0; t < SETS; ++t) {
+                                if (t > 0)
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) p[e] = cut(p[e], 0xFFFF0000u);
+                                w[t] = tops(p);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const u32x4 v = s_v[buf][step][j][lane];
+#pragma unroll
+                                for (int t = 0; t < SETS; ++t) acc[x][j] = mfma(v, w[t], acc[x][j]);
+                            }
+                        }
+                    }
+                }
+            };
+            steps(count);
+        }
+        };
+        // (a wave without rows converts all the same; its one tile is not written)
+        if (n_tiles >= 3) run(std::integral_constant<int, 3>());
+        else if (n_tiles == 2) run(std::integral_constant<int, 2>());
+        else run(std::integral_constant<int, 1>());
+        lds_barrier();  // (the last operands have been used: the next part writes others)
+        const bool whole = now == u0 && stop == u1;
+        float *record = a.part + ((size_t)blockIdx.x * 2 + (now > u0 ? 0 : 1)) * a.rows * kRecord;
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x) {
+            const int in = kRows * (kWaves * x + wave) + c, row = base + in;
+            l[x] += __shfl_xor(l[x], 16);
+            l[x] += __shfl_xor(l[x], 32);
+            if (in >= n_rows) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int d0 = 32 * g + 8 * i + 4 * half;
+                    const f32x4 sum = {acc[x][4 * half][i], acc[x][4 * half + 1][i], acc[x][4 * half + 2][i], acc[x][4 * half + 3][i]};
+                    if (whole) put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, m[x], l[x]);
+                    else *(f32x4 *)(record + (size_t)in * kRecord + d0) = sum;
+                }
+            if (!whole && g == 0) {
+                record[(size_t)in * kRecord + kD] = m[x];
+                record[(size_t)in * kRecord + kD + 1] = l[x];
+            }
+        }
+        if (now > u0 && stop == u1) note = make_int4(s, h, (int)pieces.owner(u0), base);
+        now = stop;
+    }
+    if (tid == 0) a.notes[blockIdx.x] = note;
+}
+
+// Joins the records of the unit whose end workgroup blockIdx.x noted, if it did: one of workgroup note.z (its last part), one each
+// of those behind it up to this one (their first parts).  Groups of 32 threads take a row, four dims each; GROUPS of them share a row's records.
+// Bound by three round trips to memory: the note, the maxima, the sums.
+constexpr int kMergeThreads = 256;
+template <int GROUPS, bool LIST>
+__global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend a) {
+    __shared__ float s_sum[kMergeThreads / 32][kRecord];
+    const int4 note = a.notes[blockIdx.x];
+    if (note.x < 0) return;
+    const int all = threadIdx.x >> 5, group = all % GROUPS, d0 = 4 * (threadIdx.x & 31), i = threadIdx.x & 31;
+    const int in = (int)blockIdx.y * (kMergeThreads / 32 / GROUPS) + all / GROUPS;
+    const int s = note.x, h = note.y, n = (int)blockIdx.x - note.z + 1, row = note.w + in;
+    const Unit<LIST> unit(a, s, h);
+    const bool mine = in < a.rows && row < unit.queries(a) * a.G;
     float top = kNoMax, total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int c = c0; c < c1; ++c) {
-        const float *x = p + (size_t)c * kRows * kRecord;
-        const float m = x[kD], mn = fmaxf(top, m), f0 = __builtin_amdgcn_exp2f(top - mn), f1 = __builtin_amdgcn_exp2f(m - mn);
-        sum = sum * f0 + *(const f32x4 *)(x + d0) * f1;
-        total = total * f0 + x[kD + 1] * f1;
-        top = mn;
+    if (mine) {
+        auto record = [&](int k) { return a.part + (((size_t)(note.z + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + in) * kRecord; };
+        for (int k = i; k < n; k += 32) top = fmaxf(top, record(k)[kD]);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+#pragma unroll 4
+        for (int k = group; k < n; k += GROUPS) {
+            const float *x = record(k);
+            const float f = __builtin_amdgcn_exp2f(x[kD] - top);
+            sum += *(const f32x4 *)(x + d0) * f;
+            total += x[kD + 1] * f;
+        }
     }
-    const bool none = total == 0.f;
-    const size_t o = (size_t)(row0 + t) * a.c.H * a.G + h * a.G + in % a.G;
-    sum = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total);
-    if (a.out_bf16) {
-        uint2 w = {pack2(sum[0], sum[1]), pack2(sum[2], sum[3])};
-        *(uint2 *)((bf16_t *)a.out + o * kD + d0) = w;
-    } else {
-        *(f32x4 *)((float *)a.out + o * kD + d0) = sum;
+    if constexpr (GROUPS > 1) {
+        *(f32x4 *)(s_sum[all] + d0) = sum;
+        if (i == 0) s_sum[all][kD] = total;
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int w = 1; w < GROUPS; ++w) {
+            sum += *(const f32x4 *)(s_sum[all + w] + d0);
+            total += s_sum[all + w][kD];
+        }
     }
-    if (a.lse && d0 == 0) a.lse[o] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+    if (mine) put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, top, total);
 }
 
 }  // namespace
 
+// Query rows of the launch for few: all of them up to kFewRows, else the requests' with at most 16, and a launch of the many-query
+// kernel serves the others.  768 or (more than 16 rows) 512 workgroups of the first are resident at a time, 512 of the second; there are no
+// more of them than quanta.
+constexpr int kFewRows = 48;
+static int few_rows(const CacheAttend &a) {
+    const long long rows = (long long)a.max_query * a.G;
+    return rows <= 5 ? 5 : rows <= 8 ? 8 : rows <= 16 || rows > kFewRows ? 16 : rows <= 32 ? 32 : 48;
+}
+static size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(int4)); }
+
 size_t plan_cache_attend(CacheAttend &a) {
-    const int rows = a.max_query * a.G;
-    a.row_tiles = (rows + kRows - 1) / kRows;
-    const long long units = (long long)a.S * a.c.H * a.row_tiles;
-    const int quantum = kWaves * kStep;  // keys of one step of all waves
-    const long long most = std::max(1, (a.max_keys + quantum - 1) / quantum);
-    const long long want = std::min(most, std::max(1ll, 1024 / units));
-    a.chunk = (int)((most + want - 1) / want) * quantum;
-    a.n_chunks = (int)((most * quantum + a.chunk - 1) / a.chunk);
-    return a.n_chunks > 1 ? (size_t)units * a.n_chunks * kRows * kRecord * 4 : 0;
+    const long long quanta = ((long long)a.max_keys + kQuantum - 1) / kQuantum * std::min(a.S, kEntries) * a.c.H;
+    const int rows = few_rows(a);
+    a.few_groups = (int)std::min<long long>(rows > 16 ? 512 : 768, quanta);
+    a.many = (long long)a.max_query * a.G > kFewRows;
+    const long long tiles = ((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows;
+    a.many_groups = a.many ? (int)std::min<long long>(512, quanta * tiles) : 0;
+    return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, kChunkRows));
 }
 
-void launch_cache_attend(const CacheAttend &a, hipStream_t stream) {
-    const unsigned units = (unsigned)a.S * a.c.H * a.row_tiles;
-    if (a.pos) {
-        cache_attend_kernel<3, true><<<units * a.n_chunks, kWaves * 64, 0, stream>>>(a);
-        if (a.n_chunks > 1) cache_merge_kernel<true><<<units * 2, 256, 0, stream>>>(a);
-    } else {
-        if (a.out_bf16) cache_attend_kernel<2, false><<<units * a.n_chunks, kWaves * 64, 0, stream>>>(a);
-        else cache_attend_kernel<3, false><<<units * a.n_chunks, kWaves * 64, 0, stream>>>(a);
-        if (a.n_chunks > 1) cache_merge_kernel<false><<<units * 2, 256, 0, stream>>>(a);
+void launch_cache_attend(CacheAttend a, hipStream_t stream) {
+    const dim3 block(kWaves * 64);
+    float *const part = a.part;
+    auto few = [&](auto list) {
+        constexpr bool L = decltype(list)::value;
+        a.rows = few_rows(a);
+        a.notes = (int4 *)part;
+        a.part = (float *)(a.notes + a.few_groups);
+        const dim3 grid(a.few_groups);
+        if (a.rows == 5) cache_attend_kernel<3, 1, 1, L><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<2, 1, 1, L><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 8) cache_attend_kernel<2, 1, 2, L><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 16 && a.out_bf16) cache_attend_kernel<1, 1, 2, L><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 16) cache_attend_kernel<1, 1, 3, L><<<grid, block, 0, stream>>>(a);
+        else if constexpr (!L) {
+            if (a.rows == 32 && a.out_bf16) cache_attend_kernel<1, 2, 1, L><<<grid, block, 0, stream>>>(a);
+            else if (a.rows == 32) cache_attend_kernel<1, 2, 3, L><<<grid, block, 0, stream>>>(a);
+            else if (a.out_bf16) cache_attend_kernel<1, 3, 1, L><<<grid, block, 0, stream>>>(a);
+            else cache_attend_kernel<1, 3, 3, L><<<grid, block, 0, stream>>>(a);
+        }
+        cache_merge_kernel<8, L><<<dim3(a.few_groups, std::min(a.rows, a.max_query * a.G)), kMergeThreads, 0, stream>>>(a);
+    };
+    for (a.first = 0; a.first < a.S; a.first += kEntries) {
+        a.n_here = std::min(a.S - a.first, kEntries);
+        if (a.pos) few(std::true_type());
+        else few(std::false_type());
+        if (!a.many) continue;
+        a.rows = kChunkRows;
+        a.notes = (int4 *)part;
+        a.part = (float *)(a.notes + a.many_groups);
+        if (a.out_bf16) cache_chunk_kernel<1><<<a.many_groups, block, 0, stream>>>(a);
+        else cache_chunk_kernel<3><<<a.many_groups, block, 0, stream>>>(a);
+        cache_merge_kernel<1, false><<<dim3(a.many_groups, kChunkRows / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
     }
 }
 

@@ -102,7 +102,7 @@ def plan(new_len, cached_len, table, free_ids, n_free, block, n_slots):
     return np.array(after), table, free_ids, n_free, np.array(start), np.array(slots), np.array([fresh, taken, back, 0])
 
 
-def softmax_rows(q, k, v, seen, bf16_out):
+def softmax_rows(q, k, v, seen, bf16_out, many=False):
     """(out, lse, tolerance of out, tolerance of lse) of query rows q [r, 128] against keys [n, 128], seen [r, n], in 64 bits.
 
     Tolerance.  A score is a chain of 128 exact products in fp32 and a multiplication: off by at most 130 * 2^-23 of the sum of
@@ -110,7 +110,9 @@ def softmax_rows(q, k, v, seen, bf16_out):
     the exponent subtracts the reference (one more rounding of a number of the scores' size) and exp2 is taken to be good to 2^-21.  With d the
     largest such error among a row's scores in natural units, every weight and their sum are off by a factor within e^(+-d): 2 d between them.  Sums of n
     weighted values in fp32, rescaled now and then and joined: (n + 64) 2^-23 of the sum of their magnitudes, for the denominator
-    likewise.  Weights in three bf16 terms: 2^-24; in two (bf16 outputs): 2^-16; a bf16 output is rounded by at most 2^-8."""
+    likewise.  Weights in three bf16 terms: 2^-24; in two (bf16 outputs): 2^-16; a bf16 output is rounded by at most 2^-8.  A bf16 output of a
+    call with more than 16 query rows per request (`many`) may come from weights rounded to bf16 once: each is off by at most half a step, 2^-8 of itself, so
+    the sum by at most 2^-8 of the sum of the magnitudes (the denominator is summed from the weights before they are rounded)."""
     n = k.shape[0]
     s = q @ np.where(np.isnan(k), 0, k).T / np.sqrt(128.0)
     s = np.where(np.isnan(k).any(1)[None], np.nan, s)
@@ -129,7 +131,7 @@ def softmax_rows(q, k, v, seen, bf16_out):
     with np.errstate(divide="ignore"):
         lse = top + np.log(total)
     d = np.where(seen, 130 * 2.0 ** -23 * mag, 0).max(1, initial=0) + 2.0 ** -21 + 2.0 ** -23 * np.where(any_seen, np.abs(np.where(np.isfinite(s), s, 0)).max(1, initial=0), 0) * 2
-    weight = 2 * d + 2 * (n + 64) * 2.0 ** -23 + (2.0 ** -16 if bf16_out else 2.0 ** -24)
+    weight = 2 * d + 2 * (n + 64) * 2.0 ** -23 + (2.0 ** -8 if bf16_out and many else 2.0 ** -16 if bf16_out else 2.0 ** -24)
     tol = weight[:, None] * (p @ np.abs(clean)) + (2.0 ** -8 * np.abs(out) if bf16_out else 0) + 1e-37
     lse_tol = d + (n + 64) * 2.0 ** -23 + 2.0 ** -22 * np.abs(np.where(any_seen, lse, 0))
     return out, lse, tol, lse_tol

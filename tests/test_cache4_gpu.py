@@ -239,7 +239,7 @@ def expected(q, data, table, lens, qlens, block, group, window, bf16_out, n_bloc
             k, v = ref.rows(data, np.where(there, blk, 0), pos % block, h)
             k, v = np.where(there[:, None], k, 0), np.where(there[:, None], v, 0)
             for j in range(group):
-                res.append(ref.softmax_rows(q[at: at + m, h * group + j], k, v, seen, bf16_out))
+                res.append(ref.softmax_rows(q[at: at + m, h * group + j], k, v, seen, bf16_out, max(qlens) * group > 16))
         parts.append([np.stack([r[i] for r in res], 1) for i in range(4)])
         at += m
     return [np.concatenate([p[i] for p in parts]) for i in range(4)]
