@@ -328,7 +328,7 @@ size_t ice_cache_bytes(const ice_cache_t *cache);
  *     2 a request would outgrow its row, 4 more new tokens than n_slots, 8 cached_len or n_free out of range (or a sum of these).  A refused
  *     step changes no block: seq_len = cached_len, n_free_left = n_free, query_start 0, slots -1.
  * seq_len may be cached_len and n_free_left may be n_free, so that a captured step can be replayed; other arrays must not overlap.
- * SHAPE for sizes below 1, n_requests > 65535, n_slots > 2^30, n_blocks * block_size >= 2^31 or max_blocks * block_size >= 2^31. */
+ * SHAPE for sizes below 1, n_requests > 8192, n_slots > 2^30, n_blocks * block_size >= 2^31 or max_blocks * block_size >= 2^31. */
 ice_status_t ice_plan_blocks(int32_t n_requests, int32_t block_size, int32_t max_blocks, int32_t n_blocks, const int32_t *new_len,
                              const int32_t *cached_len, int32_t *seq_len, int32_t *block_table, int32_t *free_ids,
                              const int32_t *n_free, int32_t *n_free_left, int32_t *query_start, int32_t *slots, int32_t n_slots,
@@ -371,7 +371,8 @@ ice_status_t ice_cache_attend(const ice_cache_t *cache, const void *q, int64_t q
  *   token_pos int32 [n_requests, n_kv_heads, max_tok], n_tok int32 [n_requests, n_kv_heads], as ice_selected_tokens writes them; the
  *     first n_tok entries are used, one outside [0, seq_len[s]) is left out, one that is listed twice counts twice.
  *   q: bf16, n_requests rows; out, lse as above with n_requests rows; a list without tokens gives 0 and -inf.
- *   workspace: ice_cache_attend_bytes(cache, group_size, n_requests, 1, max_tok) bytes. */
+ *   workspace: ice_cache_attend_tokens_bytes() bytes, as above. */
+size_t ice_cache_attend_tokens_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t max_tok);
 ice_status_t ice_cache_attend_tokens(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,
                                      const int32_t *seq_len, const int32_t *block_table, int32_t max_blocks, const int32_t *token_pos,
                                      const int32_t *n_tok, int32_t max_tok, void *out, int32_t out_type, float *lse_or_null,

@@ -21,7 +21,7 @@ SYMBOLS = ["ice_workspace_bytes", "ice_create", "ice_destroy", "ice_build_index"
            "ice_attend", "ice_attend_noalloc", "ice_select_attend", "ice_attend_resident", "ice_select_attend_resident", "ice_selected_tokens", "ice_attend_tokens", "ice_select_hier", "ice_select_hier3", "ice_build_top_level", "ice_export_top_level", "ice_set_geometry", "ice_export_geometry", "ice_export_index", "ice_import_index", "ice_debug_assign", "ice_debug_rerun_stage", "ice_debug_build_plan", "ice_debug_near_bounds", "ice_debug_select_fault",
            "ice_debug_peak_read", "ice_debug_peak_mfma", "ice_last_error",
            "ice_cache_bytes", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
-           "ice_cache_attend_tokens"]
+           "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes"]
 
 
 class IceConfig(C.Structure):
@@ -115,7 +115,8 @@ def lib() -> C.CDLL:
         L.ice_debug_peak_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.ice_debug_peak_mfma.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_double), C.c_void_p]
         i32, i64, ptr, desc = C.c_int32, C.c_int64, C.c_void_p, C.POINTER(IceCacheDesc)
-        L.ice_cache_bytes.restype = L.ice_cache_attend_bytes.restype = C.c_size_t
+        L.ice_cache_bytes.restype = L.ice_cache_attend_bytes.restype = L.ice_cache_attend_tokens_bytes.restype = C.c_size_t
+        L.ice_cache_attend_tokens_bytes.argtypes = [desc, i32, i32, i32]
         L.ice_cache_bytes.argtypes = [desc]
         L.ice_plan_blocks.argtypes = [i32] * 4 + [ptr] * 9 + [i32, ptr, ptr]
         L.ice_cache_write.argtypes = [desc, ptr, ptr, i64, i64, ptr, i32, ptr]
@@ -124,7 +125,8 @@ def lib() -> C.CDLL:
         L.ice_cache_attend.argtypes = [desc, ptr, i64, i32, i32, ptr, i32, i32, ptr, i32, ptr, i32, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         L.ice_cache_attend_tokens.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         for name in SYMBOLS:
-            if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes"):
+            if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
+                            "ice_cache_attend_tokens_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -160,6 +162,11 @@ def _stream(stream) -> int | None:
             return _raw_current_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _stream_on(index: int) -> int:
+    """The current stream of a device that CUDA is already up on."""
+    return _raw_current_stream(index) if _raw_current_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def make_config(batch, n_kv_heads, group_size, max_tokens, kmeans_iters=10, seed=0, init_idx=None, head_dim=128):
@@ -332,19 +339,19 @@ def ice_cache_bytes(cache: IceCacheDesc) -> int:
 def ice_plan_blocks(new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots, info, block_size,
                     stream=None) -> None:
     """int32 device tensors as in the header; block_table [n_requests, max_blocks], free_ids [n_blocks]."""
-    n, n_blocks, n_slots = new_len.numel(), free_ids.numel(), slots.numel()
+    n, n_blocks, n_slots, device, table = new_len.numel(), free_ids.numel(), slots.numel(), block_table.get_device(), block_table.shape
     for name, t, size in (("new_len", new_len, n), ("cached_len", cached_len, n), ("seq_len", seq_len, n), ("n_free", n_free, 1),
                           ("n_free_left", n_free_left, 1), ("query_start", query_start, n + 1), ("info", info, 4),
-                          ("free_ids", free_ids, n_blocks), ("slots", slots, n_slots)):
-        if t.dtype is not torch.int32 or t.numel() != size or not t.is_contiguous() or t.device != block_table.device:
+                          ("free_ids", free_ids, n_blocks), ("slots", slots, n_slots), ("block_table", block_table, block_table.numel())):
+        if not (t.dtype is torch.int32 and t.numel() == size and t.get_device() == device and t.is_contiguous()):
             raise IceError(ICE_ERR_SHAPE, "%s: contiguous int32 of %d entries on the block table's device" % (name, size))
-    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or block_table.shape[0] != n or not block_table.is_contiguous():
-        raise IceError(ICE_ERR_SHAPE, "block_table: contiguous int32 [%d, max_blocks]" % n)
-    if not block_table.is_cuda:
+    if len(table) != 2 or table[0] != n:
+        raise IceError(ICE_ERR_SHAPE, "block_table: [%d, max_blocks]" % n)
+    if device < 0:
         raise IceError(ICE_ERR_INVALID_ARG, "the arrays must be on a GPU")
-    _check(lib().ice_plan_blocks(n, block_size, block_table.shape[1], n_blocks, _ptr(new_len), _ptr(cached_len), _ptr(seq_len),
-                                 _ptr(block_table), _ptr(free_ids), _ptr(n_free), _ptr(n_free_left), _ptr(query_start), _ptr(slots), n_slots,
-                                 _ptr(info), _stream(stream)))
+    _check(lib().ice_plan_blocks(n, block_size, table[1], n_blocks, new_len.data_ptr(), cached_len.data_ptr(), seq_len.data_ptr(),
+                                 block_table.data_ptr(), free_ids.data_ptr(), n_free.data_ptr(), n_free_left.data_ptr(), query_start.data_ptr(),
+                                 slots.data_ptr(), n_slots, info.data_ptr(), _stream(stream)))
 
 
 def ice_cache_write(cache: IceCacheDesc, k, v, k_stride, v_stride, slots, n_tokens, stream=None) -> None:
@@ -359,6 +366,10 @@ def ice_cache_read(cache: IceCacheDesc, n_requests, seq_len, block_table, max_bl
 
 def ice_cache_attend_bytes(cache: IceCacheDesc, group_size, n_requests, max_query, max_keys) -> int:
     return lib().ice_cache_attend_bytes(C.byref(cache), group_size, n_requests, max_query, max_keys)
+
+
+def ice_cache_attend_tokens_bytes(cache: IceCacheDesc, group_size, n_requests, max_tok) -> int:
+    return lib().ice_cache_attend_tokens_bytes(C.byref(cache), group_size, n_requests, max_tok)
 
 
 def ice_cache_attend(cache: IceCacheDesc, q, q_stride, group_size, n_requests, query_start, n_tokens, max_query, seq_len, max_keys,
@@ -616,7 +627,7 @@ def _on_stream(call):
     holds the object's arrays, whichever device and stream are current."""
     @functools.wraps(call)
     def method(self, *args, stream=None, **more):
-        if stream is None and torch.cuda.current_device() == self._index:
+        if stream is None and _current_device() == self._index:
             return call(self, *args, **more)
         with torch.cuda.device(self._index):
             if stream is None:
@@ -626,6 +637,9 @@ def _on_stream(call):
             with torch.cuda.stream(stream):
                 return call(self, *args, **more)
     return method
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us against 0.5: it does not ask whether CUDA is up)
 
 
 def _want(ok, text):
@@ -667,14 +681,12 @@ class IceBlocks:
         return self.query_start, slots, self.info
 
 
-@functools.lru_cache(maxsize=4096)
-def _attend_bytes(n_blocks, n_kv_heads, block_size, group_size, n_requests, max_query, max_keys):
-    return ice_cache_attend_bytes(make_cache_desc(None, n_blocks, n_kv_heads, block_size), group_size, n_requests, max_query, max_keys)
-
-
 class IceCache:
     """One layer's KV cache in 4 bits (see ice_cache_t in the header).  bf16 tensors may be torch.bfloat16 or int16 bit
-    patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous."""
+    patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous.
+
+    The methods of a decode step take as long on the host as on the GPU: their checks are written out, one expression each, and they call
+    the library with addresses."""
 
     def __init__(self, n_blocks, n_kv_heads, block_size=64, device="cuda", data=None):
         self.n_blocks, self.n_kv_heads, self.block_size = n_blocks, n_kv_heads, block_size
@@ -687,63 +699,91 @@ class IceCache:
               "data: contiguous uint8 %s on a GPU" % (shape,))
         self.data, self.device, self._index = data, data.device, data.device.index
         self._desc = make_cache_desc(data, n_blocks, n_kv_heads, block_size)
+        self._ref = C.byref(self._desc)
+        self._lib = lib()
+        self._bytes = {}  # workspace of an attention call by its sizes
 
-    def _rows(self, x, name, heads=None):
-        _want(x.dim() == 3 and x.shape[2] == 128 and (heads is None or x.shape[1] == heads) and x.stride(2) == 1 and
-              (x.stride(1) == 128 or x.shape[1] == 1) and x.element_size() == 2 and not x.dtype.is_complex and x.dtype is not torch.float16 and
-              x.device == self.device, "%s: bf16 [tokens, %s, 128] on the cache's device, heads and values side by side" % (name, heads or "heads"))
-        return x.data_ptr(), x.stride(0)
+    def _rows(self, x, name):
+        """Address and stride of rows [tokens, heads, 128]."""
+        shape, stride = x.shape, x.stride()
+        if not (len(shape) == 3 and shape[2] == 128 and stride[2] == 1 and (stride[1] == 128 or shape[1] == 1) and
+                (x.dtype is torch.bfloat16 or x.dtype is torch.int16) and x.get_device() == self._index):
+            raise IceError(ICE_ERR_SHAPE, "%s: bf16 [tokens, heads, 128] on the cache's device, heads and values side by side" % name)
+        return x.data_ptr(), stride[0]
 
-    def _ints(self, t, name, *shape):
-        _want(t.dtype is torch.int32 and tuple(t.shape) == shape and t.device == self.device and t.is_contiguous(),
-              "%s: contiguous int32 %s on the cache's device" % (name, list(shape)))
+    def _ints(self, t, name, shape):
+        if not (t.shape == shape and t.dtype is torch.int32 and t.is_contiguous() and t.get_device() == self._index):
+            raise IceError(ICE_ERR_SHAPE, "%s: contiguous int32 %s on the cache's device" % (name, list(shape)))
         return t.data_ptr()
 
     def _table(self, seq_len, block_table):
-        n = seq_len.shape[0]
-        _want(block_table.dim() == 2, "block_table: [requests, max_blocks]")
-        return n, self._ints(seq_len, "seq_len", n), self._ints(block_table, "block_table", n, block_table.shape[1]), block_table.shape[1]
+        n, shape = seq_len.shape[0], block_table.shape
+        if len(shape) != 2 or shape[0] != n:
+            raise IceError(ICE_ERR_SHAPE, "block_table: [%d requests, max_blocks]" % n)
+        return n, self._ints(seq_len, "seq_len", (n,)), self._ints(block_table, "block_table", shape), shape[1]
 
     @_on_stream
     def write(self, k, v, slots):
         """k, v [tokens, n_kv_heads, 128] into their slots [tokens]; -1 is left out."""
-        kp, ks = self._rows(k, "k", self.n_kv_heads)
-        vp, vs = self._rows(v, "v", self.n_kv_heads)
-        _want(k.shape[0] == v.shape[0], "k and v: as many tokens")
-        ice_cache_write(self._desc, kp, vp, ks, vs, self._ints(slots, "slots", k.shape[0]), k.shape[0])
+        kp, ks = self._rows(k, "k")
+        vp, vs = self._rows(v, "v")
+        n = k.shape[0]
+        if k.shape != v.shape or k.shape[1] != self.n_kv_heads:
+            raise IceError(ICE_ERR_SHAPE, "k and v: [tokens, %d, 128]" % self.n_kv_heads)
+        _check(self._lib.ice_cache_write(self._ref, kp, vp, ks, vs, self._ints(slots, "slots", (n,)), n, _stream_on(self._index)))
 
     @_on_stream
     def read(self, block_table, seq_len, n_rows, first=None, out=None):
         """(K, V) bf16 [requests, n_kv_heads, n_rows, 128]: the tokens from position first[s] on, as they are held."""
         n, sp, tp, width = self._table(seq_len, block_table)
         if first is not None:
-            first = self._ints(first, "first", n)
+            first = self._ints(first, "first", (n,))
+        shape = (n, self.n_kv_heads, n_rows, 128)
         if out is None:
-            out = tuple(torch.empty((n, self.n_kv_heads, n_rows, 128), dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        K, V = out
-        for x in out:
-            _want(tuple(x.shape) == (n, self.n_kv_heads, n_rows, 128) and x.element_size() == 2 and x.is_contiguous() and x.device == self.device,
-                  "out: two contiguous bf16 tensors [requests, n_kv_heads, n_rows, 128]")
-        ice_cache_read(self._desc, n, sp, tp, width, first, n_rows, K, V)
+            K = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            V = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        else:
+            K, V = out
+            for x in out:
+                _want(x.shape == shape and x.element_size() == 2 and x.is_contiguous() and x.get_device() == self._index,
+                      "out: two contiguous bf16 tensors %s" % (shape,))
+        _check(self._lib.ice_cache_read(self._ref, n, sp, tp, width, first, n_rows, K.data_ptr(), V.data_ptr(), _stream_on(self._index)))
         return K, V
 
     def _outputs(self, q, out, out_dtype, lse, with_lse):
+        """(out, lse, its address, type of out)"""
         shape = q.shape
         if out is None:
             out = torch.empty(shape, dtype=out_dtype, device=self.device)
-        _want(out.shape == shape and out.is_contiguous() and out.device == self.device and out.dtype in (torch.float32, torch.bfloat16),
-              "out: contiguous float32 or bfloat16 %s" % (tuple(shape),))
-        if lse is None and with_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+        elif not (out.shape == shape and out.is_contiguous() and out.get_device() == self._index):
+            raise IceError(ICE_ERR_SHAPE, "out: contiguous %s on the cache's device" % (tuple(shape),))
+        kind = ICE_OUT_F32 if out.dtype is torch.float32 else ICE_OUT_BF16 if out.dtype is torch.bfloat16 else -1
         if lse is not None:
-            _want(lse.shape == shape[:2] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.device == self.device,
-                  "lse: contiguous float32 %s" % (tuple(shape[:2]),))
-        return out, lse, ICE_OUT_F32 if out.dtype is torch.float32 else ICE_OUT_BF16
+            if not (lse.shape == shape[:2] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == self._index):
+                raise IceError(ICE_ERR_SHAPE, "lse: contiguous float32 %s on the cache's device" % (tuple(shape[:2]),))
+        elif with_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+        return out, lse, None if lse is None else lse.data_ptr(), kind
+
+    def _workspace(self, size_of, *sizes):
+        """(address, bytes, tensor) of the scratch of this call alone: it comes from torch's allocator each time (under capture from the
+        graph's own pool), so that calls on other streams and other graphs never share it."""
+        nbytes = self._bytes.get(sizes)
+        if nbytes is None:
+            if len(self._bytes) >= 4096:
+                self._bytes.clear()
+            nbytes = self._bytes[sizes] = size_of(self._ref, *sizes)
+        if nbytes == 0:
+            return None, 0, None
+        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return work.data_ptr(), nbytes, work
 
     def _group(self, q):
         qp, qs = self._rows(q, "q")
-        _want(q.shape[1] % self.n_kv_heads == 0, "q: a multiple of %d heads" % self.n_kv_heads)
-        return qp, qs, q.shape[1] // self.n_kv_heads
+        group, rest = divmod(q.shape[1], self.n_kv_heads)
+        if rest:
+            raise IceError(ICE_ERR_SHAPE, "q: a multiple of %d heads" % self.n_kv_heads)
+        return qp, qs, group
 
     @_on_stream
     def attend(self, q, query_start, seq_len, block_table, max_query=None, max_len=None, window=0, out=None, out_dtype=torch.float32,
@@ -754,14 +794,14 @@ class IceCache:
         qp, qs, group = self._group(q)
         n, sp, tp, width = self._table(seq_len, block_table)
         tokens = q.shape[0]
-        out, lse, out_type = self._outputs(q, out, out_dtype, lse, with_lse)
+        out, lse, lp, kind = self._outputs(q, out, out_dtype, lse, with_lse)
         if tokens:
             max_query = tokens if max_query is None else min(max_query, tokens)
-            max_len = width * self.block_size if max_len is None else max_len
-            nbytes = _attend_bytes(self.n_blocks, self.n_kv_heads, self.block_size, group, n, max_query, max_len)
-            work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
-            ice_cache_attend(self._desc, qp, qs, group, n, self._ints(query_start, "query_start", n + 1), tokens, max_query, sp, max_len, tp,
-                             width, window, out, out_type, lse, work, nbytes)
+            if max_len is None:
+                max_len = width * self.block_size
+            wp, nbytes, work = self._workspace(self._lib.ice_cache_attend_bytes, group, n, max_query, max_len)
+            _check(self._lib.ice_cache_attend(self._ref, qp, qs, group, n, self._ints(query_start, "query_start", (n + 1,)), tokens, max_query, sp,
+                                              max_len, tp, width, window, out.data_ptr(), kind, lp, wp, nbytes, _stream_on(self._index)))
         return out if lse is None else (out, lse)
 
     @_on_stream
@@ -770,11 +810,12 @@ class IceCache:
         IceIndex.selected_tokens gives them."""
         qp, qs, group = self._group(q)
         n, sp, tp, width = self._table(seq_len, block_table)
-        _want(q.shape[0] == n, "q: one row per request")
-        most = token_pos.shape[-1]
-        pp, np_ = self._ints(token_pos, "token_pos", n, self.n_kv_heads, most), self._ints(n_tok, "n_tok", n, self.n_kv_heads)
-        out, lse, out_type = self._outputs(q, out, out_dtype, lse, with_lse)
-        nbytes = _attend_bytes(self.n_blocks, self.n_kv_heads, self.block_size, group, n, 1, most)
-        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
-        ice_cache_attend_tokens(self._desc, qp, qs, group, n, sp, tp, width, pp, np_, most, out, out_type, lse, work, nbytes)
+        if q.shape[0] != n:
+            raise IceError(ICE_ERR_SHAPE, "q: one row per request")
+        most, heads = token_pos.shape[-1], self.n_kv_heads
+        pp, np_ = self._ints(token_pos, "token_pos", (n, heads, most)), self._ints(n_tok, "n_tok", (n, heads))
+        out, lse, lp, kind = self._outputs(q, out, out_dtype, lse, with_lse)
+        wp, nbytes, work = self._workspace(self._lib.ice_cache_attend_tokens_bytes, group, n, most)
+        _check(self._lib.ice_cache_attend_tokens(self._ref, qp, qs, group, n, sp, tp, width, pp, np_, most, out.data_ptr(), kind, lp, wp,
+                                                 nbytes, _stream_on(self._index)))
         return out if lse is None else (out, lse)

@@ -434,7 +434,7 @@ ice_status_t ice_plan_blocks(int32_t n_requests, int32_t block_size, int32_t max
         return fail(ICE_ERR_INVALID_ARG, "a pointer is null");
     if (block_size != 16 && block_size != 32 && block_size != 64)
         return fail(ICE_ERR_UNSUPPORTED, "block_size %d: only 16, 32, 64 are supported", block_size);
-    if (n_requests < 1 || n_requests > 65535) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, 65535]", n_requests);
+    if (n_requests < 1 || n_requests > kPlanRequests) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, %d]", n_requests, kPlanRequests);
     if (n_slots < 1 || n_slots > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_slots %d is outside [1, 2^30]", n_slots);
     if (n_blocks < 1 || (long long)n_blocks * block_size >= 2147483648ll)
         return fail(ICE_ERR_SHAPE, "n_blocks %d: at least 1, and fewer than 2^31 slots", n_blocks);
@@ -476,8 +476,8 @@ ice_status_t ice_cache_read(const ice_cache_t *c, int32_t n_requests, const int3
 }
 
 // the sizes that say how an attention call is cut
-static ice_status_t plan_attend(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_query, int32_t max_keys, CacheAttend &a,
-                                size_t *bytes) {
+static ice_status_t plan_attend(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_query, int32_t max_keys, bool listed,
+                                CacheAttend &a, size_t *bytes) {
     if (ice_status_t st = check_cache(c)) return st;
     if (G < 1 || G > 16) return fail(ICE_ERR_UNSUPPORTED, "group_size %d: only 1 to 16 are supported", G);
     if (n_requests < 1 || n_requests > 65535) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, 65535]", n_requests);
@@ -489,14 +489,20 @@ static ice_status_t plan_attend(const ice_cache_t *c, int32_t G, int32_t n_reque
     a.max_query = max_query;
     a.max_keys = max_keys;
     a.scale_log2 = 0.12751743f;  // log2(e) / sqrt(128)
-    *bytes = plan_cache_attend(a);
+    *bytes = plan_cache_attend(a, listed);
     return ICE_OK;
 }
 
 size_t ice_cache_attend_bytes(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_query, int32_t max_keys) {
     CacheAttend a{};
     size_t bytes = 0;
-    return plan_attend(c, G, n_requests, max_query, max_keys, a, &bytes) == ICE_OK ? bytes : 0;
+    return plan_attend(c, G, n_requests, max_query, max_keys, false, a, &bytes) == ICE_OK ? bytes : 0;
+}
+
+size_t ice_cache_attend_tokens_bytes(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t max_tok) {
+    CacheAttend a{};
+    size_t bytes = 0;
+    return plan_attend(c, G, n_requests, 1, max_tok, true, a, &bytes) == ICE_OK ? bytes : 0;
 }
 
 static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
@@ -533,7 +539,7 @@ ice_status_t ice_cache_attend(const ice_cache_t *c, const void *q, int64_t q_str
     if (window < 0) return fail(ICE_ERR_SHAPE, "window must be >= 0 (0: no window)");
     CacheAttend a{};
     size_t need = 0;
-    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, a, &need)) return st;
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, false, a, &need)) return st;
     if (n_tokens == 0) return ICE_OK;
     a.T = n_tokens;
     a.query_start = query_start;
@@ -553,7 +559,7 @@ ice_status_t ice_cache_attend_tokens(const ice_cache_t *c, const void *q, int64_
     if (!pos || !n_tok) return fail(ICE_ERR_INVALID_ARG, "token_pos or n_tok is null");
     CacheAttend a{};
     size_t need = 0;
-    if (ice_status_t st = plan_attend(c, G, n_requests, 1, max_tok, a, &need)) return st;
+    if (ice_status_t st = plan_attend(c, G, n_requests, 1, max_tok, true, a, &need)) return st;
     a.T = n_requests;
     a.seq_len = seq_len;
     a.table = table;

@@ -28,12 +28,19 @@ struct CachePlan {
     int n_slots;
     int *info;
 };
+constexpr int kPlanRequests = 8192;  // of one plan at most: three sums each in LDS
 void launch_cache_plan(const CachePlan &p, hipStream_t stream);
 
 void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, long long k_stride, long long v_stride, const int *slots,
                         int n_tokens, hipStream_t stream);
 void launch_cache_read(const CacheDims &c, int n_requests, const int *seq_len, const int *table, int max_blocks, const int *first,
                        int n_rows, bf16_t *k, bf16_t *v, hipStream_t stream);
+
+// A (request, KV head) that was cut between workgroups: the first one of them, the KV head, the request's first query row, the first of the
+// unit's rows and the number of the request's rows (query, head of the group).  
+struct alignas(16) MergeNote {
+    int first, h, row0, base, rows;
+};
 
 struct CacheAttend {
     CacheDims c;
@@ -43,17 +50,19 @@ struct CacheAttend {
     const int *pos, *n_tok;  // listed tokens (then one query per request), or null
     void *out;
     float *lse, *part;
-    int4 *notes;
+    MergeNote *notes;
     int S, T, G, max_query, max_blocks, max_keys, window;
     int rows;                     // query rows (query, head of the group) that a record has room for
     int few_groups, many_groups;  // workgroups of the kernel for few queries a request, of the one for many
     bool many;                    // some request may have more query rows than the first one takes
+    int per_unit;       // > 0: nominal pieces of every (request, KV head); 0: by the lengths
+    bool whole;         // one workgroup each
     int first, n_here;  // the launch's requests
     float scale_log2;
     bool out_bf16;
 };
-// How a call is cut, from the sizes: fills few_groups, many_groups and many; returns the bytes of workspace.
-size_t plan_cache_attend(CacheAttend &a);
+// How a call is cut, from the sizes: fills few_groups, many_groups, many, per_unit and whole; returns the bytes of workspace.
+size_t plan_cache_attend(CacheAttend &a, bool listed);
 void launch_cache_attend(CacheAttend a, hipStream_t stream);
 
 }  // namespace ice

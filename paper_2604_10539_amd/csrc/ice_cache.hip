@@ -1,4 +1,6 @@
 // The 4-bit sequence cache: block tables and slots of a step, writing rows as codes and scales, reading them back.
+#include <algorithm>
+
 #include "ice_cache.h"
 
 namespace ice {
@@ -9,9 +11,11 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------------------------------------ block tables and slots
-// One workgroup: requests are scanned 1024 at a time (sums of new tokens, blocks taken and blocks given back), blocks given
-// back are pushed on the free stack, then those taken are popped.  Everything is read before anything is written that it
-// may share memory with, so lengths and the stack's height may be updated in place.
+// Every workgroup scans all requests (sums of new tokens, blocks taken, blocks given back, kept in LDS) and does its share of the
+// rest: a block given back, a block taken and a slot each find their request by bisection and read one id.  A taken block that the
+// same call gives back is read from the row it comes from, not from the stack, so nothing waits for anything and the workgroups are
+// independent.  What may be updated in place, the lengths and the stack's height, is written last: by the workgroup itself where there
+// is one, else by a second launch.  Bound by latency: a trip for the lengths, the scan, a trip for the ids.
 constexpr int kPlanThreads = 1024;
 constexpr unsigned kPlanMost = 0x7FFFFFFFu;  // sums stop here: they only have to be known exactly where the step is possible
 
@@ -19,38 +23,57 @@ enum { kPlanErrFree = 1, kPlanErrRow = 2, kPlanErrSlots = 4, kPlanErrLen = 8 };
 
 struct PlanItem {
     unsigned fresh, take, back;  // new tokens, blocks taken, blocks given back
-    int held, err;               // blocks before the step
-};
-
-__device__ inline PlanItem plan_item(const CachePlan &p, int i, int &after) {
-    PlanItem x = {0, 0, 0, 0, 0};
-    after = 0;
-    if (i >= p.n_requests) return x;
-    const long long cap = (long long)p.max_blocks << p.block_shift;
-    const long long cached = p.cached_len[i], gain = p.new_len[i];
-    if (cached < 0 || cached > cap) {
-        x.err = kPlanErrLen;
-        return x;
+    int held, need, after, err;  // blocks before the step and after it, length after it
+    __device__ PlanItem(const CachePlan &p, int i) : fresh(0), take(0), back(0), held(0), need(0), after(0), err(0) {
+        const long long cap = (long long)p.max_blocks << p.block_shift;
+        const long long cached = p.cached_len[i], gain = p.new_len[i];
+        if (cached < 0 || cached > cap) {
+            err = kPlanErrLen;
+            return;
+        }
+        const long long len = max(cached + gain, 0ll), up = (1ll << p.block_shift) - 1;
+        if (len > cap) err = kPlanErrRow;
+        held = (int)((cached + up) >> p.block_shift);
+        need = (int)((len + up) >> p.block_shift);
+        fresh = (unsigned)max(gain, 0ll);
+        take = (unsigned)max(need - held, 0);
+        back = (unsigned)max(held - need, 0);
+        after = (int)min(len, (long long)kPlanMost);
     }
-    const long long len = max(cached + gain, 0ll);
-    if (len > cap) x.err = kPlanErrRow;
-    const long long up = (1ll << p.block_shift) - 1;
-    x.held = (int)((cached + up) >> p.block_shift);
-    const int need = (int)((len + up) >> p.block_shift);
-    x.fresh = (unsigned)max(gain, 0ll);
-    x.take = (unsigned)max(need - x.held, 0);
-    x.back = (unsigned)max(x.held - need, 0);
-    after = (int)len;
-    return x;
-}
+};
 
 __device__ inline unsigned sat_add(unsigned a, unsigned b) { return min(a + b, kPlanMost); }
 
-// Exclusive sums of (fresh, take, back) over the workgroup's threads; totals in tot.
-__device__ inline void plan_scan(PlanItem &x, unsigned (*sums)[3], unsigned (&tot)[3]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    unsigned v[3] = {x.fresh, x.take, x.back};
-    const unsigned own[3] = {x.fresh, x.take, x.back};
+// Index of the last entry of sums[0 .. n] that is at most k < sums[n]: entries that add nothing share a sum with the next.
+__device__ inline int plan_owner(const unsigned *sums, int n, unsigned k) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid] <= k) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
+    extern __shared__ unsigned plan_lds[];
+    const int n = p.n_requests, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    unsigned *sums[3] = {plan_lds, plan_lds + (n + 1), plan_lds + 2 * (n + 1)};  // before each request: fresh, take, back
+    __shared__ unsigned s_wave[kPlanThreads / 64][3];
+    __shared__ int s_err;
+    if (tid == 0) s_err = 0;
+    const int n_free = *p.n_free;
+    const int each = (n + kPlanThreads - 1) / kPlanThreads, i0 = min(tid * each, n), i1 = min(i0 + each, n);
+    unsigned own[3] = {0, 0, 0};
+    int err = 0;
+    for (int i = i0; i < i1; ++i) {
+        const PlanItem x(p, i);
+        own[0] = sat_add(own[0], x.fresh);
+        own[1] = sat_add(own[1], x.take);
+        own[2] = sat_add(own[2], x.back);
+        err |= x.err;
+    }
+    unsigned v[3] = {own[0], own[1], own[2]}, total[3] = {0, 0, 0};
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
 #pragma unroll
@@ -58,140 +81,82 @@ __device__ inline void plan_scan(PlanItem &x, unsigned (*sums)[3], unsigned (&to
             const unsigned o = (unsigned)__shfl_up((int)v[k], d);
             if (lane >= d) v[k] = sat_add(v[k], o);
         }
-    __syncthreads();  // (the last scan's sums have been read)
     if (lane == 63)
-        for (int k = 0; k < 3; ++k) sums[wave][k] = v[k];
+        for (int k = 0; k < 3; ++k) s_wave[wave][k] = v[k];
     __syncthreads();
-    unsigned before[3] = {0, 0, 0};
-    for (int k = 0; k < 3; ++k) tot[k] = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w)
-        for (int k = 0; k < 3; ++k) {
-            if (w == wave) before[k] = tot[k];
-            tot[k] = sat_add(tot[k], sums[w][k]);
-        }
-    // (own is at most the inclusive sum; where that stopped at the limit the step is refused and the sums are not used)
-    x.fresh = sat_add(before[0], v[0] - min(v[0], own[0]));
-    x.take = sat_add(before[1], v[1] - min(v[1], own[1]));
-    x.back = sat_add(before[2], v[2] - min(v[2], own[2]));
-}
-
-// Slot of the step's token k, whose request is the last one with start <= k (requests without new tokens share a start).
-template <typename Start>
-__device__ inline int plan_slot(const CachePlan &p, int k, Start start) {
-    if (k >= start(p.n_requests)) return -1;
-    int lo = 0, hi = p.n_requests;  // start(lo) <= k < start(hi)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start(mid) <= k) lo = mid;
-        else hi = mid;
-    }
-    const int at = p.seq_len[lo] - (start(lo + 1) - k);
-    const int id = p.table[(size_t)lo * p.max_blocks + (at >> p.block_shift)];
-    return (id << p.block_shift) + (at & ((1 << p.block_shift) - 1));
-}
-
-constexpr int kPlanSlotsHere = 4096;  // so many slots are filled by the planning workgroup itself, without a second launch
-
-__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
-    __shared__ unsigned sums[kPlanThreads / 64][3];
-    __shared__ int s_err;
-    const int tid = threadIdx.x;
-    if (tid == 0) s_err = 0;
-    const int n_free = *p.n_free;
-    const int rounds = (p.n_requests + kPlanThreads - 1) / kPlanThreads;
-    unsigned total[3] = {0, 0, 0}, tot[3];
-    int err = 0, after;
-    __syncthreads();
-    for (int r = 0; r < rounds; ++r) {
-        PlanItem x = plan_item(p, r * kPlanThreads + tid, after);
-        err |= x.err;
-        plan_scan(x, sums, tot);
-        for (int k = 0; k < 3; ++k) total[k] = sat_add(total[k], tot[k]);
-    }
     if (err) atomicOr(&s_err, err);
+    unsigned at[3];
+    for (int k = 0; k < 3; ++k) {
+        at[k] = v[k] - min(v[k], own[k]);  // (where a sum stopped at the limit the step is refused and no sum is used)
+        for (int w = 0; w < kPlanThreads / 64; ++w) {
+            if (w == wave) at[k] = sat_add(at[k], total[k]);
+            total[k] = sat_add(total[k], s_wave[w][k]);
+        }
+    }
+    for (int i = i0; i < i1; ++i) {
+        const PlanItem x(p, i);
+        const unsigned more[3] = {x.fresh, x.take, x.back};
+        for (int k = 0; k < 3; ++k) {
+            sums[k][i] = at[k];
+            at[k] = sat_add(at[k], more[k]);
+        }
+    }
+    if (tid < 3) sums[tid][n] = total[tid];
     __syncthreads();
     err = s_err;
-    if (n_free < 0 || n_free > p.n_blocks || total[2] > (unsigned)p.n_blocks || n_free + (int)total[2] > p.n_blocks) err |= kPlanErrLen;
-    else if (total[1] > (unsigned)n_free + total[2]) err |= kPlanErrFree;
-    if (total[0] > (unsigned)p.n_slots) err |= kPlanErrSlots;
-    // a group of threads per request copies its blocks: all of them where there are few requests, a wave where there are many
-    const int group = p.n_requests >= 16 ? 64 : p.n_requests >= 4 ? 256 : kPlanThreads;
-    const int groups = kPlanThreads / group, mine = tid / group, at = tid % group;
-    __shared__ int s_base[kPlanThreads], s_from[kPlanThreads], s_n[kPlanThreads];
+    const unsigned fresh = total[0], taken = total[1], back = total[2];
+    if (n_free < 0 || n_free > p.n_blocks || back > (unsigned)p.n_blocks || n_free + (int)back > p.n_blocks) err |= kPlanErrLen;
+    else if (taken > (unsigned)n_free + back) err |= kPlanErrFree;
+    if (fresh > (unsigned)p.n_slots) err |= kPlanErrSlots;
+
+    const unsigned step = gridDim.x * kPlanThreads, first = blockIdx.x * kPlanThreads + tid;
     if (!err) {
-        const int height = n_free + (int)total[2];
-        unsigned done = 0;
-        for (int r = 0; total[2] && r < rounds; ++r) {  // pushes
-            PlanItem x = plan_item(p, r * kPlanThreads + tid, after);
-            const unsigned back = x.back;
-            plan_scan(x, sums, tot);
-            s_base[tid] = n_free + (int)(done + x.back);
-            s_from[tid] = x.held - (int)back;
-            s_n[tid] = (int)back;
-            __syncthreads();
-            for (int i = mine; i < kPlanThreads; i += groups)
-                for (int b = at; b < s_n[i]; b += group)
-                    p.free_ids[s_base[i] + b] = p.table[(size_t)(r * kPlanThreads + i) * p.max_blocks + s_from[i] + b];
-            done += tot[2];
-        }
-        __threadfence_block();
-        __syncthreads();
-        unsigned taken = 0, fresh = 0;
-        for (int r = 0; r < rounds; ++r) {  // pops, lengths, starts
-            const int i0 = r * kPlanThreads + tid;
-            PlanItem x = plan_item(p, i0, after);
-            const unsigned take = x.take;
-            plan_scan(x, sums, tot);
-            if (i0 < p.n_requests) {
-                p.seq_len[i0] = after;
-                p.query_start[i0] = (int)(fresh + x.fresh);
+        auto given_back = [&](unsigned k) {  // id of the k-th block given back
+            const int s = plan_owner(sums[2], n, k);
+            return p.table[(size_t)s * p.max_blocks + PlanItem(p, s).need + (k - sums[2][s])];
+        };
+        auto popped = [&](unsigned k) {  // id of the k-th block taken
+            const unsigned place = (unsigned)n_free + back - 1 - k;
+            return place < (unsigned)n_free ? p.free_ids[place] : given_back(place - (unsigned)n_free);
+        };
+        for (unsigned k = first; k < (unsigned)p.n_slots; k += step) {
+            int slot = -1;
+            if (k < fresh) {
+                const int s = plan_owner(sums[0], n, k);
+                const PlanItem x(p, s);
+                const int pos = x.after - (int)(sums[0][s + 1] - k), j = pos >> p.block_shift;
+                const int id = j < x.held ? p.table[(size_t)s * p.max_blocks + j] : popped(sums[1][s] + (unsigned)(j - x.held));
+                if (id >= 0 && id < p.n_blocks) slot = (id << p.block_shift) + (pos & ((1 << p.block_shift) - 1));
             }
-            s_base[tid] = height - 1 - (int)(taken + x.take);
-            s_from[tid] = x.held;
-            s_n[tid] = (int)take;
-            __syncthreads();
-            for (int i = mine; i < kPlanThreads; i += groups)
-                for (int b = at; b < s_n[i]; b += group)
-                    p.table[(size_t)(r * kPlanThreads + i) * p.max_blocks + s_from[i] + b] = p.free_ids[s_base[i] - b];
-            taken += tot[1];
-            fresh += tot[0];
+            p.slots[k] = slot;
         }
+        for (unsigned k = first; k < taken; k += step) {
+            const int s = plan_owner(sums[1], n, k);
+            p.table[(size_t)s * p.max_blocks + PlanItem(p, s).held + (k - sums[1][s])] = popped(k);
+        }
+        for (unsigned k = first; k < back; k += step) p.free_ids[(unsigned)n_free + k] = given_back(k);
     } else {
-        for (int i = tid; i < p.n_requests; i += kPlanThreads) {
-            p.seq_len[i] = p.cached_len[i];
-            p.query_start[i] = 0;
+        for (unsigned k = first; k < (unsigned)p.n_slots; k += step) p.slots[k] = -1;
+    }
+    if (blockIdx.x == 0) {
+        for (int i = tid; i <= n; i += kPlanThreads) p.query_start[i] = err ? 0 : (int)sums[0][i];
+        if (tid == 0) {
+            p.info[0] = err ? 0 : (int)fresh;
+            p.info[1] = err ? 0 : (int)taken;
+            p.info[2] = err ? 0 : (int)back;
+            p.info[3] = err;
         }
-        total[0] = total[1] = total[2] = 0;
     }
-    if (tid == 0) {
-        p.query_start[p.n_requests] = (int)total[0];
-        *p.n_free_left = n_free + (int)total[2] - (int)total[1];
-        p.info[0] = (int)total[0];
-        p.info[1] = (int)total[1];
-        p.info[2] = (int)total[2];
-        p.info[3] = err;
-    }
-    if (p.n_slots <= kPlanSlotsHere) {
-        __threadfence_block();
-        __syncthreads();
-        for (int k = tid; k < p.n_slots; k += kPlanThreads) p.slots[k] = plan_slot(p, k, [&](int i) { return p.query_start[i]; });
-    }
+    if (gridDim.x > 1) return;
+    __syncthreads();  // (the lengths have been read)
+    for (int i = tid; i < n; i += kPlanThreads) p.seq_len[i] = err ? p.cached_len[i] : PlanItem(p, i).after;
+    if (tid == 0) *p.n_free_left = err ? n_free : n_free + (int)back - (int)taken;
 }
 
-constexpr int kPlanStarts = 4096;  // starts that fit the workgroup's copy
-
-__global__ __launch_bounds__(256) void cache_slots_kernel(CachePlan p) {
-    __shared__ int starts[kPlanStarts + 1];
-    const bool here = p.n_requests <= kPlanStarts;
-    if (here)
-        for (int i = threadIdx.x; i <= p.n_requests; i += 256) starts[i] = p.query_start[i];
-    __syncthreads();
-    const long long k0 = (long long)blockIdx.x * 1024 + threadIdx.x;
-    for (int j = 0; j < 4; ++j) {
-        const long long k = k0 + 256 * j;
-        if (k >= p.n_slots) return;
-        p.slots[k] = here ? plan_slot(p, (int)k, [&](int i) { return starts[i]; }) : plan_slot(p, (int)k, [&](int i) { return p.query_start[i]; });
-    }
+__global__ __launch_bounds__(256) void cache_plan_end_kernel(CachePlan p) {
+    const int i = blockIdx.x * 256 + threadIdx.x, err = p.info[3];
+    if (i < p.n_requests) p.seq_len[i] = err ? p.cached_len[i] : PlanItem(p, i).after;
+    if (i == 0) *p.n_free_left = *p.n_free + p.info[2] - p.info[1];
 }
 
 // ----------------------------------------------------------------------------------------------------------------- write
@@ -295,9 +260,15 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDims c, int n_requ
 
 }  // namespace
 
+// One workgroup where a step moves little (a decode step: 16 requests 5 us; with a second launch 9), else up to 64: 1000 requests, 100k new tokens and
+// 50k blocks given back, 41 us by one workgroup.
 void launch_cache_plan(const CachePlan &p, hipStream_t stream) {
-    cache_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p);
-    if (p.n_slots > kPlanSlotsHere) cache_slots_kernel<<<(p.n_slots + 1023) / 1024, 256, 0, stream>>>(p);
+    const long long most = p.n_slots + std::min<long long>((long long)p.n_requests * p.max_blocks, p.n_blocks);
+    const int groups = most <= 16384 ? 1 : (int)std::min<long long>(64, (most + 8191) / 8192);
+    const size_t lds = 3 * (p.n_requests + 1) * sizeof(unsigned);
+    if (lds > 65536 - 1024) allow_dynamic_lds((const void *)cache_plan_kernel, lds);
+    cache_plan_kernel<<<groups, kPlanThreads, lds, stream>>>(p);
+    if (groups > 1) cache_plan_end_kernel<<<(p.n_requests + 255) / 256, 256, 0, stream>>>(p);
 }
 
 void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, long long k_stride, long long v_stride, const int *slots,

@@ -182,22 +182,23 @@ __device__ inline void find_nan(const CacheAttend &a, const int *table, int h, i
 // cuts fall.  Lengths are device values and ragged; so no workgroup is idle while another has more to read.  Every workgroup finds its
 // piece from the lengths.  The part of a (request, KV head) that does not span it leaves its sums in a record; the workgroup
 // whose piece holds the end of one that was cut notes it for the merge.
-template <int PACK, int NT, int SETS, bool LIST>
-__global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
+template <int W, int PACK, int NT, int SETS, bool LIST>
+__global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
     static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
     constexpr int R = kRows / PACK;  // rows in a tile of columns
-    __shared__ float s_acc[kWaves][kRows][kRecord];
-    __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of 128 keys before each request
-    __shared__ unsigned s_wave[kWaves];
+    constexpr int Q = W * kStep;     // keys of a step of all waves
+    __shared__ float s_acc[W][kRows][kRecord];
+    __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of Q keys before each request
+    __shared__ unsigned s_wave[W];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
     const int term = PACK == 1 ? 0 : c / R, col_row = PACK == 1 ? c : c % R;
 
     unsigned total = 0;
-    const unsigned per_list = (unsigned)(a.max_keys + kQuantum - 1) / kQuantum;
-    if constexpr (LIST) {
-        total = (unsigned)a.n_here * a.c.H * per_list;
+    const bool even = LIST || a.per_unit > 0;  // units of equal nominal length: no need to look at the lengths
+    if (even) {
+        total = (unsigned)a.n_here * a.c.H * (unsigned)a.per_unit;
     } else {
-        for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
+        for (int e0 = 0; e0 < a.n_here; e0 += W * 64) {
             const int e = e0 + tid;
             unsigned n = 0;
             if (e < a.n_here) {
@@ -205,14 +206,14 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
                 const int q = u.queries(a);
                 // at least one where there are rows, which want their outputs; none where the other kernel does the request
                 if (q > 0 && q * a.G <= NT * R)
-                    n = (unsigned)max((u.high(q - 1) + kQuantum - 1) / kQuantum - u.low(a, 0) / kQuantum, 1) * (unsigned)a.c.H;
+                    n = (unsigned)max((u.high(q - 1) + Q - 1) / Q - u.low(a, 0) / Q, 1) * (unsigned)a.c.H;
             }
             const unsigned incl = (unsigned)wave_scan_add((int)n);
             if (lane == 63) s_wave[wave] = incl;
             __syncthreads();
             unsigned before = total;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < W; ++w) {
                 if (w < wave) before += s_wave[w];
                 total += s_wave[w];
             }
@@ -224,13 +225,13 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
     }
     const Pieces pieces(total, gridDim.x);
     if (blockIdx.x >= pieces.groups || total == 0) {
-        if (tid == 0) a.notes[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (tid == 0 && a.notes) a.notes[blockIdx.x].first = -1;
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    int4 note = make_int4(-1, 0, 0, 0);
+    MergeNote note = {-1, 0, 0, 0, 0};
     int entry = 0;
-    if constexpr (!LIST) {  // the last request that begins at or before the piece (of those, the one that is not empty)
+    if (!even) {  // the last request that begins at or before the piece (of those, the one that is not empty)
         for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
             if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
     }
@@ -242,12 +243,12 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
     for (unsigned now = begin; now < end;) {
         int s, h;
         unsigned u0, u1;
-        if constexpr (LIST) {
-            const unsigned u = now / per_list;
+        if (even) {
+            const unsigned u = now / (unsigned)a.per_unit;
             s = (int)(u / (unsigned)a.c.H);
             h = (int)(u % (unsigned)a.c.H);
-            u0 = u * per_list;
-            u1 = u0 + per_list;
+            u0 = u * (unsigned)a.per_unit;
+            u1 = u0 + (unsigned)a.per_unit;
         } else {
             while (s_before[entry + 1] <= now) ++entry;
             const unsigned first = s_before[entry], per = (s_before[entry + 1] - first) / (unsigned)a.c.H;
@@ -261,10 +262,15 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
         const unsigned stop = min(u1, end);
         const Unit<LIST> unit(a, s, h);
         const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
+        if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
+            now = stop;
+            continue;
+        }
         // keys of this part that any row sees, that every row sees, that this lane's rows see
-        const int q0 = unit.low(a, 0) / kQuantum;
-        const int from = max(unit.low(a, 0), (q0 + (int)(now - u0)) * kQuantum);
-        const int to = min(unit.high(t_last), (q0 + (int)(stop - u0)) * kQuantum);
+        const int q0 = unit.low(a, 0) / Q;
+        const int from = max(unit.low(a, 0), (q0 + (int)(now - u0)) * Q);
+        // (the last part takes its keys to the end, whatever the nominal length)
+        const int to = stop == u1 ? unit.high(t_last) : min(unit.high(t_last), (q0 + (int)(stop - u0)) * Q);
         const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(0), to);
         int low[NT], high[NT];
         u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
@@ -277,31 +283,55 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
-        const int step0 = (q0 + (int)(now - u0)) * kWaves;  // the wave's steps: step0 + wave + kWaves n
-        const int n_mine = to > from ? max((to - kStep * (step0 + wave) + kQuantum - 1) / kQuantum, 0) : 0;
+        const int step0 = (q0 + (int)(now - u0)) * W;  // the wave's steps: step0 + wave + W n
+        const int n_mine = to > from ? max((to - kStep * (step0 + wave) + Q - 1) / Q, 0) : 0;
         const int *table = a.table + (size_t)s * a.max_blocks;
         const int *list = LIST ? a.pos + ((size_t)s * a.c.H + h) * a.max_keys : nullptr;
 
-        // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n0 + l / 2, in units of tiles of the pool.  Listed:
-        // index of key l & 31 of step n0 + l / 32, in units of rows of the pool.  -1: no such place.
-        auto places = [&](int n0) __attribute__((always_inline)) -> int {
+        // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n + l / 2, in units of tiles of the pool.  Listed:
+        // index of key l & 31 of step n + l / 32, in units of rows of the pool.  -1: no such place.  A list's positions are
+        // looked up two lots ahead, its blocks one lot, so that neither trip is waited for but at the start (16 requests x 8 heads x 1024 tokens:
+        // 14.4 us, 17.6 without; a dense lot lasts 32 steps, and a register more costs as much as its wait).
+        constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
+        auto position = [&](int n) __attribute__((always_inline)) -> int {  // listed
+            const long long e = (long long)(step0 + wave + W * (n + (lane >> 5))) * kStep + (lane & 31);
+            const int p = e < to ? list[e] : -1;
+            return p < unit.tokens ? p : -1;
+        };
+        auto block_of = [&](int p) __attribute__((always_inline)) -> int { return p >= 0 ? table[p >> (a.c.tile_shift + 4)] : -1; };
+        auto row_of = [&](int p, int id) __attribute__((always_inline)) -> int {
+            return (unsigned)id < (unsigned)a.c.n_blocks
+                       ? (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15)) : -1;
+        };
+        auto tile_of = [&](int n) __attribute__((always_inline)) -> int {  // dense
+            const int tile = (step0 + wave + W * (n + (lane >> 1))) * 2 + (lane & 1);
+            const int id = (long long)tile * 16 < to ? table[tile >> a.c.tile_shift] : -1;
+            return (unsigned)id < (unsigned)a.c.n_blocks ? (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask)) : -1;
+        };
+        struct Places {
+            int held, next, id, pos;  // on the lanes now; the next lot (listed: its positions and blocks), positions of the one behind it
+        } at = {-1, -1, -1, -1};
+        auto begin_places = [&]() __attribute__((always_inline)) {
             if constexpr (LIST) {
-                const long long e = (long long)(step0 + wave + kWaves * (n0 + (lane >> 5))) * kStep + (lane & 31);
-                if (e >= to) return -1;
-                const int p = list[e];
-                if (p < 0 || p >= unit.tokens) return -1;
-                const int id = table[p >> (a.c.tile_shift + 4)];
-                if (id < 0 || id >= a.c.n_blocks) return -1;
-                return (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15));
+                const int p = position(0);
+                at.next = position(kAhead);
+                at.held = row_of(p, block_of(p));
+                at.id = block_of(at.next);
+                at.pos = position(2 * kAhead);
             } else {
-                const int tile = (step0 + wave + kWaves * (n0 + (lane >> 1))) * 2 + (lane & 1);
-                if ((long long)tile * 16 >= to) return -1;
-                const int id = table[tile >> a.c.tile_shift];
-                if (id < 0 || id >= a.c.n_blocks) return -1;
-                return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask));
+                at.held = tile_of(0);
             }
         };
-        constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
+        auto turn_places = [&](int n) __attribute__((always_inline)) {  // step n begins a lot
+            if constexpr (LIST) {
+                at.held = row_of(at.next, at.id);
+                at.next = at.pos;
+                at.id = block_of(at.next);
+                at.pos = position(n + 2 * kAhead);
+            } else {
+                at.held = tile_of(n);
+            }
+        };
         // step n of this wave: key codes, value codes
         auto request_keys = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
             x.bad = 0;
@@ -356,7 +386,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
         const uint32_t cut1 = PACK > 1 && term >= 1 ? 0xFFFF0000u : 0u, cut2 = PACK > 2 && term >= 2 ? 0xFFFF0000u : 0u;
         // Step n; between(): what is to be requested once the key codes have been used.
         auto attend = [&](int n, Keys &y, auto between) __attribute__((always_inline)) {
-            const int key0 = (step0 + wave + kWaves * n) * kStep;
+            const int key0 = (step0 + wave + W * n) * kStep;
             f32x4 d[NT][2];
 #pragma unroll
             for (int x = 0; x < NT; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -447,14 +477,14 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
         };
 
         if (n_mine > 0) {
-            int held = places(0);
+            begin_places();
             if constexpr (NT == 1) {  // two steps in registers: one worked on, one on its way
                 Keys x, y;
                 auto request = [&](int n, Keys &z) __attribute__((always_inline)) {
                     if (n >= n_mine) return;
-                    if (n % kAhead == 0 && n) held = places(n);
-                    request_keys(held, n, z);
-                    request_values(held, n, z);
+                    if (n % kAhead == 0 && n) turn_places(n);
+                    request_keys(at.held, n, z);
+                    request_values(at.held, n, z);
                 };
                 request(0, x);
                 for (int n = 0; n < n_mine; n += 2) {
@@ -466,16 +496,16 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
                 }
             } else {  // no room for a second one: codes are requested as soon as the last ones have been used
                 Keys x;
-                request_keys(held, 0, x);
-                request_values(held, 0, x);
+                request_keys(at.held, 0, x);
+                request_values(at.held, 0, x);
                 for (int n = 0; n < n_mine; ++n) {
                     const bool more = n + 1 < n_mine;
                     attend(n, x, [&]() __attribute__((always_inline)) {
                         if (!more) return;
-                        if ((n + 1) % kAhead == 0) held = places(n + 1);
-                        request_keys(held, n + 1, x);
+                        if ((n + 1) % kAhead == 0) turn_places(n + 1);
+                        request_keys(at.held, n + 1, x);
                     });
-                    if (more) request_values(held, n + 1, x);
+                    if (more) request_values(at.held, n + 1, x);
                 }
             }
         }
@@ -502,15 +532,15 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
                 }
             }
             __syncthreads();
-            for (int in = tid >> 5; in < min(R, n_rows - R * x); in += kWaves * 2) {
+            for (int in = tid >> 5; in < min(R, n_rows - R * x); in += W * 2) {
                 const int row = R * x + in;
                 float top = kNoMax;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_acc[w][in][kD]);
+                for (int w = 0; w < W; ++w) top = fmaxf(top, s_acc[w][in][kD]);
                 f32x4 sum = {0.f, 0.f, 0.f, 0.f};
                 float all = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
+                for (int w = 0; w < W; ++w) {
                     const float f = __builtin_amdgcn_exp2f(s_acc[w][in][kD] - top);
                     f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
 #pragma unroll
@@ -531,10 +561,10 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : 3) void cache_attend_kern
             }
             __syncthreads();
         }
-        if (now > u0 && stop == u1) note = make_int4(s, h, (int)pieces.owner(u0), 0);
+        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows};
         now = stop;
     }
-    if (tid == 0) a.notes[blockIdx.x] = note;
+    if (tid == 0 && a.notes) a.notes[blockIdx.x] = note;
 }
 
 // ------------------------------------------------------------------------------------------------------------ many queries
@@ -599,11 +629,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     __syncthreads();
     const Pieces pieces(total, gridDim.x);
     if (blockIdx.x >= pieces.groups || total == 0) {
-        if (tid == 0) a.notes[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (tid == 0) a.notes[blockIdx.x].first = -1;
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    int4 note = make_int4(-1, 0, 0, 0);
+    MergeNote note = {-1, 0, 0, 0, 0};
     int entry = 0;
     for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
         if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
@@ -849,53 +879,64 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 record[(size_t)in * kRecord + kD + 1] = l[x];
             }
         }
-        if (now > u0 && stop == u1) note = make_int4(s, h, (int)pieces.owner(u0), base);
+        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, base, all_rows};
         now = stop;
     }
     if (tid == 0) a.notes[blockIdx.x] = note;
 }
 
-// Joins the records of the unit whose end workgroup blockIdx.x noted, if it did: one of workgroup note.z (its last part), one each
-// of those behind it up to this one (their first parts).  Groups of 32 threads take a row, four dims each; GROUPS of them share a row's records.
-// Bound by three round trips to memory: the note, the maxima, the sums.
+// Joins the records of the unit whose end workgroup blockIdx.x noted, if it did: one of workgroup `first` (its last part), one each of
+// those behind it up to this one (their first parts).  Groups of 32 threads take a row, four dims each; GROUPS of them share a row's records.
+// Bound by two round trips to memory: the note, the records.
 constexpr int kMergeThreads = 256;
-template <int GROUPS, bool LIST>
+template <int GROUPS>
 __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend a) {
     __shared__ float s_sum[kMergeThreads / 32][kRecord];
-    const int4 note = a.notes[blockIdx.x];
-    if (note.x < 0) return;
-    const int all = threadIdx.x >> 5, group = all % GROUPS, d0 = 4 * (threadIdx.x & 31), i = threadIdx.x & 31;
+    const MergeNote note = a.notes[blockIdx.x];
+    if (note.first < 0) return;
+    const int all = threadIdx.x >> 5, group = all % GROUPS, d0 = 4 * (threadIdx.x & 31);
     const int in = (int)blockIdx.y * (kMergeThreads / 32 / GROUPS) + all / GROUPS;
-    const int s = note.x, h = note.y, n = (int)blockIdx.x - note.z + 1, row = note.w + in;
-    const Unit<LIST> unit(a, s, h);
-    const bool mine = in < a.rows && row < unit.queries(a) * a.G;
+    const int n = (int)blockIdx.x - note.first + 1, row = note.base + in;
+    const bool mine = in < a.rows && row < note.rows;
     float top = kNoMax, total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    auto join = [&](float m, float l, const f32x4 &v) {
+        const float mn = fmaxf(top, m), f0 = __builtin_amdgcn_exp2f(top - mn), f1 = __builtin_amdgcn_exp2f(m - mn);
+        sum = sum * f0 + v * f1;
+        total = total * f0 + l * f1;
+        top = mn;
+    };
     if (mine) {
-        auto record = [&](int k) { return a.part + (((size_t)(note.z + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + in) * kRecord; };
-        for (int k = i; k < n; k += 32) top = fmaxf(top, record(k)[kD]);
+        constexpr int kAtOnce = 4;
+        for (int k = group; k < n; k += GROUPS * kAtOnce) {
+            float m[kAtOnce], l[kAtOnce];
+            f32x4 v[kAtOnce];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-#pragma unroll 4
-        for (int k = group; k < n; k += GROUPS) {
-            const float *x = record(k);
-            const float f = __builtin_amdgcn_exp2f(x[kD] - top);
-            sum += *(const f32x4 *)(x + d0) * f;
-            total += x[kD + 1] * f;
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int kk = min(k + GROUPS * j, n - 1);
+                const float *x = a.part + (((size_t)(note.first + kk) * 2 + (kk == 0 ? 1 : 0)) * a.rows + in) * kRecord;
+                v[j] = *(const f32x4 *)(x + d0);
+                m[j] = x[kD];
+                l[j] = x[kD + 1];
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                if (k + GROUPS * j < n) join(m[j], l[j], v[j]);
         }
     }
     if constexpr (GROUPS > 1) {
-        *(f32x4 *)(s_sum[all] + d0) = sum;
-        if (i == 0) s_sum[all][kD] = total;
+        float *r = s_sum[all];
+        *(f32x4 *)(r + d0) = sum;
+        if (d0 == 0) {
+            r[kD] = top;
+            r[kD + 1] = total;
+        }
         __syncthreads();
         if (group) return;
 #pragma unroll
-        for (int w = 1; w < GROUPS; ++w) {
-            sum += *(const f32x4 *)(s_sum[all + w] + d0);
-            total += s_sum[all + w][kD];
-        }
+        for (int w = 1; w < GROUPS; ++w) join(s_sum[all + w][kD], s_sum[all + w][kD + 1], *(const f32x4 *)(s_sum[all + w] + d0));
     }
-    if (mine) put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, top, total);
+    if (mine) put_row(a, (size_t)(note.row0 + row / a.G) * a.c.H * a.G + note.h * a.G + row % a.G, d0, sum, top, total);
 }
 
 }  // namespace
@@ -908,51 +949,70 @@ static int few_rows(const CacheAttend &a) {
     const long long rows = (long long)a.max_query * a.G;
     return rows <= 5 ? 5 : rows <= 8 ? 8 : rows <= 16 || rows > kFewRows ? 16 : rows <= 32 ? 32 : 48;
 }
-static size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(int4)); }
+static size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(MergeNote)); }
 
-size_t plan_cache_attend(CacheAttend &a) {
-    const long long quanta = ((long long)a.max_keys + kQuantum - 1) / kQuantum * std::min(a.S, kEntries) * a.c.H;
+// Units (request, KV head) that stay whole, one workgroup each, no merge behind it: short ones, where the merge costs more than the cut
+// gains, and lists of as many units as there are CUs.
+constexpr int kWholeKeys = 512, kWholeList = 1024, kListWaves = 8;
+
+size_t plan_cache_attend(CacheAttend &a, bool listed) {
+    const long long units = (long long)std::min(a.S, kEntries) * a.c.H;
     const int rows = few_rows(a);
-    a.few_groups = (int)std::min<long long>(rows > 16 ? 512 : 768, quanta);
     a.many = (long long)a.max_query * a.G > kFewRows;
+    a.many_groups = 0;
+    if (listed) {
+        const int quantum = kListWaves * kStep;
+        a.per_unit = (a.max_keys + quantum - 1) / quantum;
+        a.whole = a.max_keys <= kWholeList || units >= 256;
+        a.few_groups = (int)(a.whole ? units : std::min<long long>(256, units * a.per_unit));
+        return a.whole ? 0 : attend_bytes(a.few_groups, rows);
+    }
+    a.whole = a.max_keys <= kWholeKeys && !a.many;
+    a.per_unit = a.whole ? 1 : 0;
+    if (a.whole) {
+        a.few_groups = (int)units;
+        return 0;
+    }
+    const long long quanta = ((long long)a.max_keys + kQuantum - 1) / kQuantum * units;
+    a.few_groups = (int)std::min<long long>(rows > 16 ? 512 : 768, quanta);
     const long long tiles = ((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows;
-    a.many_groups = a.many ? (int)std::min<long long>(512, quanta * tiles) : 0;
+    if (a.many) a.many_groups = (int)std::min<long long>(512, quanta * tiles);
     return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, kChunkRows));
 }
 
+template <int W, bool LIST>
+static void launch_few(const CacheAttend &a, hipStream_t stream) {
+    const dim3 grid(a.whole ? a.n_here * a.c.H : a.few_groups), block(W * 64);
+    if (a.rows == 5) cache_attend_kernel<W, 3, 1, 1, LIST><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<W, 2, 1, 1, LIST><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 8) cache_attend_kernel<W, 2, 1, 2, LIST><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 16 && a.out_bf16) cache_attend_kernel<W, 1, 1, 2, LIST><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 16) cache_attend_kernel<W, 1, 1, 3, LIST><<<grid, block, 0, stream>>>(a);
+    else if constexpr (!LIST) {
+        if (a.rows == 32 && a.out_bf16) cache_attend_kernel<W, 1, 2, 1, LIST><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 32) cache_attend_kernel<W, 1, 2, 3, LIST><<<grid, block, 0, stream>>>(a);
+        else if (a.out_bf16) cache_attend_kernel<W, 1, 3, 1, LIST><<<grid, block, 0, stream>>>(a);
+        else cache_attend_kernel<W, 1, 3, 3, LIST><<<grid, block, 0, stream>>>(a);
+    }
+    if (!a.whole) cache_merge_kernel<8><<<dim3(a.few_groups, std::min(a.rows, a.max_query * a.G)), kMergeThreads, 0, stream>>>(a);
+}
+
 void launch_cache_attend(CacheAttend a, hipStream_t stream) {
-    const dim3 block(kWaves * 64);
     float *const part = a.part;
-    auto few = [&](auto list) {
-        constexpr bool L = decltype(list)::value;
-        a.rows = few_rows(a);
-        a.notes = (int4 *)part;
-        a.part = (float *)(a.notes + a.few_groups);
-        const dim3 grid(a.few_groups);
-        if (a.rows == 5) cache_attend_kernel<3, 1, 1, L><<<grid, block, 0, stream>>>(a);
-        else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<2, 1, 1, L><<<grid, block, 0, stream>>>(a);
-        else if (a.rows == 8) cache_attend_kernel<2, 1, 2, L><<<grid, block, 0, stream>>>(a);
-        else if (a.rows == 16 && a.out_bf16) cache_attend_kernel<1, 1, 2, L><<<grid, block, 0, stream>>>(a);
-        else if (a.rows == 16) cache_attend_kernel<1, 1, 3, L><<<grid, block, 0, stream>>>(a);
-        else if constexpr (!L) {
-            if (a.rows == 32 && a.out_bf16) cache_attend_kernel<1, 2, 1, L><<<grid, block, 0, stream>>>(a);
-            else if (a.rows == 32) cache_attend_kernel<1, 2, 3, L><<<grid, block, 0, stream>>>(a);
-            else if (a.out_bf16) cache_attend_kernel<1, 3, 1, L><<<grid, block, 0, stream>>>(a);
-            else cache_attend_kernel<1, 3, 3, L><<<grid, block, 0, stream>>>(a);
-        }
-        cache_merge_kernel<8, L><<<dim3(a.few_groups, std::min(a.rows, a.max_query * a.G)), kMergeThreads, 0, stream>>>(a);
-    };
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
         a.n_here = std::min(a.S - a.first, kEntries);
-        if (a.pos) few(std::true_type());
-        else few(std::false_type());
+        a.rows = few_rows(a);
+        a.notes = a.whole ? nullptr : (MergeNote *)part;
+        a.part = a.whole ? nullptr : (float *)(a.notes + a.few_groups);
+        if (a.pos) launch_few<kListWaves, true>(a, stream);
+        else launch_few<kWaves, false>(a, stream);
         if (!a.many) continue;
         a.rows = kChunkRows;
-        a.notes = (int4 *)part;
+        a.notes = (MergeNote *)part;
         a.part = (float *)(a.notes + a.many_groups);
-        if (a.out_bf16) cache_chunk_kernel<1><<<a.many_groups, block, 0, stream>>>(a);
-        else cache_chunk_kernel<3><<<a.many_groups, block, 0, stream>>>(a);
-        cache_merge_kernel<1, false><<<dim3(a.many_groups, kChunkRows / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
+        if (a.out_bf16) cache_chunk_kernel<1><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
+        else cache_chunk_kernel<3><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
+        cache_merge_kernel<1><<<dim3(a.many_groups, kChunkRows / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
     }
 }
 

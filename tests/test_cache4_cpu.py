@@ -35,7 +35,7 @@ def test_plan_refuses():
     for name in ("new", "cached", "out", "table", "free", "n_free", "left", "start", "slots", "info"):
         assert call(**{name: None}) == b.ICE_ERR_INVALID_ARG
     assert call(bs=24) == b.ICE_ERR_UNSUPPORTED
-    for change in (dict(n=0), dict(n=65536), dict(n_slots=0), dict(n_slots=2 ** 30 + 1), dict(nb=0), dict(mb=0), dict(nb=2 ** 27), dict(mb=2 ** 27)):
+    for change in (dict(n=0), dict(n=8193), dict(n_slots=0), dict(n_slots=2 ** 30 + 1), dict(nb=0), dict(mb=0), dict(nb=2 ** 27), dict(mb=2 ** 27)):
         assert call(**change) == b.ICE_ERR_SHAPE, change
 
 
@@ -91,7 +91,8 @@ def test_attention_refuses():
         assert go(**{name: None}) == b.ICE_ERR_INVALID_ARG, name
     for change in (dict(n=0), dict(max_tok=0), dict(mb=-1), dict(qs=4)):
         assert go(**change) == b.ICE_ERR_SHAPE, change
-    assert go(wb=p.ice_cache_attend_bytes(c, 4, 2, 1, 4096) - 1) == b.ICE_ERR_CAPACITY
+    assert go(wb=p.ice_cache_attend_tokens_bytes(c, 4, 2, 4096) - 1) == b.ICE_ERR_CAPACITY
+    assert p.ice_cache_attend_tokens_bytes(c, 17, 2, 4096) == 0
 
 
 def test_classes_take_arrays_on_a_gpu_only():
