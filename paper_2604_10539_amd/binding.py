@@ -1,4 +1,5 @@
-"""Thin ctypes binding of the C ABI in include/icecache.h (same names, argument marshalling only).
+"""Thin binding of the C ABI in include/icecache.h (same names, argument marshalling only): ctypes, and for the classes of the 4-bit
+cache, whose calls are short, the extension module _calls (csrc/ice_calls.cpp).
 
 Every step of the path runs in the HIP library; torch supplies device memory and the current
 stream.  There is no fallback: if libicecache.so is missing, loading fails loudly.
@@ -6,7 +7,6 @@ stream.  There is no fallback: if libicecache.so is missing, loading fails loudl
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 
 import torch
@@ -65,11 +65,12 @@ class IceError(RuntimeError):
 
 
 _lib = None
+_native = None  # the extension module, once it is bound to the library
 
 
 def lib() -> C.CDLL:
     """Loads the HIP library built by paper_2604_10539_amd/build.py; raises if it is not there."""
-    global _lib
+    global _lib, _native
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("%s is missing: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -128,6 +129,14 @@ def lib() -> C.CDLL:
             if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
                             "ice_cache_attend_tokens_bytes"):
                 getattr(L, name).restype = C.c_int
+        try:
+            from . import _calls
+        except ImportError as e:
+            raise RuntimeError("the extension module _calls is missing: run `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        _calls.bind(IceError, *(C.cast(getattr(L, name), C.c_void_p).value for name in (
+            "ice_last_error", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
+            "ice_cache_attend_tokens_bytes", "ice_cache_attend_tokens")))
+        _native = _calls
         _lib = L
     return _lib
 
@@ -339,19 +348,9 @@ def ice_cache_bytes(cache: IceCacheDesc) -> int:
 def ice_plan_blocks(new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots, info, block_size,
                     stream=None) -> None:
     """int32 device tensors as in the header; block_table [n_requests, max_blocks], free_ids [n_blocks]."""
-    n, n_blocks, n_slots, device, table = new_len.numel(), free_ids.numel(), slots.numel(), block_table.get_device(), block_table.shape
-    for name, t, size in (("new_len", new_len, n), ("cached_len", cached_len, n), ("seq_len", seq_len, n), ("n_free", n_free, 1),
-                          ("n_free_left", n_free_left, 1), ("query_start", query_start, n + 1), ("info", info, 4),
-                          ("free_ids", free_ids, n_blocks), ("slots", slots, n_slots), ("block_table", block_table, block_table.numel())):
-        if not (t.dtype is torch.int32 and t.numel() == size and t.get_device() == device and t.is_contiguous()):
-            raise IceError(ICE_ERR_SHAPE, "%s: contiguous int32 of %d entries on the block table's device" % (name, size))
-    if len(table) != 2 or table[0] != n:
-        raise IceError(ICE_ERR_SHAPE, "block_table: [%d, max_blocks]" % n)
-    if device < 0:
-        raise IceError(ICE_ERR_INVALID_ARG, "the arrays must be on a GPU")
-    _check(lib().ice_plan_blocks(n, block_size, table[1], n_blocks, new_len.data_ptr(), cached_len.data_ptr(), seq_len.data_ptr(),
-                                 block_table.data_ptr(), free_ids.data_ptr(), n_free.data_ptr(), n_free_left.data_ptr(), query_start.data_ptr(),
-                                 slots.data_ptr(), n_slots, info.data_ptr(), _stream(stream)))
+    lib()
+    _native.plan(_stream(stream) or 0, block_size, new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots,
+                 info)
 
 
 def ice_cache_write(cache: IceCacheDesc, k, v, k_stride, v_stride, slots, n_tokens, stream=None) -> None:
@@ -622,29 +621,17 @@ class IceIndex:
         return a, best
 
 
-def _on_stream(call):
-    """A method whose launches and allocations belong to the `stream` it is given (a torch stream or a raw address), on the device that
-    holds the object's arrays, whichever device and stream are current."""
-    @functools.wraps(call)
-    def method(self, *args, stream=None, **more):
-        if stream is None and _current_device() == self._index:
-            return call(self, *args, **more)
-        with torch.cuda.device(self._index):
-            if stream is None:
-                return call(self, *args, **more)
-            if isinstance(stream, int):
-                stream = torch.cuda.ExternalStream(stream, device=self.device)
-            with torch.cuda.stream(stream):
-                return call(self, *args, **more)
-    return method
-
-
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us against 0.5: it does not ask whether CUDA is up)
 
 
-def _want(ok, text):
-    if not ok:
-        raise IceError(ICE_ERR_SHAPE, text)
+def _elsewhere(call, self, stream, *args):
+    """The call under the device that holds the object's arrays and under the stream it is given (a torch stream or a raw address), so that
+    launches and allocations belong there."""
+    with torch.cuda.device(self._index):
+        if stream is None:
+            return call(self, *args)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream):
+            return call(self, *args)
 
 
 class IceBlocks:
@@ -667,15 +654,16 @@ class IceBlocks:
         self.n_free = e(1).fill_(n_blocks)
         self._index = self.block_table.device.index
 
-    @_on_stream
-    def plan(self, new_len, n_slots, slots=None):
+    def plan(self, new_len, n_slots, slots=None, stream=None):
         """new_len int32 [max_requests] on the GPU: tokens a request gains (> 0) or gives back (< 0; its length or more: it has
         ended).  n_slots: room for so many new tokens.  -> (query_start [max_requests + 1], slots [n_slots], info [4]).
         query_start and info are this object's own and change with the next call."""
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceBlocks.plan, self, stream, new_len, n_slots, slots)
         if slots is None:
             slots = torch.empty(n_slots, dtype=torch.int32, device=self.device)
-        _want(slots.numel() == n_slots, "slots: %d entries" % n_slots)
-        _want(new_len.numel() == self.max_requests, "new_len: %d entries" % self.max_requests)
+        elif slots.numel() != n_slots:
+            raise IceError(ICE_ERR_SHAPE, "slots: %d entries" % n_slots)
         ice_plan_blocks(new_len, self.seq_len, self.seq_len, self.block_table, self.free_ids, self.n_free, self.n_free, self.query_start,
                         slots, self.info, self.block_size)
         return self.query_start, slots, self.info
@@ -683,10 +671,8 @@ class IceBlocks:
 
 class IceCache:
     """One layer's KV cache in 4 bits (see ice_cache_t in the header).  bf16 tensors may be torch.bfloat16 or int16 bit
-    patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous.
-
-    The methods of a decode step take as long on the host as on the GPU: their checks are written out, one expression each, and they call
-    the library with addresses."""
+    patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous.  Every method takes `stream`, a torch stream
+    or a raw address; without one it is the current stream of the cache's device."""
 
     def __init__(self, n_blocks, n_kv_heads, block_size=64, device="cuda", data=None):
         self.n_blocks, self.n_kv_heads, self.block_size = n_blocks, n_kv_heads, block_size
@@ -695,127 +681,45 @@ class IceCache:
         shape = (n_blocks, n_kv_heads, block_size // 16, 2176)
         if data is None:
             data = torch.empty(shape, dtype=torch.uint8, device=device)
-        _want(tuple(data.shape) == shape and data.dtype is torch.uint8 and data.is_contiguous() and data.is_cuda,
-              "data: contiguous uint8 %s on a GPU" % (shape,))
+        if not (tuple(data.shape) == shape and data.dtype is torch.uint8 and data.is_contiguous() and data.is_cuda):
+            raise IceError(ICE_ERR_SHAPE, "data: contiguous uint8 %s on a GPU" % (shape,))
         self.data, self.device, self._index = data, data.device, data.device.index
-        self._desc = make_cache_desc(data, n_blocks, n_kv_heads, block_size)
-        self._ref = C.byref(self._desc)
-        self._lib = lib()
-        self._bytes = {}  # workspace of an attention call by its sizes
+        self._desc = make_cache_desc(data, n_blocks, n_kv_heads, block_size)  # (stays where it is: the calls get its address)
+        self._at = C.addressof(self._desc)
 
-    def _rows(self, x, name):
-        """Address and stride of rows [tokens, heads, 128]."""
-        shape, stride = x.shape, x.stride()
-        if not (len(shape) == 3 and shape[2] == 128 and stride[2] == 1 and (stride[1] == 128 or shape[1] == 1) and
-                (x.dtype is torch.bfloat16 or x.dtype is torch.int16) and x.get_device() == self._index):
-            raise IceError(ICE_ERR_SHAPE, "%s: bf16 [tokens, heads, 128] on the cache's device, heads and values side by side" % name)
-        return x.data_ptr(), stride[0]
-
-    def _ints(self, t, name, shape):
-        if not (t.shape == shape and t.dtype is torch.int32 and t.is_contiguous() and t.get_device() == self._index):
-            raise IceError(ICE_ERR_SHAPE, "%s: contiguous int32 %s on the cache's device" % (name, list(shape)))
-        return t.data_ptr()
-
-    def _table(self, seq_len, block_table):
-        n, shape = seq_len.shape[0], block_table.shape
-        if len(shape) != 2 or shape[0] != n:
-            raise IceError(ICE_ERR_SHAPE, "block_table: [%d requests, max_blocks]" % n)
-        return n, self._ints(seq_len, "seq_len", (n,)), self._ints(block_table, "block_table", shape), shape[1]
-
-    @_on_stream
-    def write(self, k, v, slots):
+    def write(self, k, v, slots, stream=None):
         """k, v [tokens, n_kv_heads, 128] into their slots [tokens]; -1 is left out."""
-        kp, ks = self._rows(k, "k")
-        vp, vs = self._rows(v, "v")
-        n = k.shape[0]
-        if k.shape != v.shape or k.shape[1] != self.n_kv_heads:
-            raise IceError(ICE_ERR_SHAPE, "k and v: [tokens, %d, 128]" % self.n_kv_heads)
-        _check(self._lib.ice_cache_write(self._ref, kp, vp, ks, vs, self._ints(slots, "slots", (n,)), n, _stream_on(self._index)))
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.write, self, stream, k, v, slots)
+        _native.write(self._at, self._index, _stream_on(self._index), k, v, slots)
 
-    @_on_stream
-    def read(self, block_table, seq_len, n_rows, first=None, out=None):
+    def read(self, block_table, seq_len, n_rows, first=None, out=(None, None), stream=None):
         """(K, V) bf16 [requests, n_kv_heads, n_rows, 128]: the tokens from position first[s] on, as they are held."""
-        n, sp, tp, width = self._table(seq_len, block_table)
-        if first is not None:
-            first = self._ints(first, "first", (n,))
-        shape = (n, self.n_kv_heads, n_rows, 128)
-        if out is None:
-            K = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-            V = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        else:
-            K, V = out
-            for x in out:
-                _want(x.shape == shape and x.element_size() == 2 and x.is_contiguous() and x.get_device() == self._index,
-                      "out: two contiguous bf16 tensors %s" % (shape,))
-        _check(self._lib.ice_cache_read(self._ref, n, sp, tp, width, first, n_rows, K.data_ptr(), V.data_ptr(), _stream_on(self._index)))
-        return K, V
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.read, self, stream, block_table, seq_len, n_rows, first, out)
+        return _native.read(self._at, self._index, _stream_on(self._index), block_table, seq_len, n_rows, first, *out)
 
-    def _outputs(self, q, out, out_dtype, lse, with_lse):
-        """(out, lse, its address, type of out)"""
-        shape = q.shape
-        if out is None:
-            out = torch.empty(shape, dtype=out_dtype, device=self.device)
-        elif not (out.shape == shape and out.is_contiguous() and out.get_device() == self._index):
-            raise IceError(ICE_ERR_SHAPE, "out: contiguous %s on the cache's device" % (tuple(shape),))
-        kind = ICE_OUT_F32 if out.dtype is torch.float32 else ICE_OUT_BF16 if out.dtype is torch.bfloat16 else -1
-        if lse is not None:
-            if not (lse.shape == shape[:2] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == self._index):
-                raise IceError(ICE_ERR_SHAPE, "lse: contiguous float32 %s on the cache's device" % (tuple(shape[:2]),))
-        elif with_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
-        return out, lse, None if lse is None else lse.data_ptr(), kind
-
-    def _workspace(self, size_of, *sizes):
-        """(address, bytes, tensor) of the scratch of this call alone: it comes from torch's allocator each time (under capture from the
-        graph's own pool), so that calls on other streams and other graphs never share it."""
-        nbytes = self._bytes.get(sizes)
-        if nbytes is None:
-            if len(self._bytes) >= 4096:
-                self._bytes.clear()
-            nbytes = self._bytes[sizes] = size_of(self._ref, *sizes)
-        if nbytes == 0:
-            return None, 0, None
-        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        return work.data_ptr(), nbytes, work
-
-    def _group(self, q):
-        qp, qs = self._rows(q, "q")
-        group, rest = divmod(q.shape[1], self.n_kv_heads)
-        if rest:
-            raise IceError(ICE_ERR_SHAPE, "q: a multiple of %d heads" % self.n_kv_heads)
-        return qp, qs, group
-
-    @_on_stream
     def attend(self, q, query_start, seq_len, block_table, max_query=None, max_len=None, window=0, out=None, out_dtype=torch.float32,
-               lse=None, with_lse=False):
+               lse=None, with_lse=False, stream=None):
         """Causal attention of a step's queries q [tokens, heads, 128] over their requests' cached tokens.  max_query, max_len: what the host
         knows of the most queries of a request (none has more) and the longest length (a hint).  -> out, or (out, lse) when lse is
         given or with_lse is true.  Rows of q behind query_start[-1] are left out and their outputs left as they were."""
-        qp, qs, group = self._group(q)
-        n, sp, tp, width = self._table(seq_len, block_table)
-        tokens = q.shape[0]
-        out, lse, lp, kind = self._outputs(q, out, out_dtype, lse, with_lse)
-        if tokens:
-            max_query = tokens if max_query is None else min(max_query, tokens)
-            if max_len is None:
-                max_len = width * self.block_size
-            wp, nbytes, work = self._workspace(self._lib.ice_cache_attend_bytes, group, n, max_query, max_len)
-            _check(self._lib.ice_cache_attend(self._ref, qp, qs, group, n, self._ints(query_start, "query_start", (n + 1,)), tokens, max_query, sp,
-                                              max_len, tp, width, window, out.data_ptr(), kind, lp, wp, nbytes, _stream_on(self._index)))
-        return out if lse is None else (out, lse)
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.attend, self, stream, q, query_start, seq_len, block_table, max_query, max_len, window, out, out_dtype, lse,
+                              with_lse)
+        return _native.attend(self._at, self._index, _stream_on(self._index), q, query_start, seq_len, block_table, max_query, max_len, window,
+                              out, _is_bf16(out_dtype), lse, bool(with_lse))
 
-    @_on_stream
-    def attend_tokens(self, q, seq_len, block_table, token_pos, n_tok, out=None, out_dtype=torch.float32, lse=None, with_lse=False):
+    def attend_tokens(self, q, seq_len, block_table, token_pos, n_tok, out=None, out_dtype=torch.float32, lse=None, with_lse=False, stream=None):
         """Attention of one query per request, q [requests, heads, 128], over positions token_pos[..., :n_tok] of its tokens, both as
         IceIndex.selected_tokens gives them."""
-        qp, qs, group = self._group(q)
-        n, sp, tp, width = self._table(seq_len, block_table)
-        if q.shape[0] != n:
-            raise IceError(ICE_ERR_SHAPE, "q: one row per request")
-        most, heads = token_pos.shape[-1], self.n_kv_heads
-        pp, np_ = self._ints(token_pos, "token_pos", (n, heads, most)), self._ints(n_tok, "n_tok", (n, heads))
-        out, lse, lp, kind = self._outputs(q, out, out_dtype, lse, with_lse)
-        wp, nbytes, work = self._workspace(self._lib.ice_cache_attend_tokens_bytes, group, n, most)
-        _check(self._lib.ice_cache_attend_tokens(self._ref, qp, qs, group, n, sp, tp, width, pp, np_, most, out.data_ptr(), kind, lp, wp,
-                                                 nbytes, _stream_on(self._index)))
-        return out if lse is None else (out, lse)
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.attend_tokens, self, stream, q, seq_len, block_table, token_pos, n_tok, out, out_dtype, lse, with_lse)
+        return _native.attend_tokens(self._at, self._index, _stream_on(self._index), q, seq_len, block_table, token_pos, n_tok, out,
+                                     _is_bf16(out_dtype), lse, bool(with_lse))
+
+
+def _is_bf16(dtype):
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise IceError(ICE_ERR_SHAPE, "out_dtype: float32 or bfloat16")
+    return dtype is torch.bfloat16

@@ -1,4 +1,4 @@
-"""Builds libicecache.so (HIP kernels + C ABI, gfx950 only) in-tree with hipcc."""
+"""Builds libicecache.so (HIP kernels + C ABI, gfx950 only) in-tree with hipcc, and the extension module _calls.so with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -46,5 +46,25 @@ def build_library(verbose: bool = False, extra_flags=(), lib_path: str = LIB, ob
     return lib_path
 
 
+def build_calls(verbose: bool = False) -> str:
+    """Compile the extension module (always): torch's headers and Python's, no GPU code."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    path = os.path.join(PKG, "_calls.so")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I" + os.path.join(ROOT, "include"),
+           "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "ice_calls.cpp"), "-o", path, "-L" + os.path.join(base, "lib"),
+           "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed for ice_calls.cpp:\n%s" % (cmd[0], r.stderr))
+    if verbose:
+        print(r.stderr)
+    return path
+
+
 if __name__ == "__main__":
+    print(build_calls(verbose=True))
     print(build_library(verbose=True))

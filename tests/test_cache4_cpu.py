@@ -107,7 +107,7 @@ def test_classes_take_arrays_on_a_gpu_only():
     e = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
     args = [e(2), e(2), e(2), torch.zeros((2, 4), dtype=torch.int32), e(16), e(1), e(1), e(3), e(8), e(4), 16]
     assert status(p.ice_plan_blocks, *args) == b.ICE_ERR_INVALID_ARG
-    for i, bad in ((0, torch.zeros(2)), (2, e(3)), (5, e(2)), (7, e(2)), (9, e(3)), (3, e(8)), (1, e(4)[::2])):
+    for i, bad in ((0, torch.zeros(2)), (2, e(3)), (5, e(2)), (7, e(2)), (9, e(3)), (3, e(8)), (1, e(4)[::2]), (4, None)):
         assert status(p.ice_plan_blocks, *args[:i], bad, *args[i + 1:]) == b.ICE_ERR_SHAPE, i
 
 
