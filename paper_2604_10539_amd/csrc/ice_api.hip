@@ -441,7 +441,7 @@ ice_status_t ice_plan_blocks(int32_t n_requests, int32_t block_size, int32_t max
     if (max_blocks < 1 || (long long)max_blocks * block_size >= 2147483648ll)
         return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, and fewer than 2^31 tokens", max_blocks);
     launch_cache_plan({n_requests, block_size == 64 ? 6 : block_size == 32 ? 5 : 4, max_blocks, n_blocks, new_len, cached_len, seq_len, table,
-                       free_ids, n_free, n_free_left, query_start, slots, n_slots, info},
+                       free_ids, n_free, n_free_left, query_start, slots, n_slots, info, false},
                       static_cast<hipStream_t>(stream));
     return device_status("ice_plan_blocks");
 }

@@ -27,9 +27,10 @@ struct CachePlan {
     int *n_free_left, *query_start, *slots;
     int n_slots;
     int *info;
+    bool end_later;  // lengths and the stack's height are written by a second launch
 };
 constexpr int kPlanRequests = 8192;  // of one plan at most: three sums each in LDS
-void launch_cache_plan(const CachePlan &p, hipStream_t stream);
+void launch_cache_plan(CachePlan p, hipStream_t stream);
 
 void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, long long k_stride, long long v_stride, const int *slots,
                         int n_tokens, hipStream_t stream);

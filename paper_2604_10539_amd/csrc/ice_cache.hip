@@ -12,11 +12,12 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------------------------------------ block tables and slots
 // Every workgroup scans all requests (sums of new tokens, blocks taken, blocks given back, kept in LDS) and does its share of the
-// rest: a block given back, a block taken and a slot each find their request by bisection and read one id.  A taken block that the
+// rest: a slot, a block taken and a block given back each find their request by bisection and read one id.  A taken block that the
 // same call gives back is read from the row it comes from, not from the stack, so nothing waits for anything and the workgroups are
-// independent.  What may be updated in place, the lengths and the stack's height, is written last: by the workgroup itself where there
-// is one, else by a second launch.  Bound by latency: a trip for the lengths, the scan, a trip for the ids.
-constexpr int kPlanThreads = 1024;
+// independent.  Lengths and the stack's height that are updated in place are written last: by the workgroup itself where there is one,
+// else by a second launch.  Bound by latency: a trip for the lengths, the scan, a trip for the ids.
+constexpr int kPlanThreads = 1024;           // at most
+constexpr int kPlanItems = 4096;             // requests whose lengths fit LDS beside the sums
 constexpr unsigned kPlanMost = 0x7FFFFFFFu;  // sums stop here: they only have to be known exactly where the step is possible
 
 enum { kPlanErrFree = 1, kPlanErrRow = 2, kPlanErrSlots = 4, kPlanErrLen = 8 };
@@ -57,13 +58,15 @@ __device__ inline int plan_owner(const unsigned *sums, int n, unsigned k) {
 
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
     extern __shared__ unsigned plan_lds[];
-    const int n = p.n_requests, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = p.n_requests, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = blockDim.x, waves = threads >> 6;
+    const bool kept = n <= kPlanItems;  // blocks before the step, and lengths after it, stay in LDS
     unsigned *sums[3] = {plan_lds, plan_lds + (n + 1), plan_lds + 2 * (n + 1)};  // before each request: fresh, take, back
+    int *s_held = (int *)plan_lds + 3 * (n + 1), *s_after = s_held + n;
     __shared__ unsigned s_wave[kPlanThreads / 64][3];
     __shared__ int s_err;
     if (tid == 0) s_err = 0;
     const int n_free = *p.n_free;
-    const int each = (n + kPlanThreads - 1) / kPlanThreads, i0 = min(tid * each, n), i1 = min(i0 + each, n);
+    const int each = (n + threads - 1) / threads, i0 = min(tid * each, n), i1 = min(i0 + each, n);
     unsigned own[3] = {0, 0, 0};
     int err = 0;
     for (int i = i0; i < i1; ++i) {
@@ -72,6 +75,10 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
         own[1] = sat_add(own[1], x.take);
         own[2] = sat_add(own[2], x.back);
         err |= x.err;
+        if (kept) {
+            s_held[i] = x.held;
+            s_after[i] = x.after;
+        }
     }
     unsigned v[3] = {own[0], own[1], own[2]}, total[3] = {0, 0, 0};
 #pragma unroll
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
     unsigned at[3];
     for (int k = 0; k < 3; ++k) {
         at[k] = v[k] - min(v[k], own[k]);  // (where a sum stopped at the limit the step is refused and no sum is used)
-        for (int w = 0; w < kPlanThreads / 64; ++w) {
+        for (int w = 0; w < waves; ++w) {
             if (w == wave) at[k] = sat_add(at[k], total[k]);
             total[k] = sat_add(total[k], s_wave[w][k]);
         }
@@ -109,48 +116,51 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlan p) {
     else if (taken > (unsigned)n_free + back) err |= kPlanErrFree;
     if (fresh > (unsigned)p.n_slots) err |= kPlanErrSlots;
 
-    const unsigned step = gridDim.x * kPlanThreads, first = blockIdx.x * kPlanThreads + tid;
-    if (!err) {
-        auto given_back = [&](unsigned k) {  // id of the k-th block given back
-            const int s = plan_owner(sums[2], n, k);
-            return p.table[(size_t)s * p.max_blocks + PlanItem(p, s).need + (k - sums[2][s])];
-        };
-        auto popped = [&](unsigned k) {  // id of the k-th block taken
-            const unsigned place = (unsigned)n_free + back - 1 - k;
-            return place < (unsigned)n_free ? p.free_ids[place] : given_back(place - (unsigned)n_free);
-        };
-        for (unsigned k = first; k < (unsigned)p.n_slots; k += step) {
+    auto held_of = [&](int s) { return kept ? s_held[s] : PlanItem(p, s).held; };
+    auto after_of = [&](int s) { return kept ? s_after[s] : PlanItem(p, s).after; };
+    auto given_back = [&](unsigned k) {  // id of the k-th block given back
+        const int s = plan_owner(sums[2], n, k);
+        const int need = (int)(((long long)after_of(s) + (1ll << p.block_shift) - 1) >> p.block_shift);
+        return p.table[(size_t)s * p.max_blocks + need + (k - sums[2][s])];
+    };
+    auto popped = [&](unsigned k) {  // id of the k-th block taken
+        const unsigned place = (unsigned)n_free + back - 1 - k;
+        return place < (unsigned)n_free ? p.free_ids[place] : given_back(place - (unsigned)n_free);
+    };
+    const unsigned items = (unsigned)p.n_slots + (err ? 0u : taken + back);
+    for (unsigned k = blockIdx.x * threads + tid; k < items; k += gridDim.x * threads) {
+        if (k < (unsigned)p.n_slots) {
             int slot = -1;
-            if (k < fresh) {
+            if (!err && k < fresh) {
                 const int s = plan_owner(sums[0], n, k);
-                const PlanItem x(p, s);
-                const int pos = x.after - (int)(sums[0][s + 1] - k), j = pos >> p.block_shift;
-                const int id = j < x.held ? p.table[(size_t)s * p.max_blocks + j] : popped(sums[1][s] + (unsigned)(j - x.held));
+                const int pos = after_of(s) - (int)(sums[0][s + 1] - k), j = pos >> p.block_shift, held = held_of(s);
+                const int id = j < held ? p.table[(size_t)s * p.max_blocks + j] : popped(sums[1][s] + (unsigned)(j - held));
                 if (id >= 0 && id < p.n_blocks) slot = (id << p.block_shift) + (pos & ((1 << p.block_shift) - 1));
             }
             p.slots[k] = slot;
+        } else if (k - p.n_slots < taken) {
+            const unsigned t = k - p.n_slots;
+            const int s = plan_owner(sums[1], n, t);
+            p.table[(size_t)s * p.max_blocks + held_of(s) + (t - sums[1][s])] = popped(t);
+        } else {
+            const unsigned g = k - p.n_slots - taken;
+            p.free_ids[(unsigned)n_free + g] = given_back(g);
         }
-        for (unsigned k = first; k < taken; k += step) {
-            const int s = plan_owner(sums[1], n, k);
-            p.table[(size_t)s * p.max_blocks + PlanItem(p, s).held + (k - sums[1][s])] = popped(k);
-        }
-        for (unsigned k = first; k < back; k += step) p.free_ids[(unsigned)n_free + k] = given_back(k);
-    } else {
-        for (unsigned k = first; k < (unsigned)p.n_slots; k += step) p.slots[k] = -1;
     }
     if (blockIdx.x == 0) {
-        for (int i = tid; i <= n; i += kPlanThreads) p.query_start[i] = err ? 0 : (int)sums[0][i];
+        for (int i = tid; i <= n; i += threads) p.query_start[i] = err ? 0 : (int)sums[0][i];
         if (tid == 0) {
             p.info[0] = err ? 0 : (int)fresh;
             p.info[1] = err ? 0 : (int)taken;
             p.info[2] = err ? 0 : (int)back;
             p.info[3] = err;
         }
+        if (!p.end_later) {
+            __syncthreads();  // (the lengths have been read)
+            for (int i = tid; i < n; i += threads) p.seq_len[i] = err ? p.cached_len[i] : after_of(i);
+            if (tid == 0) *p.n_free_left = err ? n_free : n_free + (int)back - (int)taken;
+        }
     }
-    if (gridDim.x > 1) return;
-    __syncthreads();  // (the lengths have been read)
-    for (int i = tid; i < n; i += kPlanThreads) p.seq_len[i] = err ? p.cached_len[i] : PlanItem(p, i).after;
-    if (tid == 0) *p.n_free_left = err ? n_free : n_free + (int)back - (int)taken;
 }
 
 __global__ __launch_bounds__(256) void cache_plan_end_kernel(CachePlan p) {
@@ -260,15 +270,16 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDims c, int n_requ
 
 }  // namespace
 
-// One workgroup where a step moves little (a decode step: 16 requests 5 us; with a second launch 9), else up to 64: 1000 requests, 100k new tokens and
-// 50k blocks given back, 41 us by one workgroup.
-void launch_cache_plan(const CachePlan &p, hipStream_t stream) {
+// A workgroup's threads for what the step can bring at most, as many workgroups as there are CUs at most.
+void launch_cache_plan(CachePlan p, hipStream_t stream) {
     const long long most = p.n_slots + std::min<long long>((long long)p.n_requests * p.max_blocks, p.n_blocks);
-    const int groups = most <= 16384 ? 1 : (int)std::min<long long>(64, (most + 8191) / 8192);
-    const size_t lds = 3 * (p.n_requests + 1) * sizeof(unsigned);
+    const int threads = p.n_requests <= 256 && p.n_slots <= 1024 ? 256 : kPlanThreads;
+    const int groups = p.n_slots <= 4096 && most <= 32768 ? 1 : (int)std::min<long long>(256, (most + threads - 1) / threads);
+    const size_t lds = (3 * (p.n_requests + 1) + (p.n_requests <= kPlanItems ? 2 * p.n_requests : 0)) * sizeof(unsigned);
     if (lds > 65536 - 1024) allow_dynamic_lds((const void *)cache_plan_kernel, lds);
-    cache_plan_kernel<<<groups, kPlanThreads, lds, stream>>>(p);
-    if (groups > 1) cache_plan_end_kernel<<<(p.n_requests + 255) / 256, 256, 0, stream>>>(p);
+    p.end_later = groups > 1 && (p.seq_len == p.cached_len || p.n_free_left == p.n_free);
+    cache_plan_kernel<<<groups, threads, lds, stream>>>(p);
+    if (p.end_later) cache_plan_end_kernel<<<(p.n_requests + 255) / 256, 256, 0, stream>>>(p);
 }
 
 void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, long long k_stride, long long v_stride, const int *slots,

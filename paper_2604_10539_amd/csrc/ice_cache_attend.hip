@@ -187,7 +187,12 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
     static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
     constexpr int R = kRows / PACK;  // rows in a tile of columns
     constexpr int Q = W * kStep;     // keys of a step of all waves
-    __shared__ float s_acc[W][kRows][kRecord];
+    // More than one tile of columns leaves no registers for a step on its way: three steps of a wave are copied to LDS by direct loads
+    // (where the waves' sums meet later), [two tiles' key codes in operand order][their value codes][their scales].
+    constexpr int kDepth = 3, kStage = 4352;
+    constexpr size_t kSums = sizeof(float) * W * kRows * kRecord, kStages = NT > 1 ? (size_t)W * kDepth * kStage : 0;
+    __shared__ __attribute__((aligned(16))) char s_raw[kSums > kStages ? kSums : kStages];
+    float(*s_acc)[kRows][kRecord] = reinterpret_cast<float(*)[kRows][kRecord]>(s_raw);
     __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of Q keys before each request
     __shared__ unsigned s_wave[W];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -384,8 +389,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const uint32_t cut1 = PACK > 1 && term >= 1 ? 0xFFFF0000u : 0u, cut2 = PACK > 2 && term >= 2 ? 0xFFFF0000u : 0u;
-        // Step n; between(): what is to be requested once the key codes have been used.
-        auto attend = [&](int n, Keys &y, auto between) __attribute__((always_inline)) {
+        // Step n; take_values(): where the value codes are still to be fetched into y.
+        auto attend = [&](int n, Keys &y, auto take_values) __attribute__((always_inline)) {
             const int key0 = (step0 + wave + W * n) * kStep;
             f32x4 d[NT][2];
 #pragma unroll
@@ -401,7 +406,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                 }
             }
             const uint32_t bad = y.bad;
-            between();
+            take_values();
             if (key0 < all_low || key0 + kStep > all_high || bad != 0) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -494,20 +499,53 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                     request(n + 2, x);
                     attend(n + 1, y, [] {});
                 }
-            } else {  // no room for a second one: codes are requested as soon as the last ones have been used
-                Keys x;
-                request_keys(at.held, 0, x);
-                request_values(at.held, 0, x);
+            } else {
+                char *const stage = s_raw + wave * (kDepth * kStage);
+                uint32_t missing = 0;  // tiles that do not exist, two bits a step, the latest request's lowest
+                auto request = [&](int n) __attribute__((always_inline)) {
+                    if (n % kAhead == 0 && n) turn_places(n);
+                    const int id0 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead)), id1 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead) + 1);
+                    missing = missing << 2 | (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u);
+                    const uint8_t *t0 = a.c.data + (size_t)max(id0, 0) * kCacheTileBytes, *t1 = a.c.data + (size_t)max(id1, 0) * kCacheTileBytes;
+                    char *to_lds = stage + (n % kDepth) * kStage;
+                    lds_dma16((const uint4 *)(t0 + k_at), to_lds);
+                    lds_dma16((const uint4 *)(t1 + k_at), to_lds + 1024);
+                    lds_dma16((const uint4 *)(t0 + kCacheV + 16 * lane), to_lds + 2048);
+                    lds_dma16((const uint4 *)(t1 + kCacheV + 16 * lane), to_lds + 3072);
+                    lds_dma4((const uint32_t *)((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
+                };
+                for (int n = 0; n < min(kDepth, n_mine); ++n) request(n);
                 for (int n = 0; n < n_mine; ++n) {
-                    const bool more = n + 1 < n_mine;
+                    const int later = min(kDepth - 1, n_mine - 1 - n);  // steps requested after this one, five loads each
+                    if (later == 2) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+                    else if (later == 1) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+                    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    const char *from_lds = stage + (n % kDepth) * kStage;
+                    const uint32_t gone = missing >> (2 * later);
+                    Keys x;
+                    x.bad = (gone & 1 ? 0xFFFFu : 0u) | (gone & 2 ? 0xFFFF0000u : 0u);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        x.k[b] = *(const u32x4 *)(from_lds + 1024 * b + 16 * lane);
+                        x.ks[b] = *(const uint8_t *)(from_lds + 4096 + 128 * b + (ks_at - kCacheKS));
+                    }
                     attend(n, x, [&]() __attribute__((always_inline)) {
-                        if (!more) return;
-                        if ((n + 1) % kAhead == 0) turn_places(n + 1);
-                        request_keys(at.held, n + 1, x);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x.v[b][i] = *(const uint32_t *)(from_lds + 2048 + 1024 * b + (v_at - kCacheV) + 256 * i);
+                            x.vs[b] = *(const uint32_t *)(from_lds + 4096 + 128 * b + (vs_at - kCacheKS));
+                        }
                     });
-                    if (more) request_values(at.held, n + 1, x);
+                    if (n + kDepth < n_mine) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stage has been read)
+                        request(n + kDepth);
+                    }
                 }
+                __syncthreads();  // (the sums go where the stages were)
             }
+        } else if constexpr (NT > 1) {
+            __syncthreads();
         }
 
         // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
@@ -994,7 +1032,12 @@ static void launch_few(const CacheAttend &a, hipStream_t stream) {
         else if (a.out_bf16) cache_attend_kernel<W, 1, 3, 1, LIST><<<grid, block, 0, stream>>>(a);
         else cache_attend_kernel<W, 1, 3, 3, LIST><<<grid, block, 0, stream>>>(a);
     }
-    if (!a.whole) cache_merge_kernel<8><<<dim3(a.few_groups, std::min(a.rows, a.max_query * a.G)), kMergeThreads, 0, stream>>>(a);
+    if (a.whole) return;
+    // threads for four records of a unit at a time: one trip for most
+    const int rows = std::min(a.rows, a.max_query * a.G), per_unit = a.few_groups / std::max(1, a.n_here * a.c.H) + 2;
+    if (per_unit <= 4) cache_merge_kernel<1><<<dim3(a.few_groups, (rows + 7) / 8), kMergeThreads, 0, stream>>>(a);
+    else if (per_unit <= 8) cache_merge_kernel<2><<<dim3(a.few_groups, (rows + 3) / 4), kMergeThreads, 0, stream>>>(a);
+    else cache_merge_kernel<8><<<dim3(a.few_groups, rows), kMergeThreads, 0, stream>>>(a);
 }
 
 void launch_cache_attend(CacheAttend a, hipStream_t stream) {

@@ -126,7 +126,7 @@ def test_reading_gives_the_held_values_and_zeros_where_there_is_no_token():
 @pytest.mark.parametrize("requests,block,n_slots", [(1, 16, 1), (3, 64, 300), (5, 32, 5000), (40, 16, 4096), (1024, 16, 9000), (1025, 32, 700), (2500, 16, 20000),
                                                     (5000, 16, 4500)])
 def test_plans_follow_each_other(requests, block, n_slots):
-    from paper_2604_10539_amd import IceBlocks
+    from paper_2604_10539_amd import IceBlocks, ice_plan_blocks
     rng = np.random.default_rng([requests, block])
     width = 400 if requests <= 5 else 12
     n_blocks = max(8, min(requests * width, requests * 5 + 200))
@@ -144,7 +144,14 @@ def test_plans_follow_each_other(requests, block, n_slots):
         if step == 6:
             gain[:] = -1
         want = ref.plan(gain, lens, table, free_ids, n_free, block, n_slots)
+        # the same step into arrays of its own, from copies
+        copy = [t.clone() for t in (b.seq_len, b.block_table, b.free_ids, b.n_free)]
+        e = lambda n: torch.full((n,), 77, dtype=torch.int32, device="cuda")  # noqa: E731
+        apart = [e(requests), copy[1], copy[2], e(1), e(requests + 1), e(n_slots), e(4)]
+        ice_plan_blocks(i32(gain), copy[0], apart[0], copy[1], copy[2], copy[3], apart[3], apart[4], apart[5], apart[6], block)
         start, slots, info = b.plan(i32(gain), n_slots)
+        for x, y in zip(apart, (b.seq_len, b.block_table, b.free_ids, b.n_free, start, slots, info)):
+            assert torch.equal(x, y)
         got = [down(t) for t in (b.seq_len, b.block_table, b.free_ids, b.n_free, start, slots, info)]
         assert np.array_equal(got[6], want[6]), (step, got[6], want[6])
         for name, g, w in zip(("seq_len", "table", "free_ids", "n_free", "query_start", "slots"), got, want):
