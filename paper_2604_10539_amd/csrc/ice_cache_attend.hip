@@ -508,11 +508,11 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                     missing = missing << 2 | (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u);
                     const uint8_t *t0 = a.c.data + (size_t)max(id0, 0) * kCacheTileBytes, *t1 = a.c.data + (size_t)max(id1, 0) * kCacheTileBytes;
                     char *to_lds = stage + (n % kDepth) * kStage;
-                    lds_dma16((const uint4 *)(t0 + k_at), to_lds);
-                    lds_dma16((const uint4 *)(t1 + k_at), to_lds + 1024);
-                    lds_dma16((const uint4 *)(t0 + kCacheV + 16 * lane), to_lds + 2048);
-                    lds_dma16((const uint4 *)(t1 + kCacheV + 16 * lane), to_lds + 3072);
-                    lds_dma4((const uint32_t *)((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
+                    lds_dma_stream<16>((t0 + k_at), to_lds);
+                    lds_dma_stream<16>((t1 + k_at), to_lds + 1024);
+                    lds_dma_stream<16>((t0 + kCacheV + 16 * lane), to_lds + 2048);
+                    lds_dma_stream<16>((t1 + kCacheV + 16 * lane), to_lds + 3072);
+                    lds_dma_stream<4>(((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
                 };
                 for (int n = 0; n < min(kDepth, n_mine); ++n) request(n);
                 for (int n = 0; n < n_mine; ++n) {
@@ -606,7 +606,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 }
 
 // ------------------------------------------------------------------------------------------------------------ many queries
-// Attention of many query rows of a (request, KV head): 192 at a time, tiles of 16 dealt to the four waves, three each.
+// Attention of many query rows of a (request, KV head): 192 at a time, tiles of 16 dealt to the four waves, three each (two: 2091 us for
+// the case below; four do not fit the registers of two workgroups on a CU).
 //
 // Bound by the matrix unit, so the codes are converted once per workgroup and not once per wave: of a round of 64 keys a wave converts 16, as
 // the few-query kernel does in registers, and leaves the operands in LDS as they are (a KiB each, 16 bytes a lane), from where all waves take
@@ -619,6 +620,10 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 constexpr int kTiles = 3;                            // tiles of 16 rows per wave
 constexpr int kChunkRows = kWaves * kTiles * kRows;  // rows of a workgroup
 constexpr int kRound = kWaves * 16;                  // keys of a round
+// What the compiler is asked for between the products (kinds of instructions, and how many).  A chunk of 2048 queries on 32 K keys, two
+// requests: its own order 1852 us; operands two ahead 1826; weights beside products, 4 a product 1781, 3 1749, 2 1728, 1 1746.
+constexpr int kVector = 0x002, kMatrix = 0x008, kLdsRead = 0x100;
+constexpr int kAhead = 2, kWeightOps = 28, kBeside = 2;
 
 struct Chunks {  // how a request's row tiles lie in the flat work of one KV head
     int tiles;
@@ -766,133 +771,174 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         if (rounds > 0) request(held, 0);
         // the rounds of a wave with NX tiles of rows, without a branch on the tile between the products
         auto run = [&](auto count) __attribute__((always_inline)) {
-        for (int n = 0; n < rounds; ++n) {
-            const int buf = n & 1;
-            {  // this wave's keys of the round become operands
-                const int key0 = key_at + n * kRound + 16 * wave;
-                bool nan = false;
-                if (key0 < all_low || key0 + 16 > all_high || gone) {
+            for (int n = 0; n < rounds; ++n) {
+                const int buf = n & 1;
+                {  // this wave's keys of the round become operands
+                    const int key0 = key_at + n * kRound + 16 * wave;
+                    bool nan = false;
+                    if (key0 < all_low || key0 + 16 > all_high || gone) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = key0 + 4 * i + g;
-                        const uint32_t byte = 0xFFu << (8 * i);
-                        if (gone || key < from || key >= to) vsc &= ~byte;  // (what no row sees may hold anything)
-                        if ((vsc & byte) == byte) {
-                            nan = true;
-                            vsc &= ~byte;
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 4 * i + g;
+                            const uint32_t byte = 0xFFu << (8 * i);
+                            if (gone || key < from || key >= to) vsc &= ~byte;  // (what no row sees may hold anything)
+                            if ((vsc & byte) == byte) {
+                                nan = true;
+                                vsc &= ~byte;
+                            }
                         }
+                        nan = __any(nan);
                     }
-                    nan = __any(nan);
+                    if (lane == 0) s_flags[buf][wave] = (gone ? 1u : 0u) | (nan ? 2u : 0u);
+                    const float sc = __uint_as_float(ksc << 23);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s_k[buf][wave][j][lane] = eight(kc[j], sc);
+                    float vf[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vf[i] = scale_of(vsc, i);
+                    auto dims = [&](auto sel) __attribute__((always_inline)) {
+                        constexpr int j = decltype(sel)::value;
+                        uint32_t v0[2], v1[2];
+                        half_values<j>(vc, vf, v0, v1);
+                        uint2 *at = (uint2 *)&s_v[buf][wave >> 1][2 * j][lane] + (wave & 1);
+                        at[0] = make_uint2(v0[0], v0[1]);
+                        at[2 * 64] = make_uint2(v1[0], v1[1]);
+                    };
+                    dims(std::integral_constant<int, 0>());
+                    dims(std::integral_constant<int, 1>());
+                    dims(std::integral_constant<int, 2>());
+                    dims(std::integral_constant<int, 3>());
                 }
-                if (lane == 0) s_flags[buf][wave] = (gone ? 1u : 0u) | (nan ? 2u : 0u);
-                const float sc = __uint_as_float(ksc << 23);
+                if (n + 1 < rounds) {
+                    if (((n + 1) & 63) == 0) held = places(n + 1);
+                    request(held, n + 1);
+                }
+                lds_barrier();
+                // scores of the round's 64 keys (those behind the last one are masked)
+                constexpr int NX = decltype(count)::value, NB = kRound / 16;
+                const int key0 = key_at + n * kRound;
+                f32x4 d[NX][NB];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s_k[buf][wave][j][lane] = eight(kc[j], sc);
-                float vf[4];
+                for (int b = 0; b < NB; ++b) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) vf[i] = scale_of(vsc, i);
-                auto dims = [&](auto sel) __attribute__((always_inline)) {
-                    constexpr int j = decltype(sel)::value;
-                    uint32_t v0[2], v1[2];
-                    half_values<j>(vc, vf, v0, v1);
-                    uint2 *at = (uint2 *)&s_v[buf][wave >> 1][2 * j][lane] + (wave & 1);
-                    at[0] = make_uint2(v0[0], v0[1]);
-                    at[2 * 64] = make_uint2(v1[0], v1[1]);
-                };
-                dims(std::integral_constant<int, 0>());
-                dims(std::integral_constant<int, 1>());
-                dims(std::integral_constant<int, 2>());
-                dims(std::integral_constant<int, 3>());
-            }
-            if (n + 1 < rounds) {
-                if (((n + 1) & 63) == 0) held = places(n + 1);
-                request(held, n + 1);
-            }
-            lds_barrier();
-            const int n_steps = min(kRound / kStep, (to - key_at - n * kRound + kStep - 1) / kStep);
-            auto steps = [&](auto tiles) __attribute__((always_inline)) {
-                constexpr int NX = decltype(tiles)::value;
-#pragma unroll 1
-                for (int step = 0; step < n_steps; ++step) {
-                    const int key0 = key_at + n * kRound + step * kStep;
-                    f32x4 d[NX][2];
+                    for (int x = 0; x < NX; ++x) d[x][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int x = 0; x < NX; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < 4; ++j) {
+                        const u32x4 k = s_k[buf][b][j][lane];
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                        for (int x = 0; x < NX; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                    }
+                }
+                // (operands are read kAhead ahead of their products)
+                __builtin_amdgcn_sched_group_barrier(kLdsRead, kAhead, 0);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const u32x4 k = s_k[buf][2 * step + b][j][lane];
+                for (int i = 0; i < 4 * NB; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, NX, 0);
+                    if (i + kAhead < 4 * NB) __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
+                }
+                uint32_t flags = 0;
 #pragma unroll
-                            for (int x = 0; x < NX; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                for (int b = 0; b < NB; ++b) flags |= s_flags[buf][b] << (2 * b);
+                flags = (uint32_t)__builtin_amdgcn_readfirstlane((int)flags);
+                if (key0 < wave_low || key0 + kRound > wave_high || flags != 0) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 16 * b + 4 * i + g;
+                            const bool none = (flags >> (2 * b)) & 1;
+#pragma unroll
+                            for (int x = 0; x < NX; ++x)
+                                if (none || key < low[x] || key >= high[x]) d[x][b][i] = -INFINITY;
                         }
-                    const uint32_t flags = (uint32_t)__builtin_amdgcn_readfirstlane((int)(s_flags[buf][2 * step] | s_flags[buf][2 * step + 1] << 2));
-                    if (key0 < wave_low || key0 + kStep > wave_high || flags != 0) {
+                    if (flags & 0xAAu) {
+                        float nan[kTiles] = {};
+                        for (int step = 0; step < kRound / kStep; ++step)
+                            find_nan<kTiles>(a, table, h, key0 + step * kStep, from, to, g, low, high, nan);
+#pragma unroll
+                        for (int x = 0; x < NX; ++x)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
+                    }
+                }
+                float top[NX];
+                bool rise = false;
+#pragma unroll
+                for (int x = 0; x < NX; ++x) {
+                    float t = d[x][0][0];
+#pragma unroll
+                    for (int e = 1; e < 4 * NB; ++e) t = fmaxf(t, d[x][e >> 2][e & 3]);
+                    top[x] = t * a.scale_log2;
+                    rise |= top[x] > m[x] + kSlack;
+                }
+                if (__any(rise)) {
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) {
+                        float t = fmaxf(top[x], __shfl_xor(top[x], 16));
+                        t = fmaxf(t, __shfl_xor(t, 32));
+                        const float mn = t > m[x] + kSlack ? t : m[x], alpha = __builtin_amdgcn_exp2f(m[x] - mn);
+                        m[x] = mn;
+                        l[x] *= alpha;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) acc[x][j] *= alpha;
+                    }
+                }
+                // weights and the value product, without a branch, so that the one's instructions fill the other's time
+#pragma unroll
+                for (int step = 0; step < kRound / kStep; ++step) {
+                    u32x4 w[NX][SETS];
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) {
+                        float p[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const int key = key0 + 16 * (e >> 2) + 4 * (e & 3) + g;
-                            const bool none = (flags >> (2 * (e >> 2))) & 1;
-#pragma unroll
-                            for (int x = 0; x < NX; ++x)
-                                if (none || key < low[x] || key >= high[x]) d[x][e >> 2][e & 3] = -INFINITY;
+                            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(d[x][2 * step + (e >> 2)][e & 3], a.scale_log2, -m[x]));
+                            l[x] += p[e];
                         }
-                        if (flags & 10u) {
-                            float nan[kTiles] = {};
-                            find_nan<kTiles>(a, table, h, key0, from, to, g, low, high, nan);
+                        if constexpr (SETS == 1) {
 #pragma unroll
-                            for (int x = 0; x < NX; ++x)
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
-                        }
-                    }
-                    if constexpr (SETS == 1) {
-                        u32x4 w[NX];
-#pragma unroll
-                        for (int x = 0; x < NX; ++x) {
-                            float p[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
-                            softmax(p, a.scale_log2, m[x], l[x], acc[x]);
-#pragma unroll
-                            for (int e = 0; e < 8; e += 2) w[x][e >> 1] = pack2(p[e], p[e + 1]);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const u32x4 v = s_v[buf][step][j][lane];
-#pragma unroll
-                            for (int x = 0; x < NX; ++x) acc[x][j] = mfma(v, w[x], acc[x][j]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < NX; ++x) {
-                            float p[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
-                            softmax(p, a.scale_log2, m[x], l[x], acc[x]);
-                            u32x4 w[SETS];
+                            for (int e = 0; e < 8; e += 2) w[x][0][e >> 1] = pack2(p[e], p[e + 1]);
+                        } else {
 #pragma unroll
                             for (int t = 0; t < SETS; ++t) {
                                 if (t > 0)
 #pragma unroll
                                     for (int e = 0; e < 8; ++e) p[e] = cut(p[e], 0xFFFF0000u);
-                                w[t] = tops(p);
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const u32x4 v = s_v[buf][step][j][lane];
-#pragma unroll
-                                for (int t = 0; t < SETS; ++t) acc[x][j] = mfma(v, w[t], acc[x][j]);
+                                w[x][t] = tops(p);
                             }
                         }
                     }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const u32x4 v = s_v[buf][step][j][lane];
+#pragma unroll
+                        for (int x = 0; x < NX; ++x)
+#pragma unroll
+                            for (int t = 0; t < SETS; ++t) acc[x][j] = mfma(v, w[x][t], acc[x][j]);
+                    }
                 }
-            };
-            steps(count);
-        }
+                // the order of the products: the first step's weights (kWeightOps a tile); its products, beside each of which kBeside
+                // instructions of the second step's weights go; the second step's products
+                __builtin_amdgcn_sched_group_barrier(kVector, kWeightOps * NX, 1);
+                __builtin_amdgcn_sched_group_barrier(kLdsRead, kAhead, 1);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                    for (int x = 0; x < NX * SETS; ++x) {
+                        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 1);
+                        __builtin_amdgcn_sched_group_barrier(kVector, kBeside, 1);
+                    }
+                    __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 1);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, NX * SETS, 1);
+                    __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 1);
+                }
+            }
         };
         // (a wave without rows converts all the same; its one tile is not written)
-        if (n_tiles >= 3) run(std::integral_constant<int, 3>());
-        else if (n_tiles == 2) run(std::integral_constant<int, 2>());
+        if (n_tiles > 1) run(std::integral_constant<int, kTiles>());
         else run(std::integral_constant<int, 1>());
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1;

@@ -300,10 +300,13 @@ __device__ inline void lds_dma16(const uint4 *src, char *lds_base) {
     const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) char *)lds_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(base) : "memory", "m0");
 }
-// The same with 4 bytes per lane: lane l's bytes land at lds_base + 4 l.
-__device__ inline void lds_dma4(const uint32_t *src, char *lds_base) {
+// The same with the non-temporal hint, 16 or 4 bytes per lane.
+template <int BYTES>
+__device__ inline void lds_dma_stream(const void *src, char *lds_base) {
+    static_assert(BYTES == 16 || BYTES == 4, "one of the two");
     const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) char *)lds_base);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(base) : "memory", "m0");
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(src), "s"(base) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off nt" ::"v"(src), "s"(base) : "memory", "m0");
 }
 __device__ inline void wait_lds_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
