@@ -570,30 +570,46 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                 }
             }
             __syncthreads();
-            for (int in = tid >> 5; in < min(R, n_rows - R * x); in += W * 2) {
-                const int row = R * x + in;
-                float top = kNoMax;
+            // (with one tile the reads of a thread's rows stand side by side, rows behind the last one read what lies there and write nothing: 24
+            // requests of mixed lengths 273 us, 281 row by row; with three tiles the registers for that are not there: drafts 64 us, 58)
+            constexpr int kPasses = NT == 1 ? (R + 2 * W - 1) / (2 * W) : 1;
+            for (int in0 = tid >> 5; in0 < (NT == 1 ? 2 * W : min(R, n_rows - R * x)); in0 += 2 * W * kPasses) {
+                f32x4 sum[kPasses];
+                float top[kPasses], all[kPasses];
 #pragma unroll
-                for (int w = 0; w < W; ++w) top = fmaxf(top, s_acc[w][in][kD]);
-                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-                float all = 0.f;
+                for (int pass = 0; pass < kPasses; ++pass) {
+                    const int in = min(in0 + 2 * W * pass, R - 1);
+                    float2 ml[W];
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(s_acc[w][in][kD] - top);
-                    f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
+                    for (int w = 0; w < W; ++w) ml[w] = *(const float2 *)&s_acc[w][in][kD];
+                    top[pass] = kNoMax;
 #pragma unroll
-                    for (int t = 1; t < PACK; ++t) v += *(const f32x4 *)(s_acc[w][in + t * R] + d0);
-                    sum += v * f;
-                    all += s_acc[w][in][kD + 1] * f;
+                    for (int w = 0; w < W; ++w) top[pass] = fmaxf(top[pass], ml[w].x);
+                    sum[pass] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    all[pass] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        const float f = __builtin_amdgcn_exp2f(ml[w].x - top[pass]);
+                        f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
+#pragma unroll
+                        for (int t = 1; t < PACK; ++t) v += *(const f32x4 *)(s_acc[w][in + t * R] + d0);
+                        sum[pass] += v * f;
+                        all[pass] += ml[w].y * f;
+                    }
                 }
-                if (whole) {
-                    put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, top, all);
-                } else {
-                    float *r = record + (size_t)row * kRecord;
-                    *(f32x4 *)(r + d0) = sum;
-                    if (d0 == 0) {
-                        r[kD] = top;
-                        r[kD + 1] = all;
+#pragma unroll
+                for (int pass = 0; pass < kPasses; ++pass) {
+                    const int in = in0 + 2 * W * pass, row = R * x + in;
+                    if (in >= R || row >= n_rows) continue;
+                    if (whole) {
+                        put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum[pass], top[pass], all[pass]);
+                    } else {
+                        float *r = record + (size_t)row * kRecord;
+                        *(f32x4 *)(r + d0) = sum[pass];
+                        if (d0 == 0) {
+                            r[kD] = top[pass];
+                            r[kD + 1] = all[pass];
+                        }
                     }
                 }
             }
