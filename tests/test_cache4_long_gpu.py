@@ -122,3 +122,14 @@ def test_captured_chunks_and_lists_follow_their_lengths():
         torch.cuda.synchronize()
         for w, g, o in zip(want, got, got_other):
             assert torch.equal(w, g) and torch.equal(w, o), i
+
+
+@pytest.mark.parametrize("group,queries,lens,dtype", [(2, 1, [150000, 140000, 160000, 147000], torch.float32), (8, 5, [90000, 120000, 105000, 98000], torch.bfloat16),
+                                                      (16, 60, [41000, 40500, 41500, 43000], torch.float32)], ids=["few", "draft", "chunk"])
+def test_as_many_long_pieces_as_there_are_workgroups(group, queries, lens, dtype):
+    """Requests so long that the work is cut into pieces of two or three lengths.  Their blocks are shared: a small pool, long tables."""
+    rng = np.random.default_rng(queries)
+    heads, block, n_blocks = 1 if queries == 60 else 2, 64, 200
+    table = rng.integers(0, n_blocks, (len(lens), -(-max(lens) // block))).astype(np.int32)
+    data = random_pool(rng, n_blocks, heads, block)
+    run_attend(rng, heads, group, block, lens, [queries] * len(lens), 0, dtype, garbage=False, data=data, table=table)
