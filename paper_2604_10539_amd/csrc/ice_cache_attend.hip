@@ -90,9 +90,10 @@ struct Keys {
 constexpr unsigned kCus = 256;
 struct Pieces {
     unsigned groups, per, from1, from2, total;  // workgroups, those of a third (half, whole), where the pieces of the second and third begin
-    __device__ Pieces(unsigned total_, unsigned most) : total(__builtin_amdgcn_readfirstlane(total_)) {
+    // whole: pieces are units, which must not be cut (there is no room for records)
+    __device__ Pieces(unsigned total_, unsigned most, bool whole) : total(__builtin_amdgcn_readfirstlane(total_)) {
         groups = min(most, max(total, 1u));
-        const bool uneven = (groups == 2 * kCus || groups == 3 * kCus) && total >= 12 * groups;
+        const bool uneven = !whole && (groups == 2 * kCus || groups == 3 * kCus) && total >= 12 * groups;
         per = uneven ? kCus : groups;
         from1 = from2 = total;
         if (uneven && groups == 2 * kCus) from1 = total / 32 * 19;
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         if (tid == 0) s_before[a.n_here] = total;
         __syncthreads();
     }
-    const Pieces pieces(total, gridDim.x);
+    const Pieces pieces(total, gridDim.x, a.whole);
     if (blockIdx.x >= pieces.groups || total == 0) {
         if (tid == 0 && a.notes) a.notes[blockIdx.x].first = -1;
         return;
@@ -705,7 +706,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     }
     if (tid == 0) s_before[a.n_here] = total;
     __syncthreads();
-    const Pieces pieces(total, gridDim.x);
+    const Pieces pieces(total, gridDim.x, false);
     if (blockIdx.x >= pieces.groups || total == 0) {
         if (tid == 0) a.notes[blockIdx.x].first = -1;
         return;

@@ -133,3 +133,26 @@ def test_as_many_long_pieces_as_there_are_workgroups(group, queries, lens, dtype
     table = rng.integers(0, n_blocks, (len(lens), -(-max(lens) // block))).astype(np.int32)
     data = random_pool(rng, n_blocks, heads, block)
     run_attend(rng, heads, group, block, lens, [queries] * len(lens), 0, dtype, garbage=False, data=data, table=table)
+
+
+@pytest.mark.parametrize("requests,heads,most", [(256, 2, 3500), (384, 2, 4100)])
+def test_long_lists_of_as_many_units_as_fill_the_card(requests, heads, most):
+    """Two or three whole units for every CU, each of many steps: no unit is cut, each list is read to its end."""
+    rng = np.random.default_rng(most)
+    group, block, n_blocks, width = 1, 32, 150, 20
+    data = random_pool(rng, n_blocks, heads, block)
+    table = rng.integers(0, n_blocks, (requests, width)).astype(np.int32)
+    lens = rng.integers(1, width * block + 1, requests)
+    c = make(n_blocks, heads, block, data)
+    pos = rng.integers(0, lens[:, None, None], (requests, heads, most)).astype(np.int32)
+    n_tok = rng.integers(most - 700, most + 1, (requests, heads)).astype(np.int32)
+    q = ref.to_bf16(rng.standard_normal((requests, heads * group, D)).astype(np.float32))
+    out, lse = c.attend_tokens(up(q), i32(lens), i32(table), i32(pos), i32(n_tok), with_lse=True)
+    res = []
+    for s in range(requests):
+        at = np.arange(lens[s])
+        for h in range(heads):
+            k, v = ref.rows(data, table[s, at // block], at % block, h)
+            p = pos[s, h, : n_tok[s, h]]
+            res.append(ref.softmax_rows(ref.widen(q[s, h: h + 1]).astype(np.float64), k[p], v[p], np.ones((1, len(p)), dtype=bool), False))
+    check(out, lse, [np.stack([r[i] for r in res]).reshape(requests, heads, *res[0][i].shape[1:]) for i in range(4)])
