@@ -270,14 +270,19 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDims c, int n_requ
 
 }  // namespace
 
-// A workgroup's threads for what the step can bring at most, as many workgroups as there are CUs at most.
+// A workgroup's threads for the scan of the lengths (256 requests: 256 threads 5.8 us, 1024 7.3; 512 requests: 512 threads 6.2 us, 1024 8.0; 1000: 6.9
+// and 8.6, 256 threads 8 to 10; 2000: 512 threads 8.5 to 10.5, 1024 9.7).  As many workgroups as CUs at most for what the step can
+// bring; one where few slots are filled and a second launch would have to write the lengths (one and many, us: 16 requests x 1 token
+// 4.4 and 5.8, 512 x 1 5.5 and 7.0, 64 x 16 5.9 and 6.0, 1000 x 1 8.6 and 7.8).
+constexpr int kPlanAlone = 512;
 void launch_cache_plan(CachePlan p, hipStream_t stream) {
     const long long most = p.n_slots + std::min<long long>((long long)p.n_requests * p.max_blocks, p.n_blocks);
-    const int threads = p.n_requests <= 256 && p.n_slots <= 1024 ? 256 : kPlanThreads;
-    const int groups = p.n_slots <= 4096 && most <= 32768 ? 1 : (int)std::min<long long>(256, (most + threads - 1) / threads);
+    const bool in_place = p.seq_len == p.cached_len || p.n_free_left == p.n_free;
+    const int threads = p.n_requests <= 256 ? 256 : p.n_requests <= 1024 ? 512 : kPlanThreads;
+    const int groups = in_place && p.n_slots <= kPlanAlone ? 1 : (int)std::min<long long>(256, (most + threads - 1) / threads);
     const size_t lds = (3 * (p.n_requests + 1) + (p.n_requests <= kPlanItems ? 2 * p.n_requests : 0)) * sizeof(unsigned);
     if (lds > 65536 - 1024) allow_dynamic_lds((const void *)cache_plan_kernel, lds);
-    p.end_later = groups > 1 && (p.seq_len == p.cached_len || p.n_free_left == p.n_free);
+    p.end_later = groups > 1 && in_place;
     cache_plan_kernel<<<groups, threads, lds, stream>>>(p);
     if (p.end_later) cache_plan_end_kernel<<<(p.n_requests + 255) / 256, 256, 0, stream>>>(p);
 }
