@@ -354,11 +354,14 @@ ice_status_t ice_cache_read(const ice_cache_t *cache, int32_t n_requests, const 
  * positions up to its own, with window > 0 only the last `window` of these.  The step's tokens are written before.
  *   q: bf16, row t at q + t * q_stride elements (a multiple of 8), [n_kv_heads * group_size][128] within it; group_size 1 to 16, query
  *     head h reads KV head h / group_size.
+ *   block_table: rows of at most 2^30 tokens.
  *   query_start int32 [n_requests + 1], ascending from 0, at most n_tokens (the rows of q and out).  max_query: no request has more queries
  *     (those beyond are left out).  max_keys: about the longest seq_len, a hint for how the work is cut, not a limit.
  *   out: fp32 or bf16 [n_tokens][n_kv_heads * group_size][128]; lse_or_null fp32 [n_tokens][n_kv_heads * group_size], the natural logarithm of the
  *     softmax's sum.  A query that sees nothing (or only scores of -inf) gets 0 and -inf.  Rows behind query_start[n_requests] are left as they were.
- *   workspace: ice_cache_attend_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0). */
+ *   workspace: ice_cache_attend_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
+ * UNSUPPORTED where the work could not be counted in 31 bits: (tokens of a table row / 128 + 3) * (max_query * group_size / 192 + 2) *
+ * requests (at most 1024 of them) * n_kv_heads; give the longest rows and the most queries that there are. */
 enum { ICE_OUT_F32 = 0, ICE_OUT_BF16 = 1 };
 size_t ice_cache_attend_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t max_query, int32_t max_keys);
 ice_status_t ice_cache_attend(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,

@@ -508,6 +508,8 @@ size_t ice_cache_attend_tokens_bytes(const ice_cache_t *c, int32_t G, int32_t n_
 static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
                                  float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
     if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
+    // (positions are rounded up to steps in 32 bits)
+    if ((long long)a.max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: more than 2^30 tokens", a.max_blocks);
     // (the sum of a launch's pieces of 128 keys is counted in 31 bits)
     const double keys = a.pos ? a.max_keys : (double)a.max_blocks * c->block_size, rows = a.pos ? 1 : a.max_query * (double)a.G;
     if ((keys / 128 + 3) * (rows / 192 + 2) * (a.S < 1024 ? a.S : 1024) * c->n_kv_heads >= 2147483648.0)

@@ -131,3 +131,16 @@ def test_the_plain_forms_of_these_tests():
     assert got[0].tolist() == [17, 13, 5] and got[6].tolist() == [3, 1, 2, 0]
     assert got[2][:4].tolist() == [0, 1, 3, 5] and got[1][0].tolist() == [4, 5, 9] and got[3] == 3
     assert got[4].tolist() == [0, 3, 3, 3] and got[5].tolist() == [4 * 16 + 14, 4 * 16 + 15, 5 * 16, -1, -1, -1]
+
+
+def test_attention_refuses_rows_whose_positions_do_not_fit():
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(FAKE, 1000, 2, 64)
+    args = dict(q=FAKE, qs=1024, G=4, n=2, start=FAKE, tokens=2, max_query=1, sl=FAKE, max_keys=4096, table=FAKE, mb=2 ** 24 + 1, window=0, out=FAKE, ot=0,
+                lse=None, ws=FAKE, wb=0)
+    assert status(p.ice_cache_attend, c, *args.values()) == b.ICE_ERR_SHAPE and "2^30" in p.ice_last_error()
+    # (the longest rows that pass get as far as the workspace)
+    assert status(p.ice_cache_attend, c, *{**args, "mb": 2 ** 24}.values()) == b.ICE_ERR_CAPACITY
+    listed = dict(q=FAKE, qs=1024, G=4, n=2, sl=FAKE, table=FAKE, mb=2 ** 24 + 1, pos=FAKE, n_tok=FAKE, max_tok=4096, out=FAKE, ot=0, lse=None, ws=FAKE, wb=0)
+    assert status(p.ice_cache_attend_tokens, c, *listed.values()) == b.ICE_ERR_SHAPE and "2^30" in p.ice_last_error()
