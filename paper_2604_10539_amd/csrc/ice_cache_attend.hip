@@ -531,7 +531,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                     lds_dma_stream<16>((t0 + k_at), to_lds);
                     lds_dma_stream<16>((t1 + k_at), to_lds + 1024);
                     lds_dma_stream<16>((t0 + kCacheV + 16 * lane), to_lds + 2048);
-                    lds_dma_stream<16>((t1 + kCacheV + 16 * lane), to_lds + 3072);
+                    lds_dma_stream<16>((t1 + kCacheV + 16 * lane), to_lds + 3 * 1024);
                     lds_dma_stream<4>(((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
                 };
                 for (int n = 0; n < min(kDepth, n_mine); ++n) request(n);
