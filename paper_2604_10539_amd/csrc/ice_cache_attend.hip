@@ -44,16 +44,28 @@ template <bool LIST>
 struct Unit {
     int row0, n_query, len;  // first query row, queries, cached tokens (listed: entries of the list)
     int tokens;              // cached tokens
-    __device__ Unit(const CacheAttend &a, int s, int h) {
-        tokens = max(a.seq_len[s], 0);
-        tokens = (int)min((long long)tokens, (long long)a.max_blocks << (a.c.tile_shift + 4));
+    // UNIFORM: the same on all lanes.  A request's words are asked for before one is looked at: left to the compiler, the length was asked for
+    // once the request was known to have queries, a trip more (0.1 to 1 us a call).
+    template <bool UNIFORM>
+    __device__ Unit(const CacheAttend &a, int s, int h, std::integral_constant<bool, UNIFORM>) {
+        int t = a.seq_len[s], x = LIST ? a.n_tok[s * a.c.H + h] : a.query_start[s], y = LIST ? 0 : a.query_start[s + 1];
+        if constexpr (LIST) {
+        } else if constexpr (UNIFORM) {
+            t = __builtin_amdgcn_readfirstlane(t);
+            x = __builtin_amdgcn_readfirstlane(x);
+            y = __builtin_amdgcn_readfirstlane(y);
+            asm volatile("" : "+s"(t), "+s"(x), "+s"(y));
+        } else {
+            asm volatile("" : "+v"(t), "+v"(x), "+v"(y));
+        }
+        tokens = (int)min((long long)max(t, 0), (long long)a.max_blocks << (a.c.tile_shift + 4));
         if constexpr (LIST) {
             row0 = s;
             n_query = 1;
-            len = min(max(a.n_tok[s * a.c.H + h], 0), a.max_keys);
+            len = min(max(x, 0), a.max_keys);
         } else {
-            row0 = min(max(a.query_start[s], 0), a.T);
-            n_query = min(max(a.query_start[s + 1], row0), a.T) - row0;
+            row0 = min(max(x, 0), a.T);
+            n_query = min(max(y, row0), a.T) - row0;
             len = tokens;
         }
     }
@@ -227,7 +239,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             const int e = e0 + tid;
             unsigned n = 0;
             if (e < a.n_here) {
-                const Unit<LIST> u(a, a.first + e, 0);
+                const Unit<LIST> u(a, a.first + e, 0, std::false_type());
                 const int q = u.queries(a);
                 // at least one where there are rows, which want their outputs; none where the other kernel does the request
                 if (q > 0 && q * a.G <= NT * R)
@@ -285,7 +297,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         s = __builtin_amdgcn_readfirstlane(s) + a.first;
         h = __builtin_amdgcn_readfirstlane(h);
         const unsigned stop = min(u1, end);
-        const Unit<LIST> unit(a, s, h);
+        const Unit<LIST> unit(a, s, h, std::true_type());
         const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
         if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
             now = stop;
@@ -691,7 +703,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     unsigned total = 0;
     for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
         const int e = e0 + tid;
-        const unsigned n = e < a.n_here ? Chunks(a, Unit<false>(a, a.first + e, 0)).per_head * (unsigned)a.c.H : 0u;
+        const unsigned n = e < a.n_here ? Chunks(a, Unit<false>(a, a.first + e, 0, std::false_type())).per_head * (unsigned)a.c.H : 0u;
         const unsigned incl = (unsigned)wave_scan_add((int)n);
         if (lane == 63) s_wave[wave] = incl;
         __syncthreads();
@@ -724,7 +736,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     for (unsigned now = begin; now < end;) {
         while (s_before[entry + 1] <= now) ++entry;
         const int s = __builtin_amdgcn_readfirstlane(entry) + a.first;
-        const Unit<false> unit(a, s, 0);
+        const Unit<false> unit(a, s, 0, std::true_type());
         const Chunks ch(a, unit);
         const unsigned first = s_before[entry];
         const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
