@@ -156,3 +156,12 @@ def test_long_lists_of_as_many_units_as_fill_the_card(requests, heads, most):
             p = pos[s, h, : n_tok[s, h]]
             res.append(ref.softmax_rows(ref.widen(q[s, h: h + 1]).astype(np.float64), k[p], v[p], np.ones((1, len(p)), dtype=bool), False))
     check(out, lse, [np.stack([r[i] for r in res]).reshape(requests, heads, *res[0][i].shape[1:]) for i in range(4)])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("group,queries,window", [(4, 1, 0), (4, 2, 70), (16, 1, 0), (10, 3, 0), (8, 5, 300)])
+def test_whole_units_of_many_requests(group, queries, window, dtype):
+    """Enough (request, KV head) pairs, short enough, that none is cut: one workgroup each, no scratch; 4 to 40 rows."""
+    rng = np.random.default_rng([group, queries])
+    lens = [0, 1, queries, 1000] + [int(x) for x in rng.integers(0, 1000, 16)]
+    run_attend(rng, 7, group, 16, lens, [queries] * 19 + [0], window, dtype, garbage=False, max_len=1000)
