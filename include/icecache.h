@@ -426,6 +426,17 @@ ice_status_t ice_debug_build_plan(const ice_config_t *cfg, int32_t n_tokens, int
 ice_status_t ice_debug_near_bounds(int32_t n, const float *key_norm2, const float *own_norm2, const float *own_score,
                                    const float *best_score, float *need, float *dist2);
 
+/* Test hook: how ice_cache_attend (query_start null: ice_cache_attend_tokens) cuts its work, worked out on the host with the kernels' own
+ * arithmetic; nothing is enqueued.  query_start [n_requests + 1] and len (seq_len [n_requests], or n_tok [n_requests, n_kv_heads]) are HOST arrays.
+ * A part is what a workgroup does at a time: of a unit (some query rows of a KV head of a request), whose flat work is the quanta [u0, u1), the quanta [now,
+ * stop).  *n_parts = their number; the first max_parts of them in parts, 15 words each: first request of the launch, kernel (0: few
+ * queries, 1: many), workgroup, request, KV head, first row of the unit (query * group_size + head of the group), rows, first key and
+ * the one behind the last, u0, u1, now, stop, the record that takes its sums (-1: none, the part is the whole unit), and, of the part that ends
+ * a unit that was cut, the workgroup of its first part (else -1). */
+ice_status_t ice_debug_cache_cut(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, const int32_t *query_start, int32_t n_tokens,
+                                 int32_t max_query, const int32_t *len, int32_t max_keys, int32_t max_blocks, int32_t window, int32_t *parts,
+                                 int64_t max_parts, int64_t *n_parts);
+
 /* Test hook for the failure path of ice_select / ice_select_attend when a unit is served by several
  * workgroups (fewer than 256 units): those workgroups hand their page scores to the last one of
  * them through device memory, and that one waits for a missing score only a bounded number of

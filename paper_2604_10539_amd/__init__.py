@@ -1,7 +1,7 @@
 """MI355X-native IceCache hot path: HIP kernels behind a C ABI (include/icecache.h) and a thin
 ctypes binding.  Importing the package does not load the library; the first call does."""
 from .binding import (ICE_OUT_BF16, ICE_OUT_F32, IceBlocks, IceCache, IceCacheDesc, ice_cache_attend, ice_cache_attend_bytes,  # noqa: F401
-                      ice_cache_attend_tokens, ice_cache_attend_tokens_bytes, ice_cache_bytes, ice_cache_read, ice_cache_write, ice_plan_blocks, make_cache_desc,
+                      ice_cache_attend_tokens, ice_cache_attend_tokens_bytes, ice_cache_bytes, ice_cache_read, ice_cache_write, ice_debug_cache_cut, ice_plan_blocks, make_cache_desc,
                       ICE_GEOMETRY_RAW, ICE_GEOMETRY_TRANSFORMED, ICE_STAGE_ASSIGN, ICE_STAGE_MEANS,  # noqa: F401
                       ICE_STAGE_PAGINATE, ICE_STAGE_SORT, IceConfig, IceError, IceIndex, IceIndexView, ice_attend,
                       ice_attend_noalloc, ice_attend_resident, ice_attend_tokens, ice_build_index, ice_create,

@@ -21,7 +21,7 @@ SYMBOLS = ["ice_workspace_bytes", "ice_create", "ice_destroy", "ice_build_index"
            "ice_attend", "ice_attend_noalloc", "ice_select_attend", "ice_attend_resident", "ice_select_attend_resident", "ice_selected_tokens", "ice_attend_tokens", "ice_select_hier", "ice_select_hier3", "ice_build_top_level", "ice_export_top_level", "ice_set_geometry", "ice_export_geometry", "ice_export_index", "ice_import_index", "ice_debug_assign", "ice_debug_rerun_stage", "ice_debug_build_plan", "ice_debug_near_bounds", "ice_debug_select_fault",
            "ice_debug_peak_read", "ice_debug_peak_mfma", "ice_last_error",
            "ice_cache_bytes", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
-           "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes"]
+           "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes", "ice_debug_cache_cut"]
 
 
 class IceConfig(C.Structure):
@@ -125,6 +125,7 @@ def lib() -> C.CDLL:
         L.ice_cache_attend_bytes.argtypes = [desc, i32, i32, i32, i32]
         L.ice_cache_attend.argtypes = [desc, ptr, i64, i32, i32, ptr, i32, i32, ptr, i32, ptr, i32, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         L.ice_cache_attend_tokens.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
+        L.ice_debug_cache_cut.argtypes = [desc, i32, i32, ptr, i32, i32, ptr, i32, i32, i32, ptr, i64, C.POINTER(C.c_int64)]
         for name in SYMBOLS:
             if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
                             "ice_cache_attend_tokens_bytes"):
@@ -619,6 +620,24 @@ class IceIndex:
         best = torch.empty((self.U, n), dtype=torch.float32, device=self.device) if with_best else None
         ice_debug_assign(self.handle, K, n, centroids_bf16, Cn, a, best, stream)
         return a, best
+
+
+CUT_FIELDS = ("first", "many", "workgroup", "request", "head", "base", "rows", "from", "to", "u0", "u1", "now", "stop", "record", "note")
+
+
+def ice_debug_cache_cut(cache: IceCacheDesc, group_size, n_requests, query_start, n_tokens, max_query, length, max_keys, max_blocks, window=0):
+    """numpy arrays: query_start (None: listed tokens) and length int32 on the host -> the parts, int32 [n, 15] in the order of CUT_FIELDS."""
+    import numpy as np
+    start = None if query_start is None else np.ascontiguousarray(query_start, dtype=np.int32)
+    length = np.ascontiguousarray(length, dtype=np.int32)
+    n = C.c_int64(0)
+    parts = np.empty((1 << 12, len(CUT_FIELDS)), dtype=np.int32)
+    while True:
+        _check(lib().ice_debug_cache_cut(C.byref(cache), group_size, n_requests, None if start is None else start.ctypes.data, n_tokens, max_query,
+                                         length.ctypes.data, max_keys, max_blocks, window, parts.ctypes.data, len(parts), C.byref(n)))
+        if n.value <= len(parts):
+            return parts[: n.value]
+        parts = np.empty((n.value, len(CUT_FIELDS)), dtype=np.int32)
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us against 0.5: it does not ask whether CUDA is up)

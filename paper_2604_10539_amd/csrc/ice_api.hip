@@ -571,6 +571,23 @@ ice_status_t ice_cache_attend_tokens(const ice_cache_t *c, const void *q, int64_
     return cache_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need, stream, "ice_cache_attend_tokens");
 }
 
+ice_status_t ice_debug_cache_cut(const ice_cache_t *c, int32_t G, int32_t n_requests, const int32_t *query_start, int32_t n_tokens, int32_t max_query,
+                                 const int32_t *len, int32_t max_keys, int32_t max_blocks, int32_t window, int32_t *parts, int64_t max_parts,
+                                 int64_t *n_parts) {
+    if (ice_status_t st = check_cache(c)) return st;
+    if (!len || !parts || !n_parts) return fail(ICE_ERR_INVALID_ARG, "a pointer is null");
+    if (max_blocks < 1 || (long long)max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, at most 2^30 tokens", max_blocks);
+    if (window < 0 || n_tokens < 0 || max_parts < 0) return fail(ICE_ERR_SHAPE, "window, n_tokens and max_parts must be >= 0");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, !query_start, a, &need)) return st;
+    a.T = query_start ? n_tokens : n_requests;
+    a.max_blocks = max_blocks;
+    a.window = window;
+    *n_parts = cut_cache_attend(a, !query_start, query_start, len, parts, max_parts);
+    return ICE_OK;
+}
+
 static ice_status_t select_hier_common(ice_index_t *ix, const void *q, int32_t budget, int32_t n_top, int32_t n_probe_top,
                                        int32_t n_probe, int32_t n_refine, int32_t *ids, int32_t *n_sel, float *scores,
                                        int32_t *clusters, int32_t *tops, float *out, void *stream, const char *who) {

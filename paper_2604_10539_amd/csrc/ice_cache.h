@@ -65,5 +65,9 @@ struct CacheAttend {
 // How a call is cut, from the sizes: fills few_groups, many_groups, many, per_unit and whole; returns the bytes of workspace.
 size_t plan_cache_attend(CacheAttend &a, bool listed);
 void launch_cache_attend(CacheAttend a, hipStream_t stream);
+// The parts that the workgroups of a planned call take, from lengths on the host (query_start and seq_len, or n_tok): their number, the first `most` of
+// them in parts, kCutInts words each (see ice_debug_cache_cut).
+constexpr int kCutInts = 15;
+long long cut_cache_attend(CacheAttend a, bool listed, const int *query_start, const int *len, int *parts, long long most);
 
 }  // namespace ice

@@ -1,6 +1,8 @@
 // Attention over the 4-bit sequence cache.
 #include <algorithm>
+#include <array>
 #include <type_traits>
+#include <vector>
 
 #include "ice_cache.h"
 
@@ -44,6 +46,8 @@ template <bool LIST>
 struct Unit {
     int row0, n_query, len;  // first query row, queries, cached tokens (listed: entries of the list)
     int tokens;              // cached tokens
+    // t: the request's length; x, y: its entry of query_start and the next one, or x the length of its list.
+    __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y) { set(a, s, t, x, y); }
     // UNIFORM: the same on all lanes.  A request's words are asked for before one is looked at: left to the compiler, the length was asked for
     // once the request was known to have queries, a trip more (0.1 to 1 us a call).
     template <bool UNIFORM>
@@ -58,6 +62,9 @@ struct Unit {
         } else {
             asm volatile("" : "+v"(t), "+v"(x), "+v"(y));
         }
+        set(a, s, t, x, y);
+    }
+    __host__ __device__ void set(const CacheAttend &a, int s, int t, int x, int y) {
         tokens = (int)min((long long)max(t, 0), (long long)a.max_blocks << (a.c.tile_shift + 4));
         if constexpr (LIST) {
             row0 = s;
@@ -69,11 +76,35 @@ struct Unit {
             len = tokens;
         }
     }
-    __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
+    __host__ __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
     // keys [low, high) that query t sees
-    __device__ int high(int t) const { return LIST ? len : max(len - n_query + t + 1, 0); }
-    __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(high(t) - a.window, 0) : 0; }
+    __host__ __device__ int high(int t) const { return LIST ? len : max(len - n_query + t + 1, 0); }
+    __host__ __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(high(t) - a.window, 0) : 0; }
 };
+
+// Quanta of `quantum` keys that the queries t0 .. t1 see, at least one: rows that see nothing want their outputs too.
+template <typename U> __host__ __device__ inline int quanta_of(const CacheAttend &a, const U &u, int t0, int t1, int quantum) {
+    return max((u.high(t1) + quantum - 1) / quantum - u.low(a, t0) / quantum, 1);
+}
+// The same of a request in the kernel for few queries, if it takes that many rows.
+template <typename U> __host__ __device__ inline int few_quanta(const CacheAttend &a, const U &u, int most_rows, int quantum) {
+    const int q = u.queries(a);
+    return q > 0 && q * a.G <= most_rows ? quanta_of(a, u, 0, q - 1, quantum) : 0;
+}
+
+// Keys [from, to) of the part [now, stop) of the flat work's unit [u0, u1), the queries t0 .. t1.
+struct PartKeys {
+    int from, to;
+    template <typename U>
+    __host__ __device__ PartKeys(const CacheAttend &a, const U &u, int t0, int t1, int quantum, unsigned u0, unsigned u1, unsigned now, unsigned stop) {
+        const int low = u.low(a, t0), high = u.high(t1), q0 = low / quantum;
+        from = max(low, (q0 + (int)(now - u0)) * quantum);
+        // (the last part takes its keys to the end, whatever the unit's nominal length)
+        to = stop == u1 ? high : min(high, (q0 + (int)(stop - u0)) * quantum);
+    }
+};
+// The partial result that a part of a unit that was cut leaves: two a workgroup, of a unit that began before it and of one that goes on behind it.
+__host__ __device__ inline unsigned record_of(unsigned workgroup, bool began_before) { return 2 * workgroup + (began_before ? 0 : 1); }
 
 // Writes four dims of a row from its sums relative to 2^top, and the logarithm of its denominator.
 __device__ inline void put_row(const CacheAttend &a, size_t row, int d0, f32x4 sum, float top, float total) {
@@ -103,8 +134,8 @@ constexpr unsigned kCus = 256;
 struct Pieces {
     unsigned groups, per, from1, from2, total;  // workgroups, those of a third (half, whole), where the pieces of the second and third begin
     // whole: pieces are units, which must not be cut (there is no room for records)
-    __device__ Pieces(unsigned total_, unsigned most, bool whole) : total(__builtin_amdgcn_readfirstlane(total_)) {
-        groups = min(most, max(total, 1u));
+    __host__ __device__ Pieces(unsigned total_, unsigned most, bool whole) : total(total_) {
+        groups = total < 1 ? 1 : total < most ? total : most;
         const bool uneven = !whole && (groups == 2 * kCus || groups == 3 * kCus) && total >= 12 * groups;
         per = uneven ? kCus : groups;
         from1 = from2 = total;
@@ -114,13 +145,13 @@ struct Pieces {
             from2 = total / 48 * 35;
         }
     }
-    __device__ unsigned begin(unsigned i) const {
+    __host__ __device__ unsigned begin(unsigned i) const {
         const unsigned t = i < per ? 0 : i < 2 * per || from2 == total ? 1 : 2, k = i - t * per;
         if (i == per && per == groups) return total;
         const unsigned from = t == 0 ? 0 : t == 1 ? from1 : from2, n = (t == 0 ? from1 : t == 1 ? from2 : total) - from;
-        return from + k * (n / per) + min(k, n % per);
+        return from + k * (n / per) + (k < n % per ? k : n % per);
     }
-    __device__ unsigned owner(unsigned x) const {
+    __host__ __device__ unsigned owner(unsigned x) const {
         const unsigned t = x < from1 ? 0 : x < from2 ? 1 : 2, from = t == 0 ? 0 : t == 1 ? from1 : from2;
         const unsigned n = (t == 0 ? from1 : t == 1 ? from2 : total) - from, base = n / per, longer = n % per * (base + 1);
         x -= from;
@@ -244,10 +275,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             unsigned n = 0;
             if (e < a.n_here) {
                 const Unit<LIST> u(a, a.first + e, 0, std::false_type());
-                const int q = u.queries(a);
-                // at least one where there are rows, which want their outputs; none where the other kernel does the request
-                if (q > 0 && q * a.G <= NT * R)
-                    n = (unsigned)max((u.high(q - 1) + Q - 1) / Q - u.low(a, 0) / Q, 1) * (unsigned)a.c.H;
+                n = (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
             }
             const unsigned incl = (unsigned)wave_scan_add((int)n);
             if (lane == 63) s_wave[wave] = incl;
@@ -264,7 +292,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         if (tid == 0) s_before[a.n_here] = total;
         __syncthreads();
     }
-    const Pieces pieces(total, gridDim.x, a.whole);
+    const Pieces pieces(__builtin_amdgcn_readfirstlane(total), gridDim.x, a.whole);
     if (blockIdx.x >= pieces.groups || total == 0) {
         if (tid == 0 && a.notes) a.notes[blockIdx.x].first = -1;
         return;
@@ -309,9 +337,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         }
         // keys of this part that any row sees, that every row sees, that this lane's rows see
         const int q0 = unit.low(a, 0) / Q;
-        const int from = max(unit.low(a, 0), (q0 + (int)(now - u0)) * Q);
-        // (the last part takes its keys to the end, whatever the nominal length)
-        const int to = stop == u1 ? unit.high(t_last) : min(unit.high(t_last), (q0 + (int)(stop - u0)) * Q);
+        const PartKeys keys(a, unit, 0, t_last, Q, u0, u1, now, stop);
+        const int from = keys.from, to = keys.to;
         const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(0), to);
         int low[NT], high[NT];
         u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
@@ -586,7 +613,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 
         // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
         const bool whole = now == u0 && stop == u1;
-        float *record = a.part + ((size_t)blockIdx.x * 2 + (now > u0 ? 0 : 1)) * a.rows * kRecord;
+        float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
         const int d0 = 4 * (tid & 31);
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
@@ -679,23 +706,37 @@ constexpr int kVector = 0x002, kMatrix = 0x008, kLdsRead = 0x100;
 constexpr int kAhead = 2, kWeightOps = 28, kBeside = 2;
 
 struct Chunks {  // how a request's row tiles lie in the flat work of one KV head
-    int tiles;
+    int n_rows, tiles;
     unsigned pair, single, per_head;  // quanta of a pair, of the middle tile of an odd number, of all
-    template <typename U> __device__ static int quanta(const CacheAttend &a, const U &u, int n_rows, int tile) {
-        const int t0 = kChunkRows * tile / a.G, t1 = (min(kChunkRows * (tile + 1), n_rows) - 1) / a.G;
-        return max((u.high(t1) + kQuantum - 1) / kQuantum - u.low(a, t0) / kQuantum, 1);
+    template <typename U> __host__ __device__ static int quanta(const CacheAttend &a, const U &u, int n_rows, int tile) {
+        return quanta_of(a, u, kChunkRows * tile / a.G, (min(kChunkRows * (tile + 1), n_rows) - 1) / a.G, kQuantum);
     }
-    template <typename U> __device__ Chunks(const CacheAttend &a, const U &u) {
-        const int n_rows = u.queries(a) * a.G;
+    template <typename U> __host__ __device__ Chunks(const CacheAttend &a, const U &u) {
+        n_rows = u.queries(a) * a.G;
         tiles = 0;
         pair = single = per_head = 0;
         if (n_rows <= kRows) return;  // (the few-query kernel's, which takes that many where there are requests with more than kFewRows)
         tiles = (n_rows + kChunkRows - 1) / kChunkRows;
         const int middle = quanta(a, u, n_rows, (tiles - 1) / 2);
-        // an estimate for the pairs (a line, or with a window concave: the middle is the most); a pair's second tile takes what is left of it
+        // An estimate for the pairs: with as many keys as queries the tiles' quanta are a line, or with a window concave, and twice the middle covers any
+        // pair.  It is no bound: tiles of queries in front of the first key see nothing, and then a pair's first tile alone may need more.
+        // So a pair's second tile gets what the first one leaves of it, and that is one quantum at least (see at()); what a unit needs beyond its nominal length its last
+        // part takes along (PartKeys).
         if (tiles > 1) pair = (unsigned)max(2 * middle + 2, quanta(a, u, n_rows, tiles - 1) + 1);
         if (tiles & 1) single = (unsigned)middle;
         per_head = (unsigned)(tiles / 2) * pair + single;
+    }
+    // The row tile that the flat work's quantum `now` belongs to, and its place there; head0: where the KV head begins.
+    struct Tile {
+        int tile;
+        unsigned u0, u1;
+    };
+    template <typename U> __host__ __device__ Tile at(const CacheAttend &a, const U &u, unsigned head0, unsigned now) const {
+        const unsigned paired = head0 + (unsigned)(tiles / 2) * pair;
+        if (now >= paired) return {tiles / 2, paired, paired + single};
+        const int p = (int)((now - head0) / pair);
+        const unsigned p0 = head0 + (unsigned)p * pair, split = p0 + (unsigned)min(quanta(a, u, n_rows, tiles - 1 - p), (int)pair - 1);
+        return now >= split ? Tile{p, split, p0 + pair} : Tile{tiles - 1 - p, p0, split};
     }
 };
 
@@ -723,7 +764,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     }
     if (tid == 0) s_before[a.n_here] = total;
     __syncthreads();
-    const Pieces pieces(total, gridDim.x, false);
+    const Pieces pieces(__builtin_amdgcn_readfirstlane(total), gridDim.x, false);
     if (blockIdx.x >= pieces.groups || total == 0) {
         if (tid == 0) a.notes[blockIdx.x].first = -1;
         return;
@@ -745,30 +786,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const Chunks ch(a, unit);
         const unsigned first = s_before[entry];
         const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
-        const unsigned head0 = first + (unsigned)h * ch.per_head, off = now - head0;
-        const int all_rows = unit.queries(a) * a.G;
-        int tile;
-        unsigned u0, u1;
-        if (off < (unsigned)(ch.tiles / 2) * ch.pair) {
-            const int p = (int)(off / ch.pair);
-            const unsigned p0 = head0 + (unsigned)p * ch.pair, split = p0 + (unsigned)Chunks::quanta(a, unit, all_rows, ch.tiles - 1 - p);
-            const bool second = now >= split;
-            tile = second ? p : ch.tiles - 1 - p;
-            u0 = second ? split : p0;
-            u1 = second ? p0 + ch.pair : split;
-        } else {
-            tile = ch.tiles / 2;
-            u0 = head0 + (unsigned)(ch.tiles / 2) * ch.pair;
-            u1 = u0 + ch.single;
-        }
-        tile = __builtin_amdgcn_readfirstlane(tile);
-        const unsigned stop = min(u1, end);
+        const Chunks::Tile place = ch.at(a, unit, first + (unsigned)h * ch.per_head, now);
+        const int all_rows = ch.n_rows, tile = __builtin_amdgcn_readfirstlane(place.tile);
+        const unsigned u0 = place.u0, u1 = place.u1, stop = min(u1, end);
         const int base = kChunkRows * tile, n_rows = min(all_rows - base, kChunkRows);
         const int t_first = base / a.G, t_last = (base + n_rows - 1) / a.G;
         const int q0 = unit.low(a, t_first) / kQuantum + (int)(now - u0);
-        const int from = max(unit.low(a, t_first), q0 * kQuantum);
-        // (the unit's last part takes its keys to the end, whatever was estimated for it)
-        const int to = stop == u1 ? unit.high(t_last) : min(unit.high(t_last), (q0 + (int)(stop - now)) * kQuantum);
+        const PartKeys keys(a, unit, t_first, t_last, kQuantum, u0, u1, now, stop);
+        const int from = keys.from, to = keys.to;
         const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(t_first), to);
         const int key_at = q0 * kQuantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
@@ -995,7 +1020,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         else run(std::integral_constant<int, 1>());
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1;
-        float *record = a.part + ((size_t)blockIdx.x * 2 + (now > u0 ? 0 : 1)) * a.rows * kRecord;
+        float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
             const int in = kRows * (kWaves * x + wave) + c, row = base + in;
@@ -1051,7 +1076,7 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend 
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 const int kk = min(k + GROUPS * j, n - 1);
-                const float *x = a.part + (((size_t)(note.first + kk) * 2 + (kk == 0 ? 1 : 0)) * a.rows + in) * kRecord;
+                const float *x = a.part + ((size_t)record_of(note.first + kk, kk > 0) * a.rows + in) * kRecord;
                 v[j] = *(const f32x4 *)(x + d0);
                 m[j] = x[kD];
                 l[j] = x[kD + 1];
@@ -1119,6 +1144,70 @@ size_t plan_cache_attend(CacheAttend &a, bool listed) {
     const long long tiles = ((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows;
     if (a.many) a.many_groups = (int)std::min<long long>(512, quanta * tiles);
     return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, kChunkRows));
+}
+
+// The launches of a call, workgroup by workgroup as the kernels take their pieces, from the lengths on the host.
+template <bool LIST, typename F> static void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
+    const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = few_rows(a);
+    const bool even = LIST || a.per_unit > 0;
+    const auto unit = [&](int s, int h) {
+        return LIST ? Unit<LIST>(a, s, 1 << 30, len[s * a.c.H + h], 0) : Unit<LIST>(a, s, len[s], start[s], start[s + 1]);
+    };
+    std::vector<unsigned> before(1, 0);  // quanta before each request
+    for (int e = 0; e < a.n_here; ++e)
+        before.push_back(before.back() + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, unit(a.first + e, 0), rows, quantum)));
+    const unsigned launched = a.whole ? a.n_here * a.c.H : a.few_groups;
+    const Pieces pieces(before.back(), launched, a.whole);
+    if (before.back() == 0) return;
+    for (unsigned i = 0; i < pieces.groups && i < launched; ++i)
+        for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
+            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
+            const unsigned per = (before[entry + 1] - before[entry]) / a.c.H, h = (now - before[entry]) / per;
+            const unsigned u0 = before[entry] + h * per, u1 = u0 + per;
+            stop = std::min(u1, end);
+            const auto u = unit(a.first + entry, (int)h);
+            const int n_rows = u.queries(a) * a.G;
+            if (n_rows <= 0 || n_rows > rows) continue;
+            const PartKeys keys(a, u, 0, (n_rows - 1) / a.G, quantum, u0, u1, now, stop);
+            const bool cut = now > u0 || stop < u1;
+            put({a.first, 0, (int)i, a.first + entry, (int)h, 0, n_rows, keys.from, keys.to, (int)u0, (int)u1, (int)now, (int)stop,
+                 cut ? (int)record_of(i, now > u0) : -1, now > u0 && stop == u1 ? (int)pieces.owner(u0) : -1});
+        }
+}
+template <typename F> static void cut_many(const CacheAttend &a, const int *start, const int *len, F put) {
+    const auto unit = [&](int s) { return Unit<false>(a, s, len[s], start[s], start[s + 1]); };
+    std::vector<unsigned> before(1, 0);
+    for (int e = 0; e < a.n_here; ++e) before.push_back(before.back() + (unsigned)a.c.H * Chunks(a, unit(a.first + e)).per_head);
+    const Pieces pieces(before.back(), a.many_groups, false);
+    if (before.back() == 0) return;
+    for (unsigned i = 0; i < pieces.groups && i < (unsigned)a.many_groups; ++i)
+        for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
+            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
+            const auto u = unit(a.first + entry);
+            const Chunks ch(a, u);
+            const unsigned h = (now - before[entry]) / ch.per_head;
+            const Chunks::Tile p = ch.at(a, u, before[entry] + h * ch.per_head, now);
+            stop = std::min(p.u1, end);
+            const int base = kChunkRows * p.tile, n_rows = std::min(ch.n_rows - base, kChunkRows);
+            const PartKeys keys(a, u, base / a.G, (base + n_rows - 1) / a.G, kQuantum, p.u0, p.u1, now, stop);
+            const bool cut = now > p.u0 || stop < p.u1;
+            put({a.first, 1, (int)i, a.first + entry, (int)h, base, n_rows, keys.from, keys.to, (int)p.u0, (int)p.u1, (int)now, (int)stop,
+                 cut ? (int)record_of(i, now > p.u0) : -1, now > p.u0 && stop == p.u1 ? (int)pieces.owner(p.u0) : -1});
+        }
+}
+long long cut_cache_attend(CacheAttend a, bool listed, const int *start, const int *len, int *parts, long long most) {
+    long long n = 0;
+    const auto put = [&](const std::array<int, kCutInts> &part) {
+        if (n < most) std::copy(part.begin(), part.end(), parts + n * kCutInts);
+        ++n;
+    };
+    for (a.first = 0; a.first < a.S; a.first += kEntries) {
+        a.n_here = std::min(a.S - a.first, kEntries);
+        if (listed) cut_few<true>(a, start, len, put);
+        else cut_few<false>(a, start, len, put);
+        if (a.many) cut_many(a, start, len, put);
+    }
+    return n;
 }
 
 template <int W, bool LIST>
