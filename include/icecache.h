@@ -351,7 +351,8 @@ ice_status_t ice_cache_read(const ice_cache_t *cache, int32_t n_requests, const 
 
 /* Causal attention of a step's queries over their requests' cached tokens (Eq. 1, softmax(q . k / sqrt(d)) . v, fp32 accumulation):
  * query j of request s, row query_start[s] + j of q, stands at position seq_len[s] - (number of s's queries) + j and sees the
- * positions up to its own, with window > 0 only the last `window` of these.  The step's tokens are written before.
+ * positions up to its own, with window > 0 only the last `window` of these.  The step's tokens are written before.  (Where seq_len is
+ * larger than a row of the table holds, the queries stand there all the same and the tokens behind the row do not exist.)
  *   q: bf16, row t at q + t * q_stride elements (a multiple of 8), [n_kv_heads * group_size][128] within it; group_size 1 to 16, query
  *     head h reads KV head h / group_size.
  *   block_table: rows of at most 2^30 tokens.

@@ -44,8 +44,8 @@ __device__ inline float cut(float v, uint32_t mask) { return v - __uint_as_float
 // A request's query rows and the keys they see; for listed tokens, those of one KV head.
 template <bool LIST>
 struct Unit {
-    int row0, n_query, len;  // first query row, queries, cached tokens (listed: entries of the list)
-    int tokens;              // cached tokens
+    int row0, n_query, first;  // first query row, queries, the position behind the first one's own (listed: entries of the list)
+    int tokens;              // the length, or what the table has room for if that is less: the queries' positions follow the length all the same
     // t: the request's length; x, y: its entry of query_start and the next one, or x the length of its list.
     __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y) { set(a, s, t, x, y); }
     // UNIFORM: the same on all lanes.  A request's words are asked for before one is looked at: left to the compiler, the length was asked for
@@ -69,17 +69,19 @@ struct Unit {
         if constexpr (LIST) {
             row0 = s;
             n_query = 1;
-            len = min(max(x, 0), a.max_keys);
+            first = min(max(x, 0), a.max_keys);
         } else {
             row0 = min(max(x, 0), a.T);
             n_query = min(max(y, row0), a.T) - row0;
-            len = tokens;
+            first = (int)((unsigned)max(t, 0) - (unsigned)n_query + 1u);  // (of a request without queries it may wrap)
         }
     }
     __host__ __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
-    // keys [low, high) that query t sees
-    __host__ __device__ int high(int t) const { return LIST ? len : max(len - n_query + t + 1, 0); }
-    __host__ __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(high(t) - a.window, 0) : 0; }
+    // Keys [low, high) that query t sees; sees_from and sees_to: the same for who keeps to keys that some query sees.
+    __host__ __device__ int sees_to(int t) const { return LIST ? first : first + t; }
+    __host__ __device__ int sees_from(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(first + t, 0) - a.window : 0; }
+    __host__ __device__ int high(int t) const { return LIST ? first : min(max(sees_to(t), 0), tokens); }
+    __host__ __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? min(max(sees_from(a, t), 0), tokens) : 0; }
 };
 
 // Quanta of `quantum` keys that the queries t0 .. t1 see, at least one: rows that see nothing want their outputs too.
@@ -339,14 +341,14 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         const int q0 = unit.low(a, 0) / Q;
         const PartKeys keys(a, unit, 0, t_last, Q, u0, u1, now, stop);
         const int from = keys.from, to = keys.to;
-        const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(0), to);
+        const int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
         int low[NT], high[NT];
         u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             const int row = min(R * x + col_row, n_rows - 1), t = row / a.G;
-            low[x] = max(unit.low(a, t), from);
-            high[x] = min(unit.high(t), to);
+            low[x] = max(unit.sees_from(a, t), from);
+            high[x] = min(unit.sees_to(t), to);
             const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
@@ -794,7 +796,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const int q0 = unit.low(a, t_first) / kQuantum + (int)(now - u0);
         const PartKeys keys(a, unit, t_first, t_last, kQuantum, u0, u1, now, stop);
         const int from = keys.from, to = keys.to;
-        const int all_low = max(unit.low(a, t_last), from), all_high = min(unit.high(t_first), to);
+        const int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(t_first), to);
         const int key_at = q0 * kQuantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
         // this lane's rows: columns of tiles wave + 4 x
@@ -803,16 +805,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
             const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1), t = row / a.G;
-            low[x] = max(unit.low(a, t), from);
-            high[x] = min(unit.high(t), to);
+            low[x] = max(unit.sees_from(a, t), from);
+            high[x] = min(unit.sees_to(t), to);
             const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
         {  // keys that all rows of this wave see
             const int r0 = min(kRows * wave, n_rows - 1), r1 = min(kRows * (kWaves * (kTiles - 1) + wave) + kRows - 1, n_rows - 1);
-            wave_low = max(unit.low(a, (base + r1) / a.G), from);
-            wave_high = min(unit.high((base + r0) / a.G), to);
+            wave_low = max(unit.sees_from(a, (base + r1) / a.G), from);
+            wave_high = min(unit.sees_to((base + r0) / a.G), to);
         }
         const int *table = a.table + (size_t)s * a.max_blocks;
         auto places = [&](int n0) __attribute__((always_inline)) -> int {  // this wave's tile of round n0 + l

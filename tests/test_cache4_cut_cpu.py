@@ -131,6 +131,15 @@ def test_more_requests_than_one_launch_takes(queries):
     check(2, 4, lens, [1] * 2400 + [queries] * 100)
 
 
+@pytest.mark.parametrize("group,queries", [(2, 2), (2, 40), (4, 700)])
+def test_lengths_beyond_the_table_keep_the_queries_positions(group, queries):
+    """seq_len says where the queries stand, the table's row how many tokens there are: queries behind the row see all of it, or with a window
+    what it leaves them."""
+    for length in (150, 159, 160, 161, 161 + queries, 400, 2 ** 31 - 1):
+        for window in (0, 1, 50, 300, 2 ** 31 - 1):
+            check(2, group, [length, 90], [queries, 1], window, max_keys=300, width=10)
+
+
 @pytest.mark.parametrize("requests,heads,most", [(1, 1, 1), (1, 8, 256), (1, 8, 2500), (3, 2, 5000), (16, 8, 1024), (40, 1, 700), (256, 2, 3500), (384, 2, 4100), (1100, 1, 2100)])
 def test_lists(requests, heads, most):
     import paper_2604_10539_amd as p
