@@ -7,6 +7,7 @@ stream.  There is no fallback: if libicecache.so is missing, loading fails loudl
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import os
 
 import torch
@@ -70,7 +71,7 @@ _native = None  # the extension module, once it is bound to the library
 
 def lib() -> C.CDLL:
     """Loads the HIP library built by paper_2604_10539_amd/build.py; raises if it is not there."""
-    global _lib, _native
+    global _lib
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("%s is missing: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -130,16 +131,26 @@ def lib() -> C.CDLL:
             if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
                             "ice_cache_attend_tokens_bytes"):
                 getattr(L, name).restype = C.c_int
+        _lib = L
+    return _lib
+
+
+def _extension():
+    """The extension module, bound to the library.  It belongs to one Python and one torch; only the 4-bit cache's classes and
+    ice_plan_blocks need it."""
+    global _native
+    if _native is None:
+        L = lib()
         try:
-            from . import _calls
+            _calls = importlib.import_module(__package__ + "._calls")
         except ImportError as e:
-            raise RuntimeError("the extension module _calls is missing: run `python -c 'import __graft_entry__ as g; g.build()'`") from e
+            raise RuntimeError("the 4-bit cache's extension module _calls cannot be imported (%s): run "
+                               "`python -c 'import __graft_entry__ as g; g.build()'`" % e) from e
         _calls.bind(IceError, *(C.cast(getattr(L, name), C.c_void_p).value for name in (
             "ice_last_error", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
             "ice_cache_attend_tokens_bytes", "ice_cache_attend_tokens")))
         _native = _calls
-        _lib = L
-    return _lib
+    return _native
 
 
 def ice_last_error() -> str:
@@ -349,8 +360,7 @@ def ice_cache_bytes(cache: IceCacheDesc) -> int:
 def ice_plan_blocks(new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots, info, block_size,
                     stream=None) -> None:
     """int32 device tensors as in the header; block_table [n_requests, max_blocks], free_ids [n_blocks]."""
-    lib()
-    _native.plan(_stream(stream) or 0, block_size, new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots,
+    _extension().plan(_stream(stream) or 0, block_size, new_len, cached_len, seq_len, block_table, free_ids, n_free, n_free_left, query_start, slots,
                  info)
 
 
@@ -660,6 +670,7 @@ class IceBlocks:
     plan() moves it on by a step without waiting for the GPU."""
 
     def __init__(self, n_blocks, block_size, max_requests, max_len, device="cuda"):
+        _extension()
         self.block_size, self.n_blocks, self.max_requests = block_size, n_blocks, max_requests
         self.device = torch.device(device)
         if block_size not in (16, 32, 64) or n_blocks < 1 or max_requests < 1 or max_len < 1:
@@ -694,6 +705,7 @@ class IceCache:
     or a raw address; without one it is the current stream of the cache's device."""
 
     def __init__(self, n_blocks, n_kv_heads, block_size=64, device="cuda", data=None):
+        _extension()
         self.n_blocks, self.n_kv_heads, self.block_size = n_blocks, n_kv_heads, block_size
         if ice_cache_bytes(make_cache_desc(None, n_blocks, n_kv_heads, block_size)) == 0:
             raise IceError(ICE_ERR_SHAPE, ice_last_error())

@@ -144,3 +144,33 @@ def test_attention_refuses_rows_whose_positions_do_not_fit():
     assert status(p.ice_cache_attend, c, *{**args, "mb": 2 ** 24}.values()) == b.ICE_ERR_CAPACITY
     listed = dict(q=FAKE, qs=1024, G=4, n=2, sl=FAKE, table=FAKE, mb=2 ** 24 + 1, pos=FAKE, n_tok=FAKE, max_tok=4096, out=FAKE, ot=0, lse=None, ws=FAKE, wb=0)
     assert status(p.ice_cache_attend_tokens, c, *listed.values()) == b.ICE_ERR_SHAPE and "2^30" in p.ice_last_error()
+
+
+@pytest.mark.parametrize("how", ["none", "broken"])
+def test_only_the_caches_classes_need_the_extension_module(how, tmp_path):
+    """Without the extension module the library loads and the index's calls work; who needs the module is told why it cannot be had."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import importlib.abc, sys
+class Finder(importlib.abc.MetaPathFinder):
+    def find_spec(self, name, path, target=None):
+        if name == "paper_2604_10539_amd._calls":
+            raise ImportError(%r)
+sys.meta_path.insert(0, Finder())
+import paper_2604_10539_amd as p
+assert p.ice_workspace_bytes(p.make_config(1, 8, 4, 4096), 16, 64) > 0
+assert p.ice_cache_bytes(p.make_cache_desc(None, 1, 1, 16)) == 2176
+for make in (lambda: p.IceCache(4, 2, 16, device="cpu"), lambda: p.IceBlocks(16, 16, 2, 100, device="cpu"), lambda: p.ice_plan_blocks(*[None] * 10, 16)):
+    try:
+        make()
+    except RuntimeError as e:
+        assert not isinstance(e, p.IceError) and "_calls" in str(e) and %r in str(e), e
+    else:
+        raise AssertionError("no error")
+print("fine")
+""" % (("No module named _calls", "No module named") if how == "none" else ("undefined symbol: abc", "undefined symbol: abc"))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "fine", r.stderr
