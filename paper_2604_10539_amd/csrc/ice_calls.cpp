@@ -93,7 +93,7 @@ struct Cache {
         if (!(t.dim() == 3 && t.size(2) == 128 && t.stride(2) == 1 && (t.stride(1) == 128 || t.size(1) == 1) && here(t) &&
               (t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kShort)))
             refuse_shape("%s: bf16 [tokens, heads, 128] on the cache's device, heads and values side by side", name);
-        *stride = t.stride(0);
+        *stride = t.size(0) > 1 ? t.stride(0) : t.size(1) * 128;  // (of a single row it may be anything)
         return t.const_data_ptr();
     }
     struct Table {

@@ -33,3 +33,22 @@ def test_queries_that_stand_behind_the_tables_row(queries, window):
     longer = np.full((4, -(-max(lens) // block)), -1, dtype=np.int32)
     longer[:, :width] = table
     check(out, lse, expected(ref.widen(q).astype(np.float64), data, longer, lens, qlens, block, group, window, False, n_blocks))
+
+
+def test_a_single_token_has_no_row_stride():
+    """Tensors of one token whose first stride means nothing: 1, or an odd projection's width."""
+    rng = np.random.default_rng(2)
+    heads, group, block = 2, 4, 16
+    c, other = make(3, heads, block, np.zeros((3, heads, 1, 2176), np.uint8)), make(3, heads, block, np.zeros((3, heads, 1, 2176), np.uint8))
+    k, v, q = (up(ref.to_bf16(rng.standard_normal((1, heads * m, D)).astype(np.float32))) for m in (1, 1, group))
+    wide = torch.zeros((1, 3 * heads * D + 3), dtype=torch.int16, device="cuda")
+    wide[:, heads * D: 2 * heads * D] = v.flatten(1)
+    odd_k, odd_v, odd_q = k[0].unsqueeze(-1).permute(2, 0, 1), wide.as_strided((1, heads, D), (wide.shape[1], D, 1), heads * D), q[0].unsqueeze(-1).permute(2, 0, 1)
+    assert odd_k.stride(0) == 1 and odd_v.stride(0) % 8 and odd_q.stride(0) == 1
+    table, lens, start, slots = i32([[2]]), i32([1]), i32([0, 1]), i32([2 * block])
+    c.write(k, v, slots)
+    other.write(odd_k, odd_v, slots)
+    assert torch.equal(c.data, other.data) and bool(c.data.any())
+    assert torch.equal(c.attend(q, start, lens, table), c.attend(odd_q, start, lens, table))
+    pos, n_tok = i32(np.zeros((1, heads, 1))), i32(np.ones((1, heads)))
+    assert torch.equal(c.attend_tokens(q, lens, table, pos, n_tok), c.attend_tokens(odd_q, lens, table, pos, n_tok))
