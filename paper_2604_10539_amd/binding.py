@@ -733,8 +733,9 @@ class IceCache:
     def attend(self, q, query_start, seq_len, block_table, max_query=None, max_len=None, window=0, out=None, out_dtype=torch.float32,
                lse=None, with_lse=False, stream=None):
         """Causal attention of a step's queries q [tokens, heads, 128] over their requests' cached tokens.  max_query, max_len: what the host
-        knows of the most queries of a request (none has more) and the longest length (a hint).  -> out, or (out, lse) when lse is
-        given or with_lse is true.  Rows of q behind query_start[-1] are left out and their outputs left as they were."""
+        knows of the most queries of a request (none has more) and the longest length (a hint).  Give max_query wherever it is known, 1 for a decode
+        step: without it any request may have all of q's rows, and the call is cut, launched and, for bfloat16 outputs, rounded for such
+        a one (see the header's Precision).  -> out, or (out, lse) when lse is given or with_lse is true.  Rows of q behind query_start[-1] are left out and their outputs left as they were."""
         if stream is not None or _current_device() != self._index:
             return _elsewhere(IceCache.attend, self, stream, q, query_start, seq_len, block_table, max_query, max_len, window, out, out_dtype, lse,
                               with_lse)
