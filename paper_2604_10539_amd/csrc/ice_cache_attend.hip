@@ -1113,6 +1113,9 @@ static int few_rows(const CacheAttend &a) {
     const long long rows = (long long)a.max_query * a.G;
     return rows <= 5 ? 5 : rows <= 8 ? 8 : rows <= 16 || rows > kFewRows ? 16 : rows <= 32 ? 32 : 48;
 }
+// ... and those of a unit of the many-query kernel: a record has room for what a request can have (single tokens of 16 requests whose most queries are not
+// known, 64 rows: 35 MB for 512 workgroups instead of 104).
+static int chunk_rows(const CacheAttend &a) { return (int)std::min<long long>(kChunkRows, (long long)a.max_query * a.G); }
 static size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(MergeNote)); }
 
 // Units (request, KV head) that stay whole, one workgroup each, no merge behind it: short ones, where the merge costs more than the cut gains, longer
@@ -1145,7 +1148,7 @@ size_t plan_cache_attend(CacheAttend &a, bool listed) {
     a.few_groups = (int)std::min<long long>(rows > 16 ? 512 : 768, quanta);
     const long long tiles = ((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows;
     if (a.many) a.many_groups = (int)std::min<long long>(512, quanta * tiles);
-    return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, kChunkRows));
+    return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, chunk_rows(a)));
 }
 
 // The launches of a call, workgroup by workgroup as the kernels take their pieces, from the lengths on the host.
@@ -1244,12 +1247,12 @@ void launch_cache_attend(CacheAttend a, hipStream_t stream) {
         if (a.pos) launch_few<kListWaves, true>(a, stream);
         else launch_few<kWaves, false>(a, stream);
         if (!a.many) continue;
-        a.rows = kChunkRows;
+        a.rows = chunk_rows(a);
         a.notes = (MergeNote *)part;
         a.part = (float *)(a.notes + a.many_groups);
         if (a.out_bf16) cache_chunk_kernel<1><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
         else cache_chunk_kernel<3><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
-        cache_merge_kernel<1><<<dim3(a.many_groups, kChunkRows / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
+        cache_merge_kernel<1><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
     }
 }
 

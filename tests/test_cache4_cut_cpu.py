@@ -84,7 +84,7 @@ def check(heads, group, lens, qlens, window=0, max_query=None, max_keys=None, bl
             seen = [length - n + t + 1 for t in (base // group, (base + here - 1) // group)]  # keys up to the query's own position
             low = max(seen[0] - window, 0) if window else 0
             expected[int(many), s, base] = (here, min(low, capacity), min(max(seen[1], 0), capacity))
-    check_units(x, nbytes, heads, expected, (few, CHUNK))
+    check_units(x, nbytes, heads, expected, (few, min(CHUNK, rows_most)))
 
 
 def test_row_tiles_that_see_nothing_in_front_of_a_window():
@@ -138,6 +138,14 @@ def test_lengths_beyond_the_table_keep_the_queries_positions(group, queries):
     for length in (150, 159, 160, 161, 161 + queries, 400, 2 ** 31 - 1):
         for window in (0, 1, 50, 300, 2 ** 31 - 1):
             check(2, group, [length, 90], [queries, 1], window, max_keys=300, width=10)
+
+
+def test_records_have_room_for_the_rows_that_there_can_be_and_no_more():
+    """A call of many queries keeps 512 workgroups' records; a unit of it has 192 rows, or all that a request may have."""
+    import paper_2604_10539_amd as p
+    c = p.make_cache_desc(None, 1, 8, 16)
+    for rows in (49, 64, 191, 192, 193, 5000):
+        assert p.ice_cache_attend_bytes(c, 1, 16, rows, 32768) == 512 * (2 * min(rows, CHUNK) * RECORD + 32)
 
 
 @pytest.mark.parametrize("requests,heads,most", [(1, 1, 1), (1, 8, 256), (1, 8, 2500), (3, 2, 5000), (16, 8, 1024), (40, 1, 700), (256, 2, 3500), (384, 2, 4100), (1100, 1, 2100)])
