@@ -505,15 +505,20 @@ size_t ice_cache_attend_tokens_bytes(const ice_cache_t *c, int32_t G, int32_t n_
     return plan_attend(c, G, n_requests, 1, max_tok, true, a, &bytes) == ICE_OK ? bytes : 0;
 }
 
+// (the sum of a launch's pieces of 128 keys is counted in 31 bits)
+static ice_status_t check_count(const ice_cache_t *c, const CacheAttend &a, bool listed) {
+    const double keys = listed ? a.max_keys : (double)a.max_blocks * c->block_size, rows = listed ? 1 : a.max_query * (double)a.G;
+    if ((keys / 128 + 3) * (rows / 192 + 2) * (a.S < 1024 ? a.S : 1024) * c->n_kv_heads >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %.0f keys x %.0f query rows: too many for one call", a.S, c->n_kv_heads, keys, rows);
+    return ICE_OK;
+}
+
 static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
                                  float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
     if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
     // (positions are rounded up to steps in 32 bits)
     if ((long long)a.max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: more than 2^30 tokens", a.max_blocks);
-    // (the sum of a launch's pieces of 128 keys is counted in 31 bits)
-    const double keys = a.pos ? a.max_keys : (double)a.max_blocks * c->block_size, rows = a.pos ? 1 : a.max_query * (double)a.G;
-    if ((keys / 128 + 3) * (rows / 192 + 2) * (a.S < 1024 ? a.S : 1024) * c->n_kv_heads >= 2147483648.0)
-        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %.0f keys x %.0f query rows: too many for one call", a.S, c->n_kv_heads, keys, rows);
+    if (ice_status_t st = check_count(c, a, a.pos != nullptr)) return st;
     if ((q_stride & 7) || (a.T > 1 && q_stride < (int64_t)c->n_kv_heads * a.G * kD))
         return fail(ICE_ERR_SHAPE, "q's stride must be a multiple of 8 and at least n_kv_heads * group_size * 128");
     if (!out || !aligned16(out)) return fail(ICE_ERR_INVALID_ARG, "out is null or misaligned");
@@ -584,6 +589,7 @@ ice_status_t ice_debug_cache_cut(const ice_cache_t *c, int32_t G, int32_t n_requ
     a.T = query_start ? n_tokens : n_requests;
     a.max_blocks = max_blocks;
     a.window = window;
+    if (ice_status_t st = check_count(c, a, !query_start)) return st;
     *n_parts = cut_cache_attend(a, !query_start, query_start, len, parts, max_parts);
     return ICE_OK;
 }

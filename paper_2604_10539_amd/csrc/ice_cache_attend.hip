@@ -2,7 +2,6 @@
 #include <algorithm>
 #include <array>
 #include <type_traits>
-#include <vector>
 
 #include "ice_cache.h"
 
@@ -1158,15 +1157,16 @@ template <bool LIST, typename F> static void cut_few(const CacheAttend &a, const
     const auto unit = [&](int s, int h) {
         return LIST ? Unit<LIST>(a, s, 1 << 30, len[s * a.c.H + h], 0) : Unit<LIST>(a, s, len[s], start[s], start[s + 1]);
     };
-    std::vector<unsigned> before(1, 0);  // quanta before each request
+    unsigned before[kEntries + 1] = {0};  // quanta before each request
     for (int e = 0; e < a.n_here; ++e)
-        before.push_back(before.back() + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, unit(a.first + e, 0), rows, quantum)));
+        before[e + 1] = before[e] + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, unit(a.first + e, 0), rows, quantum));
+    const unsigned total = before[a.n_here];
     const unsigned launched = a.whole ? a.n_here * a.c.H : a.few_groups;
-    const Pieces pieces(before.back(), launched, a.whole);
-    if (before.back() == 0) return;
+    const Pieces pieces(total, launched, a.whole);
+    if (total == 0) return;
     for (unsigned i = 0; i < pieces.groups && i < launched; ++i)
         for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
-            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
+            const int entry = (int)(std::upper_bound(before, before + a.n_here + 1, now) - before) - 1;
             const unsigned per = (before[entry + 1] - before[entry]) / a.c.H, h = (now - before[entry]) / per;
             const unsigned u0 = before[entry] + h * per, u1 = u0 + per;
             stop = std::min(u1, end);
@@ -1181,13 +1181,13 @@ template <bool LIST, typename F> static void cut_few(const CacheAttend &a, const
 }
 template <typename F> static void cut_many(const CacheAttend &a, const int *start, const int *len, F put) {
     const auto unit = [&](int s) { return Unit<false>(a, s, len[s], start[s], start[s + 1]); };
-    std::vector<unsigned> before(1, 0);
-    for (int e = 0; e < a.n_here; ++e) before.push_back(before.back() + (unsigned)a.c.H * Chunks(a, unit(a.first + e)).per_head);
-    const Pieces pieces(before.back(), a.many_groups, false);
-    if (before.back() == 0) return;
+    unsigned before[kEntries + 1] = {0};
+    for (int e = 0; e < a.n_here; ++e) before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, unit(a.first + e)).per_head;
+    const Pieces pieces(before[a.n_here], a.many_groups, false);
+    if (before[a.n_here] == 0) return;
     for (unsigned i = 0; i < pieces.groups && i < (unsigned)a.many_groups; ++i)
         for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
-            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
+            const int entry = (int)(std::upper_bound(before, before + a.n_here + 1, now) - before) - 1;
             const auto u = unit(a.first + entry);
             const Chunks ch(a, u);
             const unsigned h = (now - before[entry]) / ch.per_head;

@@ -124,6 +124,14 @@ def test_pieces_of_two_or_three_lengths(group, queries, lens):
     check(2, group, lens, [queries] * len(lens), block=64)
 
 
+def test_the_measured_cases():
+    from perf import operators
+    for case in operators.listed():
+        if case["kind"] == "attend":
+            cached, gain = operators._lengths(case)
+            check(case["heads"], case["group"], [c + g for c, g in zip(cached, gain)], gain, case["window"], block=case["block"])
+
+
 @pytest.mark.parametrize("queries", [1, 60])
 def test_more_requests_than_one_launch_takes(queries):
     rng = np.random.default_rng(queries)
@@ -173,6 +181,7 @@ def test_the_hook_refuses():
     c = p.make_cache_desc(None, 1, 2, 16)
     good = dict(group_size=4, n_requests=1, query_start=[0, 1], n_tokens=1, max_query=1, length=[5], max_keys=5, max_blocks=1)
     for change, status in ((dict(group_size=17), b.ICE_ERR_UNSUPPORTED), (dict(n_requests=0), b.ICE_ERR_SHAPE), (dict(max_blocks=0), b.ICE_ERR_SHAPE),
+                           (dict(n_requests=1024, query_start=[0] * 1025, length=[0] * 1024, max_query=2 ** 24, max_blocks=2 ** 20), b.ICE_ERR_UNSUPPORTED),
                            (dict(window=-1), b.ICE_ERR_SHAPE), (dict(max_query=0), b.ICE_ERR_SHAPE), (dict(max_blocks=2 ** 27), b.ICE_ERR_SHAPE)):
         with pytest.raises(p.IceError) as e:
             b.ice_debug_cache_cut(c, **{**good, **change})
