@@ -10,8 +10,8 @@
  * Conventions
  *   Pointers  Every tensor pointer is a DEVICE pointer owned by the caller, 16-byte aligned,
  *             contiguous and row-major as annotated.  bf16 = upper 16 bits of an IEEE fp32.
- *             The only host pointers are ice_config_t*, ice_index_view_t*, ice_index_t** and
- *             the flop count written by ice_debug_peak_mfma.
+ *             The only host pointers are ice_config_t*, ice_index_view_t*, ice_index_t**, ice_cache_t*,
+ *             the flop count written by ice_debug_peak_mfma and the arrays of the test hooks that say so.
  *   Memory    The library never allocates device memory.  The caller passes one workspace of
  *             ice_workspace_bytes() bytes (256-byte aligned) to ice_create(); page pools,
  *             tables, representatives, centroids and scratch all live inside it.

@@ -15,7 +15,7 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // rest: a slot, a block taken and a block given back each find their request by bisection and read one id.  A taken block that the
 // same call gives back is read from the row it comes from, not from the stack, so nothing waits for anything and the workgroups are
 // independent.  Lengths and the stack's height that are updated in place are written last: by the workgroup itself where there is one,
-// else by a second launch.  Bound by latency: a trip for the lengths, the scan, a trip for the ids.
+// else by a second launch.  Bound by latency: a trip for the lengths, the scan, the lengths again (a cache's trip), a trip for the ids.
 constexpr int kPlanThreads = 1024;           // at most
 constexpr int kPlanItems = 4096;             // requests whose lengths fit LDS beside the sums
 constexpr unsigned kPlanMost = 0x7FFFFFFFu;  // sums stop here: they only have to be known exactly where the step is possible

@@ -130,7 +130,8 @@ struct Keys {
 // where every CU has two or three, in the order of their indexes, the first kCus pieces are 3 / 16 longer than the average and the last ones as
 // much shorter, if pieces are long enough for whole quanta to follow that.  Equal pieces and these: a chunk of 2048 queries on 32 K keys, two
 // requests, 1750 and 1637 us; 24 mixed requests 273 and 259; 16 requests of up to 32 K tokens 71.0 and 68.5; drafts of 32 requests, 16 quanta a
-// piece, 57.3 and 55.5; but one request of 131 K tokens, 11 quanta a piece, 36.3 and 39.0.
+// piece, 57.3 and 55.5; but one request of 131 K tokens, 11 quanta a piece, 36.3 and 39.0.  The line is drawn between these two; where it is best was not
+// measured.
 constexpr unsigned kCus = 256;
 struct Pieces {
     unsigned groups, per, from1, from2, total;  // workgroups, those of a third (half, whole), where the pieces of the second and third begin
@@ -693,7 +694,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 // the few-query kernel does in registers, and leaves the operands in LDS as they are (a KiB each, 16 bytes a lane), from where all waves take
 // them.  Two buffers of 32 KiB: one barrier per round, and a wave may run a round ahead.  The next round's codes are on their way
 // meanwhile.  Outputs in bf16: weights rounded to bf16, one set of products; float32: three terms, cut off (three sets).  Two chunks of
-// 2048 queries on 32 K keys, 8 KV heads of 4 query heads, bf16: 1650 us, 1.17 PFLOP/s (a library product of 8192^3 reaches 1.13).
+// 2048 queries on 32 K keys, 8 KV heads of 4 query heads, bf16: 1620 to 1730 us on several cards, 1.12 to 1.19 PFLOP/s; a library product of 8192^3 in a
+// steady loop reaches 1.21 to 1.64 by the operands' layout (1.64 beside 1.18 here on one card).
 //
 // The work is flat as above.  A causal row tile sees the more keys the later it stands; so the tiles of a (request, KV head) are taken
 // in pairs, the last and the first, the last but one and the second, which cost the same together, and a pair's place in the flat
