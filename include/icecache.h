@@ -364,7 +364,8 @@ ice_status_t ice_cache_read(const ice_cache_t *cache, int32_t n_requests, const 
  *     fp32 outputs.  For bf16 outputs it does so in 16 bits or more where max_query * group_size <= 16, and for requests with at most 16 query rows (queries *
  *     group_size) where it is above 48; else it is rounded to bf16 once, which moves an output by at most 2^-8 of the sum of its terms' magnitudes and by about the
  *     rounding of the output itself (0.15 % and 0.17 % of its size on random values).  So what max_query allows decides how a bf16 output is rounded;
- *     the precision of fp32 outputs does not depend on it.
+ *     the precision of fp32 outputs does not depend on it.  The values are summed with weights of up to 2^8 each and then
+ *     divided by the weights' sum: magnitudes whose plain sum over the keys passes 2^119 may come out infinite.
  *   workspace: ice_cache_attend_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
  * UNSUPPORTED where the work could not be counted in 31 bits: (tokens of a table row / 128 + 3) * (max_query * group_size / 192 + 2) *
  * requests (at most 1024 of them) * n_kv_heads; give the longest rows and the most queries that there are. */
