@@ -405,7 +405,7 @@ def _own_run(s):
     dtype = getattr(torch, case["out"])
     if case["kind"] == "cross":
         return cache.attend_cross(s["q"], s["plan"], s["seq_len"], s["table"], max_shared=s["max_shared"], max_len=s["max_len"], out_dtype=dtype, with_lse=True)
-    return cache.attend_shared(s["q"], s["query_start"], s["plan"], s["seq_len"], s["table"], max_query=s["max_query"], max_shared=s["max_shared"],
+    return cache.attend_shared(s["q"], s["query_start"], s["source"], s["plan"], s["seq_len"], s["table"], max_query=s["max_query"], max_shared=s["max_shared"],
                                max_len=s["max_len"], max_source=s["max_source"], window=case["window"], out_dtype=dtype, with_lse=True)
 
 
