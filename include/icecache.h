@@ -388,6 +388,73 @@ ice_status_t ice_cache_attend_tokens(const ice_cache_t *cache, const void *q, in
                                      const int32_t *n_tok, int32_t max_tok, void *out, int32_t out_type, float *lse_or_null,
                                      void *workspace, size_t workspace_bytes, void *stream);
 
+/* A step's tokens enter the cache with their positions' rotation: ice_cache_write for keys that are rotated on the way, and the queries beside them.
+ * Token t belongs to the request s with query_start[s] <= t < query_start[s + 1]; its place in the request's row is
+ * seq_len[s] - query_start[s + 1] + t (seq_len after the step), its position that and, where source is given and names another row
+ * (source[s] in [0, n_requests), not s), seq_len[source[s]] more: the request's text begins with the tokens of that row (see ice_plan_sources).
+ *   k, v: bf16, as for ice_cache_write.  They are held at the token's place; one whose place or block does not exist is left out.
+ *   q_or_null: bf16, row t at q + t * q_stride elements, [n_q_heads][128] within it; q_out the same with q_out_stride; q_out may be q (with the same
+ *     stride).  Otherwise the arrays must not overlap.  q is given only with a rope.
+ *   rope_or_null: fp32 [n_positions][rotated], cos and then sin of rotated / 2 angles; rotated is a multiple of 16, up to 128.  Pair i of a row's first
+ *     `rotated` dimensions, (i, i + rotated / 2), or (2i, 2i + 1) with neighbours = 1, becomes (x cos - y sin, x sin + y cos): products and sums each rounded to
+ *     fp32; a query is then rounded to bf16, a key is held from fp32.  A token whose position has no row in it is left out, its row of q_out too.
+ *     NULL: keys enter as they are and positions are not looked at.
+ * Rows behind query_start[n_requests] are left as they were. */
+ice_status_t ice_cache_append(const ice_cache_t *cache, const void *q_or_null, int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride,
+                              const void *k, const void *v, int64_t k_stride, int64_t v_stride, int32_t n_tokens, int32_t n_requests,
+                              const int32_t *query_start, const int32_t *seq_len, const int32_t *source_or_null, const int32_t *block_table,
+                              int32_t max_blocks, const float *rope_or_null, int32_t n_positions, int32_t rotated, int32_t neighbours, void *stream);
+
+/* Rows of a block table that several requests read, their sources: a prefix that many requests' texts begin with, which lies in the cache once, in a
+ * row of its own among the requests' (n_rows = n_requests); or an encoder's states, rows of another table and cache.  One level: a source's own
+ * source is not looked at.  This call sorts a step's queries by source, so that a source's tokens are read once for all of them; a step makes it
+ * once, and every layer reads it.
+ *   source int32 [n_requests]: a row of the table in [0, n_rows), or anything else: none.
+ *   seq_len_or_null int32 [n_requests]: the requests' lengths behind their sources, where the sources are rows of the same table (a request that
+ *     names its own row then has no source); NULL where they are not, places are then 0.
+ *   plan int32 [2 * n_rows + 2 + 2 * n_tokens]:
+ *     start [n_rows + 2]: where in the list each row's queries begin; those of requests without a source at start[n_rows], and start[n_rows + 1] is their number;
+ *     lowest [n_rows]: the lowest place of a row's queries (seq_len[s] - its queries, of the requests that have any), 2^31 - 1 if it has none;
+ *     token [n_tokens]: the list, rows of q by source, those of one source in their own order; -1 behind the last one;
+ *     place [n_tokens]: the places of the listed queries, as for ice_cache_append; -1 behind the last one.
+ * SHAPE for n_requests or n_rows outside [1, 8192], n_tokens outside [0, 2^30]. */
+ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_tokens, const int32_t *source, const int32_t *query_start,
+                              const int32_t *seq_len_or_null, int32_t *plan, void *stream);
+
+/* Attention of every query to all tokens of its request's source (cross attention): softmax(q . k / sqrt(d)) . v without a mask, the source read
+ * once for all queries that share it.
+ *   plan: as ice_plan_sources wrote it for the same n_rows and n_tokens, and query_start and source of this step.
+ *   seq_len [n_rows], block_table [n_rows][max_blocks]: those of the sources.  max_keys: about the longest of them, a hint.
+ *   max_shared: no source has more queries (tokens; those beyond are left out), in [1, 2^24].
+ *   q, out, out_type, lse, Precision: as for ice_cache_attend, with max_shared in the place of max_query, and a source's queries in the place of a
+ *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
+ *   workspace: ice_cache_attend_cross_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
+ * SHAPE for n_rows > 8192; UNSUPPORTED as for ice_cache_attend. */
+size_t ice_cache_attend_cross_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, int32_t max_shared, int32_t max_keys);
+ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_rows, const int32_t *plan,
+                                    int32_t n_tokens, int32_t max_shared, const int32_t *seq_len, int32_t max_keys, const int32_t *block_table,
+                                    int32_t max_blocks, void *out, int32_t out_type, float *lse_or_null, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/* Causal attention of requests whose texts begin with a source's tokens: ice_cache_attend over the source's row and the request's own as one
+ * text, the source read once for all requests that share it.  Query j of request s stands at place seq_len[s] - (number of s's queries) + j of its
+ * row and at that position behind the source's seq_len tokens; it sees the positions up to its own, with window > 0 only the last `window`.
+ * A request without a source (see ice_plan_sources) is attended to as by ice_cache_attend.
+ *   source, plan: as given to and written by ice_plan_sources for this step, n_rows = n_requests, with seq_len.
+ *   max_query, max_keys: of the requests' own queries and tokens, as for ice_cache_attend; max_shared: no source has more queries (tokens of all its requests;
+ *     those beyond are left out, their outputs as they were), in [1, 2^24]; max_source_keys: about the longest source, a hint.
+ *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there; a bf16 output's weights on its own tokens follow max_query, those on the source
+ *     max_shared.
+ *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 528 for every row of out, and scratch.
+ * SHAPE for n_requests > 8192; UNSUPPORTED as for ice_cache_attend. */
+size_t ice_cache_attend_shared_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t n_tokens, int32_t max_query,
+                                     int32_t max_shared, int32_t max_keys, int32_t max_source_keys);
+ice_status_t ice_cache_attend_shared(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,
+                                     const int32_t *query_start, const int32_t *source, const int32_t *plan, int32_t n_tokens, int32_t max_query,
+                                     int32_t max_shared, const int32_t *seq_len, int32_t max_keys, int32_t max_source_keys, const int32_t *block_table,
+                                     int32_t max_blocks, int32_t window, void *out, int32_t out_type, float *lse_or_null, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
 /* Test and snapshot surface.  Export fills `view` with pointers INTO the workspace (no copy).
  * Import copies caller arrays (device pointers, same layout; the export-only fields are
  * ignored; n_tokens, page_size, n_clusters, max_pages must fit the workspace) into the index and
@@ -443,6 +510,11 @@ ice_status_t ice_debug_near_bounds(int32_t n, const float *key_norm2, const floa
 ice_status_t ice_debug_cache_cut(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, const int32_t *query_start, int32_t n_tokens,
                                  int32_t max_query, const int32_t *len, int32_t max_keys, int32_t max_blocks, int32_t window, int32_t *parts,
                                  int64_t max_parts, int64_t *n_parts);
+
+/* Test hook: ice_debug_cache_cut for ice_cache_attend_cross (and the sources' half of ice_cache_attend_shared without a window).  start: the list's start
+ * [n_rows + 2], seq_len [n_rows], HOST arrays; a part's request is its source, its first row counts the source's queries. */
+ice_status_t ice_debug_cross_cut(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, const int32_t *start, int32_t n_tokens, int32_t max_shared,
+                                 const int32_t *seq_len, int32_t max_keys, int32_t max_blocks, int32_t *parts, int64_t max_parts, int64_t *n_parts);
 
 /* Test hook for the failure path of ice_select / ice_select_attend when a unit is served by several
  * workgroups (fewer than 256 units): those workgroups hand their page scores to the last one of

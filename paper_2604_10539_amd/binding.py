@@ -22,7 +22,9 @@ SYMBOLS = ["ice_workspace_bytes", "ice_create", "ice_destroy", "ice_build_index"
            "ice_attend", "ice_attend_noalloc", "ice_select_attend", "ice_attend_resident", "ice_select_attend_resident", "ice_selected_tokens", "ice_attend_tokens", "ice_select_hier", "ice_select_hier3", "ice_build_top_level", "ice_export_top_level", "ice_set_geometry", "ice_export_geometry", "ice_export_index", "ice_import_index", "ice_debug_assign", "ice_debug_rerun_stage", "ice_debug_build_plan", "ice_debug_near_bounds", "ice_debug_select_fault",
            "ice_debug_peak_read", "ice_debug_peak_mfma", "ice_last_error",
            "ice_cache_bytes", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
-           "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes", "ice_debug_cache_cut"]
+           "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes", "ice_debug_cache_cut",
+           "ice_plan_sources", "ice_cache_append", "ice_cache_attend_cross_bytes", "ice_cache_attend_cross", "ice_cache_attend_shared_bytes",
+           "ice_cache_attend_shared", "ice_debug_cross_cut"]
 
 
 class IceConfig(C.Structure):
@@ -127,8 +129,17 @@ def lib() -> C.CDLL:
         L.ice_cache_attend.argtypes = [desc, ptr, i64, i32, i32, ptr, i32, i32, ptr, i32, ptr, i32, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         L.ice_cache_attend_tokens.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
         L.ice_debug_cache_cut.argtypes = [desc, i32, i32, ptr, i32, i32, ptr, i32, i32, i32, ptr, i64, C.POINTER(C.c_int64)]
+        L.ice_cache_attend_cross_bytes.restype = L.ice_cache_attend_shared_bytes.restype = C.c_size_t
+        L.ice_plan_sources.argtypes = [i32] * 3 + [ptr] * 5
+        L.ice_cache_append.argtypes = [desc, ptr, i64, i32, ptr, i64, ptr, ptr, i64, i64, i32, i32, ptr, ptr, ptr, ptr, i32, ptr, i32, i32, i32, ptr]
+        L.ice_cache_attend_cross_bytes.argtypes = [desc, i32, i32, i32, i32]
+        L.ice_cache_attend_cross.argtypes = [desc, ptr, i64, i32, i32, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, ptr, C.c_size_t, ptr]
+        L.ice_cache_attend_shared_bytes.argtypes = [desc] + [i32] * 7
+        L.ice_cache_attend_shared.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, ptr, i32, i32, i32, ptr, i32, i32, ptr, i32, i32, ptr, i32, ptr, ptr,
+                                              C.c_size_t, ptr]
+        L.ice_debug_cross_cut.argtypes = [desc, i32, i32, ptr, i32, i32, ptr, i32, i32, ptr, i64, C.POINTER(C.c_int64)]
         for name in SYMBOLS:
-            if name not in ("ice_last_error", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
+            if name not in ("ice_last_error", "ice_cache_attend_cross_bytes", "ice_cache_attend_shared_bytes", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
                             "ice_cache_attend_tokens_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
@@ -136,8 +147,8 @@ def lib() -> C.CDLL:
 
 
 def _extension():
-    """The extension module, bound to the library.  It belongs to one Python and one torch; only the 4-bit cache's classes and
-    ice_plan_blocks need it."""
+    """The extension module, bound to the library.  It belongs to one Python and one torch; only the 4-bit cache's classes,
+    ice_plan_blocks and ice_plan_sources need it."""
     global _native
     if _native is None:
         L = lib()
@@ -148,7 +159,8 @@ def _extension():
                                "`python -c 'import __graft_entry__ as g; g.build()'`" % e) from e
         _calls.bind(IceError, *(C.cast(getattr(L, name), C.c_void_p).value for name in (
             "ice_last_error", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
-            "ice_cache_attend_tokens_bytes", "ice_cache_attend_tokens")))
+            "ice_cache_attend_tokens_bytes", "ice_cache_attend_tokens", "ice_plan_sources", "ice_cache_append", "ice_cache_attend_cross_bytes",
+            "ice_cache_attend_cross", "ice_cache_attend_shared_bytes", "ice_cache_attend_shared")))
         _native = _calls
     return _native
 
@@ -395,6 +407,41 @@ def ice_cache_attend_tokens(cache: IceCacheDesc, q, q_stride, group_size, n_requ
     _check(lib().ice_cache_attend_tokens(C.byref(cache), q, q_stride, group_size, n_requests, _ptr(seq_len), _ptr(block_table), max_blocks,
                                          _ptr(token_pos), _ptr(n_tok), max_tok, _ptr(out), out_type, _ptr(lse), _ptr(workspace),
                                          workspace_bytes, _stream(stream)))
+
+
+def ice_plan_sources(source, query_start, seq_len, plan, n_rows, n_tokens, stream=None) -> None:
+    """int32 device tensors as in the header; seq_len None where the sources are rows of another table."""
+    _extension().plan_sources(_stream(stream) or 0, source, query_start, seq_len, plan, n_rows, n_tokens)
+
+
+def ice_cache_append(cache: IceCacheDesc, q, q_stride, n_q_heads, q_out, q_out_stride, k, v, k_stride, v_stride, n_tokens, n_requests, query_start, seq_len,
+                     source, block_table, max_blocks, rope, n_positions, rotated, neighbours, stream=None) -> None:
+    """q, q_out, k, v: addresses (rows need not be contiguous with each other)."""
+    _check(lib().ice_cache_append(C.byref(cache), q, q_stride, n_q_heads, q_out, q_out_stride, k, v, k_stride, v_stride, n_tokens, n_requests, _ptr(query_start),
+                                  _ptr(seq_len), _ptr(source), _ptr(block_table), max_blocks, _ptr(rope), n_positions, rotated, neighbours, _stream(stream)))
+
+
+def ice_cache_attend_cross_bytes(cache: IceCacheDesc, group_size, n_rows, max_shared, max_keys) -> int:
+    return lib().ice_cache_attend_cross_bytes(C.byref(cache), group_size, n_rows, max_shared, max_keys)
+
+
+def ice_cache_attend_cross(cache: IceCacheDesc, q, q_stride, group_size, n_rows, plan, n_tokens, max_shared, seq_len, max_keys, block_table, max_blocks, out,
+                           out_type, lse, workspace, workspace_bytes, stream=None) -> None:
+    """q: an address (its rows need not be contiguous with each other)."""
+    _check(lib().ice_cache_attend_cross(C.byref(cache), q, q_stride, group_size, n_rows, _ptr(plan), n_tokens, max_shared, _ptr(seq_len), max_keys,
+                                        _ptr(block_table), max_blocks, _ptr(out), out_type, _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ice_cache_attend_shared_bytes(cache: IceCacheDesc, group_size, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys) -> int:
+    return lib().ice_cache_attend_shared_bytes(C.byref(cache), group_size, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys)
+
+
+def ice_cache_attend_shared(cache: IceCacheDesc, q, q_stride, group_size, n_requests, query_start, source, plan, n_tokens, max_query, max_shared, seq_len,
+                            max_keys, max_source_keys, block_table, max_blocks, window, out, out_type, lse, workspace, workspace_bytes, stream=None) -> None:
+    """q: an address (its rows need not be contiguous with each other)."""
+    _check(lib().ice_cache_attend_shared(C.byref(cache), q, q_stride, group_size, n_requests, _ptr(query_start), _ptr(source), _ptr(plan), n_tokens, max_query,
+                                         max_shared, _ptr(seq_len), max_keys, max_source_keys, _ptr(block_table), max_blocks, window, _ptr(out), out_type,
+                                         _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 # ------------------------------------------------------------------------------------------------
@@ -650,6 +697,20 @@ def ice_debug_cache_cut(cache: IceCacheDesc, group_size, n_requests, query_start
         parts = np.empty((n.value, len(CUT_FIELDS)), dtype=np.int32)
 
 
+def ice_debug_cross_cut(cache: IceCacheDesc, group_size, n_rows, start, n_tokens, max_shared, length, max_keys, max_blocks):
+    """numpy arrays on the host: start, the sorted list's, and length int32 -> the parts, int32 [n, 15] in the order of CUT_FIELDS."""
+    import numpy as np
+    start, length = (np.ascontiguousarray(x, dtype=np.int32) for x in (start, length))
+    n = C.c_int64(0)
+    parts = np.empty((1 << 12, len(CUT_FIELDS)), dtype=np.int32)
+    while True:
+        _check(lib().ice_debug_cross_cut(C.byref(cache), group_size, n_rows, start.ctypes.data, n_tokens, max_shared, length.ctypes.data, max_keys, max_blocks,
+                                         parts.ctypes.data, len(parts), C.byref(n)))
+        if n.value <= len(parts):
+            return parts[: n.value]
+        parts = np.empty((n.value, len(CUT_FIELDS)), dtype=np.int32)
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us against 0.5: it does not ask whether CUDA is up)
 
 
@@ -699,6 +760,20 @@ class IceBlocks:
         return self.query_start, slots, self.info
 
 
+    def plan_sources(self, source, n_tokens, plan=None, stream=None):
+        """The queries of the step that plan() planned, sorted by the source of their requests, for the layers' attend_shared.  source int32
+        [max_requests] on the GPU: the row whose tokens come before request s's own in its text; -1 (any row that there is not, or its own): none.  n_tokens: rows of q.
+        -> plan, int32 [2 * max_requests + 2 + 2 * n_tokens] (see ice_plan_sources in the header).
+
+        A source is a row like any other: it gains its tokens by plan() once, and gives them back when no request names it any more."""
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceBlocks.plan_sources, self, stream, source, n_tokens, plan)
+        if plan is None:
+            plan = torch.empty(2 * self.max_requests + 2 + 2 * n_tokens, dtype=torch.int32, device=self.device)
+        ice_plan_sources(source, self.query_start, self.seq_len, plan, self.max_requests, n_tokens)
+        return plan
+
+
 class IceCache:
     """One layer's KV cache in 4 bits (see ice_cache_t in the header).  bf16 tensors may be torch.bfloat16 or int16 bit
     patterns.  Tables, lengths, slots and positions are int32 tensors on the GPU, contiguous.  Every method takes `stream`, a torch stream
@@ -723,6 +798,17 @@ class IceCache:
         if stream is not None or _current_device() != self._index:
             return _elsewhere(IceCache.write, self, stream, k, v, slots)
         _native.write(self._at, self._index, _stream_on(self._index), k, v, slots)
+
+    def append(self, k, v, query_start, seq_len, block_table, q=None, out=None, rope=None, neighbours=False, source=None, stream=None):
+        """A step's tokens enter the cache, k, v [tokens, n_kv_heads, 128], and its queries q [tokens, heads, 128] come back, both rotated by their
+        positions.  rope float32 [positions, rotated]: cos and then sin of rotated / 2 angles (None: k enters as it is, without q); pairs are rotated / 2 apart, or
+        neighbours.  seq_len: after the step.  source int32 [requests]: as for IceBlocks.plan_sources; a request's positions follow its source's tokens.
+        -> q rotated, bf16: out if it is given (it may be q), else new; None without q.  Rows of tokens behind query_start[-1], and of those whose position
+        has no row in rope, are left as they were."""
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.append, self, stream, k, v, query_start, seq_len, block_table, q, out, rope, neighbours, source)
+        return _native.append(self._at, self._index, _stream_on(self._index), k, v, query_start, seq_len, block_table, q, out, rope, bool(neighbours),
+                              source)
 
     def read(self, block_table, seq_len, n_rows, first=None, out=(None, None), stream=None):
         """(K, V) bf16 [requests, n_kv_heads, n_rows, 128]: the tokens from position first[s] on, as they are held."""
@@ -749,6 +835,29 @@ class IceCache:
             return _elsewhere(IceCache.attend_tokens, self, stream, q, seq_len, block_table, token_pos, n_tok, out, out_dtype, lse, with_lse)
         return _native.attend_tokens(self._at, self._index, _stream_on(self._index), q, seq_len, block_table, token_pos, n_tok, out,
                                      _is_bf16(out_dtype), lse, bool(with_lse))
+
+
+    def attend_cross(self, q, plan, seq_len, block_table, max_shared=None, max_len=None, out=None, out_dtype=torch.float32, lse=None, with_lse=False,
+                     stream=None):
+        """Attention of queries q [tokens, heads, 128] to all tokens of their requests' sources, the rows of block_table and seq_len; plan: the queries sorted
+        by source, by ice_plan_sources (without lengths).  max_shared, max_len: what the host knows of the most queries (tokens) that share a source (none has
+        more) and the longest source (a hint).  Queries without a source get 0 and -inf.  -> out, or (out, lse), as attend."""
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.attend_cross, self, stream, q, plan, seq_len, block_table, max_shared, max_len, out, out_dtype, lse, with_lse)
+        return _native.attend_cross(self._at, self._index, _stream_on(self._index), q, plan, seq_len, block_table, max_shared, max_len, out,
+                                    _is_bf16(out_dtype), lse, bool(with_lse))
+
+    def attend_shared(self, q, query_start, source, plan, seq_len, block_table, max_query=None, max_shared=None, max_len=None, max_source=None, window=0,
+                      out=None, out_dtype=torch.float32, lse=None, with_lse=False, stream=None):
+        """attend where requests' texts begin with the tokens of a source, a row of the same table: causal attention over that row and the request's own as
+        one text; a source is read once for all queries that share it.  source and plan: as given to and returned by IceBlocks.plan_sources for this
+        step.  max_query, max_len: as for attend, of the requests' own; max_shared: the most queries (tokens) of all requests that share a source (none has
+        more); max_source: about the longest source (a hint).  Give them wherever they are known.  -> out, or (out, lse), as attend."""
+        if stream is not None or _current_device() != self._index:
+            return _elsewhere(IceCache.attend_shared, self, stream, q, query_start, source, plan, seq_len, block_table, max_query, max_shared, max_len,
+                              max_source, window, out, out_dtype, lse, with_lse)
+        return _native.attend_shared(self._at, self._index, _stream_on(self._index), q, query_start, source, plan, seq_len, block_table, max_query, max_shared,
+                                     max_len, max_source, window, out, _is_bf16(out_dtype), lse, bool(with_lse))
 
 
 def _is_bf16(dtype):

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libicecache.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["ice_api.hip", "ice_build.hip", "ice_decode.hip", "ice_hier.hip", "ice_peaks.hip", "ice_cache.hip",
-           "ice_cache_attend.hip"]
+           "ice_cache_attend.hip", "ice_cache_shared.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
          # packed-fp32 instruction selection is switched off for all device code

@@ -513,8 +513,8 @@ static ice_status_t check_count(const ice_cache_t *c, const CacheAttend &a, bool
     return ICE_OK;
 }
 
-static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
-                                 float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
+static ice_status_t set_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type, float *lse, void *ws,
+                               size_t ws_bytes, size_t need) {
     if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
     // (positions are rounded up to steps in 32 bits)
     if ((long long)a.max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: more than 2^30 tokens", a.max_blocks);
@@ -531,6 +531,12 @@ static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const voi
     a.out_bf16 = out_type == ICE_OUT_BF16;
     a.lse = lse;
     a.part = static_cast<float *>(ws);
+    return ICE_OK;
+}
+
+static ice_status_t cache_attend(const ice_cache_t *c, CacheAttend &a, const void *q, int64_t q_stride, void *out, int32_t out_type,
+                                 float *lse, void *ws, size_t ws_bytes, size_t need, void *stream, const char *who) {
+    if (ice_status_t st = set_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
     launch_cache_attend(a, static_cast<hipStream_t>(stream));
     return device_status(who);
 }
@@ -574,6 +580,168 @@ ice_status_t ice_cache_attend_tokens(const ice_cache_t *c, const void *q, int64_
     a.pos = pos;
     a.n_tok = n_tok;
     return cache_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need, stream, "ice_cache_attend_tokens");
+}
+
+// ---- rows of a table that requests share
+
+ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_tokens, const int32_t *source, const int32_t *query_start,
+                              const int32_t *seq_len, int32_t *plan, void *stream) {
+    if (!source || !query_start || !plan) return fail(ICE_ERR_INVALID_ARG, "source, query_start or plan is null");
+    if (n_requests < 1 || n_requests > kSourceRows) return fail(ICE_ERR_SHAPE, "n_requests %d is outside [1, %d]", n_requests, kSourceRows);
+    if (n_rows < 1 || n_rows > kSourceRows) return fail(ICE_ERR_SHAPE, "n_rows %d is outside [1, %d]", n_rows, kSourceRows);
+    if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_tokens %d is outside [0, 2^30]", n_tokens);
+    launch_plan_sources({n_requests, n_rows, n_tokens, source, query_start, seq_len, plan}, static_cast<hipStream_t>(stream));
+    return device_status("ice_plan_sources");
+}
+
+ice_status_t ice_cache_append(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride, const void *k,
+                              const void *v, int64_t k_stride, int64_t v_stride, int32_t n_tokens, int32_t n_requests, const int32_t *query_start,
+                              const int32_t *seq_len, const int32_t *source, const int32_t *table, int32_t max_blocks, const float *rope,
+                              int32_t n_positions, int32_t rotated, int32_t neighbours, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
+    if (!query_start) return fail(ICE_ERR_INVALID_ARG, "query_start is null");
+    if (n_tokens < 0) return fail(ICE_ERR_SHAPE, "n_tokens must be >= 0");
+    if (neighbours != 0 && neighbours != 1) return fail(ICE_ERR_INVALID_ARG, "neighbours %d: 0 or 1", neighbours);
+    if (rope) {
+        if (!aligned16(rope)) return fail(ICE_ERR_INVALID_ARG, "rope is misaligned");
+        if (n_positions < 1) return fail(ICE_ERR_SHAPE, "n_positions must be >= 1");
+        if (rotated < 16 || rotated > kD || rotated % 16) return fail(ICE_ERR_UNSUPPORTED, "rotated %d: a multiple of 16, at most %d", rotated, kD);
+    } else if (q) {
+        return fail(ICE_ERR_INVALID_ARG, "queries without a table of rotations: nothing to do with them");
+    }
+    if (q && (n_q_heads < 1 || n_q_heads > 65536)) return fail(ICE_ERR_SHAPE, "n_q_heads %d is outside [1, 65536]", n_q_heads);
+    if (n_tokens == 0) return ICE_OK;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(ICE_ERR_INVALID_ARG, "k or v is null or misaligned");
+    if (q && (!aligned16(q) || !q_out || !aligned16(q_out))) return fail(ICE_ERR_INVALID_ARG, "q or q_out is null or misaligned");
+    const int64_t row = (int64_t)c->n_kv_heads * kD, q_row = (int64_t)n_q_heads * kD;
+    if ((k_stride & 7) || (v_stride & 7) || (n_tokens > 1 && (k_stride < row || v_stride < row)))
+        return fail(ICE_ERR_SHAPE, "strides must be multiples of 8 and at least n_kv_heads * 128");
+    if (q && ((q_stride & 7) || (q_out_stride & 7) || (n_tokens > 1 && (q_stride < q_row || q_out_stride < q_row))))
+        return fail(ICE_ERR_SHAPE, "strides of q and q_out must be multiples of 8 and at least n_q_heads * 128");
+    CacheAppend a{};
+    a.q_heads = q ? n_q_heads : 0;
+    if ((double)((n_tokens + 3ll) / 4) * (a.q_heads + 2.0 * c->n_kv_heads) > 4e7) return fail(ICE_ERR_UNSUPPORTED, "too many rows for one call");
+    a.c = cache_dims(c);
+    a.q = static_cast<const bf16_t *>(q);
+    a.k = static_cast<const bf16_t *>(k);
+    a.v = static_cast<const bf16_t *>(v);
+    a.q_out = static_cast<bf16_t *>(q_out);
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
+    a.n_tokens = n_tokens, a.n_requests = n_requests, a.max_blocks = max_blocks;
+    a.query_start = query_start, a.seq_len = seq_len, a.table = table, a.source = source;
+    a.rope = rope, a.n_positions = n_positions, a.half = rope ? rotated / 2 : 0, a.neighbours = neighbours != 0;
+    launch_cache_append(a, static_cast<hipStream_t>(stream));
+    return device_status("ice_cache_append");
+}
+
+static ice_status_t check_rows(int32_t n_rows) {
+    return n_rows < 1 || n_rows > kSourceRows ? fail(ICE_ERR_SHAPE, "%d rows of the table: outside [1, %d]", n_rows, kSourceRows) : ICE_OK;
+}
+
+// where a list's parts lie (ice_plan_sources)
+static void set_list(CacheAttend &a, const int32_t *plan) {
+    a.query_start = plan;
+    a.lowest = plan + a.S + 2;
+    a.token = plan + 2 * (size_t)a.S + 2;
+    a.place = a.token + a.T;
+}
+
+size_t ice_cache_attend_cross_bytes(const ice_cache_t *c, int32_t G, int32_t n_rows, int32_t max_shared, int32_t max_keys) {
+    CacheAttend a{};
+    size_t bytes = 0;
+    if (check_rows(n_rows) != ICE_OK) return 0;
+    return plan_attend(c, G, n_rows, max_shared, max_keys, false, a, &bytes) == ICE_OK ? bytes : 0;
+}
+
+ice_status_t ice_cache_attend_cross(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t G, int32_t n_rows, const int32_t *plan, int32_t n_tokens,
+                                    int32_t max_shared, const int32_t *seq_len, int32_t max_keys, const int32_t *table, int32_t max_blocks, void *out,
+                                    int32_t out_type, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_rows(n_rows)) return st;
+    if (ice_status_t st = check_table(c, n_rows, seq_len, table, max_blocks)) return st;
+    if (!plan) return fail(ICE_ERR_INVALID_ARG, "plan is null");
+    if (n_tokens < 0) return fail(ICE_ERR_SHAPE, "n_tokens must be >= 0");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_attend(c, G, n_rows, max_shared, max_keys, false, a, &need)) return st;
+    if (n_tokens == 0) return ICE_OK;
+    a.T = n_tokens;
+    set_list(a, plan);
+    a.seq_len = seq_len;
+    a.table = table;
+    a.max_blocks = max_blocks;
+    if (ice_status_t st = set_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
+    launch_cache_cross(a, static_cast<hipStream_t>(stream));
+    return device_status("ice_cache_attend_cross");
+}
+
+// the two halves of a call, and what it needs: the rows' sums, and behind them the scratch that the halves use one after the other
+static ice_status_t plan_shared(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t n_tokens, int32_t max_query, int32_t max_shared,
+                                int32_t max_keys, int32_t max_source_keys, CacheAttend &own, CacheAttend &join, size_t *bytes) {
+    if (ice_status_t st = check_rows(n_requests)) return st;
+    if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_tokens %d is outside [0, 2^30]", n_tokens);
+    size_t first = 0, second = 0;
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, false, own, &first)) return st;
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_shared, max_source_keys, false, join, &second)) return st;
+    own.T = join.T = n_tokens;
+    *bytes = cache_state_bytes(own) + std::max(first, second);
+    return ICE_OK;
+}
+
+size_t ice_cache_attend_shared_bytes(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t n_tokens, int32_t max_query, int32_t max_shared,
+                                     int32_t max_keys, int32_t max_source_keys) {
+    CacheAttend own{}, join{};
+    size_t bytes = 0;
+    return plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, own, join, &bytes) == ICE_OK ? bytes : 0;
+}
+
+ice_status_t ice_cache_attend_shared(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t G, int32_t n_requests, const int32_t *query_start,
+                                     const int32_t *source, const int32_t *plan, int32_t n_tokens, int32_t max_query, int32_t max_shared,
+                                     const int32_t *seq_len, int32_t max_keys, int32_t max_source_keys, const int32_t *table, int32_t max_blocks,
+                                     int32_t window, void *out, int32_t out_type, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    if (ice_status_t st = check_cache_data(c)) return st;
+    if (ice_status_t st = check_rows(n_requests)) return st;
+    if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
+    if (!query_start || !source || !plan) return fail(ICE_ERR_INVALID_ARG, "query_start, source or plan is null");
+    if (window < 0) return fail(ICE_ERR_SHAPE, "window must be >= 0 (0: no window)");
+    CacheAttend own{}, join{};
+    size_t need = 0;
+    if (ice_status_t st = plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, own, join, &need)) return st;
+    if (n_tokens == 0) return ICE_OK;
+    for (CacheAttend *a : {&own, &join}) {
+        a->seq_len = seq_len;
+        a->table = table;
+        a->max_blocks = max_blocks;
+        a->window = window;
+        a->source = source;
+    }
+    own.query_start = query_start;
+    set_list(join, plan);
+    for (CacheAttend *a : {&own, &join}) {
+        if (ice_status_t st = set_attend(c, *a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
+        a->state = static_cast<float *>(ws);
+        a->part = a->state + cache_state_bytes(own) / sizeof(float);
+    }
+    launch_cache_shared(own, join, static_cast<hipStream_t>(stream));
+    return device_status("ice_cache_attend_shared");
+}
+
+ice_status_t ice_debug_cross_cut(const ice_cache_t *c, int32_t G, int32_t n_rows, const int32_t *start, int32_t n_tokens, int32_t max_shared,
+                                 const int32_t *len, int32_t max_keys, int32_t max_blocks, int32_t *parts, int64_t max_parts, int64_t *n_parts) {
+    if (ice_status_t st = check_cache(c)) return st;
+    if (ice_status_t st = check_rows(n_rows)) return st;
+    if (!start || !len || !parts || !n_parts) return fail(ICE_ERR_INVALID_ARG, "a pointer is null");
+    if (max_blocks < 1 || (long long)max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, at most 2^30 tokens", max_blocks);
+    if (n_tokens < 0 || max_parts < 0) return fail(ICE_ERR_SHAPE, "n_tokens and max_parts must be >= 0");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_attend(c, G, n_rows, max_shared, max_keys, false, a, &need)) return st;
+    a.T = n_tokens;
+    a.max_blocks = max_blocks;
+    if (ice_status_t st = check_count(c, a, false)) return st;
+    *n_parts = cut_cache_cross(a, start, len, parts, max_parts);
+    return ICE_OK;
 }
 
 ice_status_t ice_debug_cache_cut(const ice_cache_t *c, int32_t G, int32_t n_requests, const int32_t *query_start, int32_t n_tokens, int32_t max_query,

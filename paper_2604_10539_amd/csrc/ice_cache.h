@@ -38,9 +38,9 @@ void launch_cache_read(const CacheDims &c, int n_requests, const int *seq_len, c
                        int n_rows, bf16_t *k, bf16_t *v, hipStream_t stream);
 
 // A (request, KV head) that was cut between workgroups: the first one of them, the KV head, the request's first query row, the first of the
-// unit's rows and the number of the request's rows (query, head of the group).  
+// unit's rows and the number of the request's rows (query, head of the group); of Own, whether the request has no source.
 struct alignas(16) MergeNote {
-    int first, h, row0, base, rows;
+    int first, h, row0, base, rows, alone;
 };
 
 struct CacheAttend {
@@ -61,13 +61,43 @@ struct CacheAttend {
     int first, n_here;  // the launch's requests
     float scale_log2;
     bool out_bf16;
+    // of queries that are gathered by source (ice_plan_sources): the sorted list's tokens and places, each source's lowest place; the requests' sources;
+    // the sums of the queries over their own tokens, a record each
+    const int *token, *place, *lowest, *source;
+    float *state;
 };
 // How a call is cut, from the sizes: fills few_groups, many_groups, many, per_unit and whole; returns the bytes of workspace.
 size_t plan_cache_attend(CacheAttend &a, bool listed);
 void launch_cache_attend(CacheAttend a, hipStream_t stream);
+void launch_cache_cross(const CacheAttend &a, hipStream_t stream);
+void launch_cache_shared(const CacheAttend &own, const CacheAttend &join, hipStream_t stream);
 // The parts that the workgroups of a planned call take, from lengths on the host (query_start and seq_len, or n_tok): their number, the first `most` of
 // them in parts, kCutInts words each (see ice_debug_cache_cut).
 constexpr int kCutInts = 15;
 long long cut_cache_attend(CacheAttend a, bool listed, const int *query_start, const int *len, int *parts, long long most);
+long long cut_cache_cross(CacheAttend a, const int *start, const int *len, int *parts, long long most);
+size_t cache_state_bytes(const CacheAttend &a);
+
+// The queries of a step sorted by the row of the table that their requests name.
+struct CacheSources {
+    int n_requests, n_rows, n_tokens;
+    const int *source, *query_start, *seq_len;
+    int *plan;
+};
+constexpr int kSourceRows = 8192;  // requests, and rows of the table, of one call at most
+void launch_plan_sources(const CacheSources &p, hipStream_t stream);
+
+struct CacheAppend {
+    CacheDims c;
+    const bf16_t *q, *k, *v;
+    long long q_stride, k_stride, v_stride, q_out_stride;
+    bf16_t *q_out;
+    int q_heads, n_tokens, n_requests, max_blocks;
+    const int *query_start, *seq_len, *table, *source;
+    const float *rope;
+    int n_positions, half;  // pairs of a row that are rotated
+    bool neighbours;
+};
+void launch_cache_append(const CacheAppend &a, hipStream_t stream);
 
 }  // namespace ice

@@ -221,6 +221,149 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, const bf1
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------- append
+// Eight dims of a row whose blocks of 32 lie on four lanes side by side: codes and the block's scale byte, from 32 bits.
+__device__ inline uint32_t hold(const float (&f)[8], int &scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+    top = max(top, dpp_u32<0xB1>(top));
+    top = max(top, dpp_u32<0x4E>(top));
+    const int exponent = (int)(top >> 23);
+    const bool lost = exponent == 255;
+    scale = lost ? 255 : min(max(exponent - 2 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 27), 252);
+    const float sf = __uint_as_float((uint32_t)scale << 23);
+    uint32_t code = 0;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[0], f[1], sf, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[2], f[3], sf, 1);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[4], f[5], sf, 2);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[6], f[7], sf, 3);
+    return lost ? 0u : code;
+}
+__device__ inline void widen8(const uint4 &w, float (&f)[8]) {
+    const uint32_t d[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(d[e] << 16);
+        f[2 * e + 1] = __uint_as_float(d[e] & 0xFFFF0000u);
+    }
+}
+__device__ inline uint32_t round2(float a, float b) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// A wave takes four consecutive tokens, 16 lanes of 8 dims to a row, and PER heads of them: of the queries, then the keys, then the values.
+// Pair i of a row's rotated dims (half apart, or neighbours) becomes (x cos - y sin, x sin + y cos), products and sums each rounded to
+// 32 bits; a query is then rounded to bf16 and a key held, so either is rounded to fewer bits once.
+template <int PER>
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int chunks) {
+    const int lane = threadIdx.x & 63, i = lane & 15, r = lane >> 4;
+    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int chunk = (int)(unit % chunks);
+    const long long t0 = unit / chunks * 4;
+    if (t0 >= a.n_tokens) return;
+    const int t = (int)min(t0 + r, (long long)a.n_tokens - 1), n = a.n_requests;
+    const int pair_lanes = a.half >> 3, head0 = chunk * PER;
+    const bool turned = i < 2 * pair_lanes, first = i < pair_lanes;
+    const int other = a.neighbours || !turned ? i : first ? i + pair_lanes : i - pair_lanes;
+    uint4 w[PER], u[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int c = head0 + j;
+        const bf16_t *x = nullptr;
+        if (c < a.q_heads) x = a.q + t * a.q_stride + (long long)c * kD;
+        else if (c < a.q_heads + a.c.H) x = a.k + t * a.k_stride + (long long)(c - a.q_heads) * kD;
+        else if (c < a.q_heads + 2 * a.c.H) x = a.v + t * a.v_stride + (long long)(c - a.q_heads - a.c.H) * kD;
+        w[j] = u[j] = make_uint4(0, 0, 0, 0);
+        if (x) {
+            w[j] = *(const uint4 *)(x + 8 * i);
+            if (a.half && !a.neighbours && c < a.q_heads + a.c.H) u[j] = *(const uint4 *)(x + 8 * other);
+        }
+    }
+    // The request of each of the four tokens: the number of requests that end at or before it, 64 starts looked at in a trip.
+    int owner[4] = {0, 0, 0, 0}, step = 1;
+    while ((long long)step * 64 < n) step *= 64;
+    for (; step; step /= 64) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const long long e = owner[k] + (long long)(lane + 1) * step;
+            const bool before = e <= n && a.query_start[e] <= t0 + k;
+            owner[k] += (int)__popcll(__ballot(before)) * step;
+        }
+    }
+    const int s = r == 0 ? owner[0] : r == 1 ? owner[1] : r == 2 ? owner[2] : owner[3];
+    const bool real = t0 + r < a.n_tokens && s < n;
+    const int s_safe = min(s, n - 1);
+    const int end = min(max(a.query_start[s_safe + 1], 0), a.n_tokens), len = max(a.seq_len[s_safe], 0);
+    const int source = a.source ? a.source[s_safe] : -1;
+    const long long place = (long long)len - end + t;
+    const long long position = place + ((unsigned)source < (unsigned)n && source != s ? max(a.seq_len[(unsigned)source < (unsigned)n ? source : 0], 0) : 0);
+    const bool known = real && (!a.half || (position >= 0 && position < a.n_positions));
+    const int tokens_shift = a.c.tile_shift + 4;
+    const bool in_row = known && place >= 0 && place < (long long)a.max_blocks << tokens_shift;
+    const int block = in_row ? a.table[(size_t)s_safe * a.max_blocks + (size_t)(place >> tokens_shift)] : -1;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        cs[e] = 1.f;
+        sn[e] = 0.f;
+    }
+    if (a.half && known && turned) {
+        const float *row = a.rope + position * (2 * a.half) + (a.neighbours ? 4 * i : 8 * (first ? i : i - pair_lanes));
+        const float4 c0 = *(const float4 *)row, s0 = *(const float4 *)(row + a.half);
+        cs[0] = c0.x, cs[1] = c0.y, cs[2] = c0.z, cs[3] = c0.w;
+        sn[0] = s0.x, sn[1] = s0.y, sn[2] = s0.z, sn[3] = s0.w;
+        if (!a.neighbours) {
+            const float4 c1 = *(const float4 *)(row + 4), s1 = *(const float4 *)(row + a.half + 4);
+            cs[4] = c1.x, cs[5] = c1.y, cs[6] = c1.z, cs[7] = c1.w;
+            sn[4] = s1.x, sn[5] = s1.y, sn[6] = s1.z, sn[7] = s1.w;
+        }
+    }
+    const bool held = in_row && block >= 0 && block < a.c.n_blocks;
+    const int at = (int)place & ((16 << a.c.tile_shift) - 1), row = at & 15;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+#pragma clang fp contract(off)
+        const int c = head0 + j;
+        if (c >= a.q_heads + 2 * a.c.H) break;
+        float f[8];
+        widen8(w[j], f);
+        if (a.half && turned && c < a.q_heads + a.c.H) {
+            if (a.neighbours) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = f[2 * e], y = f[2 * e + 1];
+                    const float xc = x * cs[e], ys = y * sn[e], xs = x * sn[e], yc = y * cs[e];
+                    f[2 * e] = xc - ys;
+                    f[2 * e + 1] = xs + yc;
+                }
+            } else {
+                float o[8];
+                widen8(u[j], o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float mine = f[e] * cs[e], theirs = o[e] * sn[e];
+                    f[e] = first ? mine - theirs : theirs + mine;
+                }
+            }
+        }
+        if (c < a.q_heads) {
+            if (known)
+                *(uint4 *)(a.q_out + t * a.q_out_stride + (long long)c * kD + 8 * i) =
+                    make_uint4(round2(f[0], f[1]), round2(f[2], f[3]), round2(f[4], f[5]), round2(f[6], f[7]));
+            continue;
+        }
+        const int side = c >= a.q_heads + a.c.H ? 1 : 0, h = c - a.q_heads - side * a.c.H;
+        int scale;
+        const uint32_t code = hold(f, scale);
+        if (!held) continue;
+        uint8_t *tile = a.c.data + ((((size_t)block * a.c.H + h) << a.c.tile_shift) + (at >> 4)) * kCacheTileBytes;
+        *(uint32_t *)(tile + kCacheV * side + 64 * row + 4 * i) = code;
+        if ((i & 3) == 0) tile[kCacheKS + 64 * side + cache_scale_byte(row, i >> 2)] = (uint8_t)scale;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------------------------ read
 // A wave takes 16 consecutive positions of one (request, KV head), keys or values; 16 lanes to a row.  Bound by the writes.
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheDims c, int n_requests, const int *seq_len, const int *table, int max_blocks,
@@ -291,6 +434,18 @@ void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, lo
                         int n_tokens, hipStream_t stream) {
     const long long units = ((long long)n_tokens + 15) / 16 * c.H * 2;
     cache_write_kernel<<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(c, k, v, k_stride, v_stride, slots, n_tokens);
+}
+
+void launch_cache_append(const CacheAppend &a, hipStream_t stream) {
+    const int heads = a.q_heads + 2 * a.c.H;
+    const long long quads = ((long long)a.n_tokens + 3) / 4;
+    if (quads * heads <= 8192) {
+        cache_append_kernel<1><<<(unsigned)((quads * heads + 3) / 4), 256, 0, stream>>>(a, heads);
+        return;
+    }
+    constexpr int kPer = 4;
+    const int chunks = (heads + kPer - 1) / kPer;
+    cache_append_kernel<kPer><<<(unsigned)((quads * chunks + 3) / 4), 256, 0, stream>>>(a, chunks);
 }
 
 void launch_cache_read(const CacheDims &c, int n_requests, const int *seq_len, const int *table, int max_blocks, const int *first,

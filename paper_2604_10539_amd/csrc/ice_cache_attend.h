@@ -1,4 +1,5 @@
-// Attention over the 4-bit sequence cache.
+// Attention over the 4-bit sequence cache: its kernels, and their launches by form.
+#pragma once
 #include <algorithm>
 #include <array>
 #include <type_traits>
@@ -20,6 +21,7 @@ constexpr int kQuantum = kWaves * kStep;
 constexpr int kRows = 16;      // columns of a tile of query rows
 constexpr int kRecord = 132;   // floats per row of a partial result: 128 sums, maximum, denominator
 constexpr int kEntries = 1024; // requests of one launch at most
+constexpr int kFar = 0x7FFFFFF0; // positions of gathered queries end here
 constexpr float kNoMax = -3.402823466e38f;  // maximum of a row that has seen no key: below every finite score
 constexpr float kSlack = 8.f;  // a row's reference may lie this far (in powers of two) below its maximum before sums are rescaled
 
@@ -40,10 +42,19 @@ __device__ inline uint32_t pack2(float a, float b) {
 __device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }
 __device__ inline float cut(float v, uint32_t mask) { return v - __uint_as_float(__float_as_uint(v) & mask); }
 
-// A request's query rows and the keys they see; for listed tokens, those of one KV head.
-template <bool LIST>
+// What a launch computes.  Causal: a step's queries over their requests' tokens.  Listed: one query of a request over listed tokens.
+// Cross: the queries of all requests that name a source, a row of the table, over all of its tokens; an entry of the launch is a row of the table and
+// its queries are gathered through the sorted list (ice_plan_sources).  Own and Join are the halves of attention behind a shared source: Own is Causal
+// with its rows' sums left in a.state, Join is Cross whose rows then take these sums along and become outputs.
+enum Form { kCausal, kListed, kCross, kOwn, kJoin };
+constexpr bool gathered(int form) { return form == kCross || form == kJoin; }
+
+// A request's query rows and the keys they see; for listed tokens, those of one KV head; for gathered queries, those of a source.
+template <int FORM>
 struct Unit {
-    int row0, n_query, first;  // first query row, queries, the position behind the first one's own (listed: entries of the list)
+    static constexpr bool LIST = FORM == kListed;
+    int row0, n_query, first;  // first query row, queries, the position behind the first one's own (listed: entries of the list; gathered: the
+                             // position behind the lowest one's own)
     int tokens;              // the length, or what the table has room for if that is less: the queries' positions follow the length all the same
     // t: the request's length; x, y: its entry of query_start and the next one, or x the length of its list.
     __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y) { set(a, s, t, x, y); }
@@ -61,9 +72,13 @@ struct Unit {
         } else {
             asm volatile("" : "+v"(t), "+v"(x), "+v"(y));
         }
-        set(a, s, t, x, y);
+        set(a, s, t, x, y, FORM == kJoin && a.window > 0 ? a.lowest[s] : 0);
     }
-    __host__ __device__ void set(const CacheAttend &a, int s, int t, int x, int y) {
+    // A gathered query's position: its place behind the source's tokens.
+    static __host__ __device__ int position(int length, int place) {
+        return (int)min(max((long long)max(length, 0) + place, -1ll), (long long)kFar);
+    }
+    __host__ __device__ void set(const CacheAttend &a, int s, int t, int x, int y, int lowest = 0) {
         tokens = (int)min((long long)max(t, 0), (long long)a.max_blocks << (a.c.tile_shift + 4));
         if constexpr (LIST) {
             row0 = s;
@@ -72,13 +87,17 @@ struct Unit {
         } else {
             row0 = min(max(x, 0), a.T);
             n_query = min(max(y, row0), a.T) - row0;
-            first = (int)((unsigned)max(t, 0) - (unsigned)n_query + 1u);  // (of a request without queries it may wrap)
+            if constexpr (gathered(FORM)) first = position(t, lowest) + 1;
+            else first = (int)((unsigned)max(t, 0) - (unsigned)n_query + 1u);  // (of a request without queries it may wrap)
         }
     }
     __host__ __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
     // Keys [low, high) that query t sees; sees_from and sees_to: the same for who keeps to keys that some query sees.
-    __host__ __device__ int sees_to(int t) const { return LIST ? first : first + t; }
-    __host__ __device__ int sees_from(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? max(first + t, 0) - a.window : 0; }
+    // (of gathered queries every one may see all tokens but those that the lowest one's window leaves out)
+    __host__ __device__ int sees_to(int t) const { return LIST ? first : gathered(FORM) ? tokens : first + t; }
+    __host__ __device__ int sees_from(const CacheAttend &a, int t) const {
+        return !LIST && FORM != kCross && a.window > 0 ? max(first + (gathered(FORM) ? 0 : t), 0) - a.window : 0;
+    }
     __host__ __device__ int high(int t) const { return LIST ? first : min(max(sees_to(t), 0), tokens); }
     __host__ __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? min(max(sees_from(a, t), 0), tokens) : 0; }
 };
@@ -107,13 +126,68 @@ struct PartKeys {
 // The partial result that a part of a unit that was cut leaves: two a workgroup, of a unit that began before it and of one that goes on behind it.
 __host__ __device__ inline unsigned record_of(unsigned workgroup, bool began_before) { return 2 * workgroup + (began_before ? 0 : 1); }
 
+// Two sums of a row, relative to 2^top and 2^m, become one.
+__device__ inline void join_sums(f32x4 &sum, float &top, float &total, const f32x4 &v, float m, float l) {
+    const float mn = fmaxf(top, m), f0 = __builtin_amdgcn_exp2f(top - mn), f1 = __builtin_amdgcn_exp2f(m - mn);
+    sum = sum * f0 + v * f1;
+    total = total * f0 + l * f1;
+    top = mn;
+}
 // Writes four dims of a row from its sums relative to 2^top, and the logarithm of its denominator.
+template <int FORM>
 __device__ inline void put_row(const CacheAttend &a, size_t row, int d0, f32x4 sum, float top, float total) {
+    if constexpr (FORM == kOwn || FORM == kJoin) {
+        float *r = a.state + row * kRecord;
+        if constexpr (FORM == kOwn) {
+            *(f32x4 *)(r + d0) = sum;
+            if (d0 == 0) *(float2 *)(r + kD) = make_float2(top, total);
+            return;
+        }
+        const float2 ml = *(const float2 *)(r + kD);
+        join_sums(sum, top, total, *(const f32x4 *)(r + d0), ml.x, ml.y);
+    }
     const bool none = total == 0.f;  // no key at all: the largest of any weights is 2^-kSlack or more
     sum = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total);
     if (a.out_bf16) *(uint2 *)((bf16_t *)a.out + row * kD + d0) = make_uint2(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]));
     else *(f32x4 *)((float *)a.out + row * kD + d0) = sum;
     if (a.lse && d0 == 0) a.lse[row] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+}
+
+// The token whose query is row `row` of a unit that begins at `row0` of the step's queries, or of the sorted list: -1 where the list names none.
+template <int FORM> __device__ inline int token_of(const CacheAttend &a, int row0, int row) {
+    if constexpr (!gathered(FORM)) return row0 + row / a.G;
+    const int t = a.token[row0 + row / a.G];
+    return (unsigned)t < (unsigned)a.T ? t : -1;
+}
+template <int FORM> __device__ inline const bf16_t *query_at(const CacheAttend &a, int token, int h, int row) {
+    return a.q + (long long)(gathered(FORM) ? max(token, 0) : token) * a.q_stride + (long long)(h * a.G + row % a.G) * kD;
+}
+// alone: of Own, the request has no source, its sums are its output.
+template <int FORM>
+__device__ inline void put_query(const CacheAttend &a, int token, int h, int row, int d0, const f32x4 &sum, float top, float total, bool alone) {
+    if (gathered(FORM) && token < 0) return;
+    const size_t at = (size_t)token * a.c.H * a.G + h * a.G + row % a.G;
+    if (FORM == kOwn && alone) put_row<kCausal>(a, at, d0, sum, top, total);
+    else put_row<FORM>(a, at, d0, sum, top, total);
+}
+// What counts as a source: a row of the table, not the request's own.
+template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, int s) {
+    if constexpr (FORM != kOwn) return false;
+    const int to = __builtin_amdgcn_readfirstlane(a.source[s]);
+    return (unsigned)to >= (unsigned)a.S || to == s;
+}
+// Keys [low, high) of the part [from, to) that row `row` of the unit sees.
+template <int FORM>
+__device__ inline void sees(const CacheAttend &a, const Unit<FORM> &u, int length, int row, int from, int to, int &low, int &high) {
+    const int t = row / a.G;
+    if constexpr (FORM == kJoin) {
+        const int behind = Unit<FORM>::position(length, a.place[u.row0 + t]) + 1;
+        low = a.window > 0 ? max(behind - a.window, from) : from;
+        high = min(behind, to);
+    } else {
+        low = max(u.sees_from(a, t), from);
+        high = min(u.sees_to(t), to);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------------------- few queries
@@ -230,6 +304,20 @@ __device__ inline void find_nan(const CacheAttend &a, const int *table, int h, i
     }
 }
 
+// Queries whose requests have no source see nothing: 0 and -inf.
+__device__ inline void clear_unsourced(const CacheAttend &a) {
+    const int from = min(max(a.query_start[a.S], 0), a.T), to = min(max(a.query_start[a.S + 1], 0), a.T), heads = a.c.H * a.G;
+    for (int e = from + (int)blockIdx.x; e < to; e += (int)gridDim.x) {
+        const int t = a.token[e];
+        if ((unsigned)t >= (unsigned)a.T) continue;
+        for (int i = threadIdx.x; i < heads * (kD / 4); i += (int)blockDim.x) {
+            const size_t row = (size_t)t * heads + i / (kD / 4);
+            const int d0 = 4 * (i % (kD / 4));
+            put_row<kCross>(a, row, d0, f32x4{0.f, 0.f, 0.f, 0.f}, kNoMax, 0.f);
+        }
+    }
+}
+
 // Attention of few query rows (queries times heads of a group: at most 16 NT) of every request over its keys.
 //
 // S^T = K Q^T puts a row's scores on one lane (g, c): column c, tokens 4 i + g of each tile; these registers are the
@@ -251,8 +339,9 @@ __device__ inline void find_nan(const CacheAttend &a, const int *table, int h, i
 // Bound by the vector unit (busy 61 %) and HBM together where there is much to read: one token of 16 requests of up to 32 K tokens, 8 KV heads,
 // 68 us with the merge, 5.3 TB/s; about 220 vector instructions beside 16 products for 32 keys.  Else by its trips: one request of
 // 4 K tokens 10 us.  Five drafted tokens of 32 requests, 40 rows, a window of 4096: 55 us, 23 of them products.  Lists of 1024 for 128 units 13.5.
-template <int W, int PACK, int NT, int SETS, bool LIST>
+template <int W, int PACK, int NT, int SETS, int FORM>
 __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
+    constexpr bool LIST = FORM == kListed;
     static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
     constexpr int R = kRows / PACK;  // rows in a tile of columns
     constexpr int Q = W * kStep;     // keys of a step of all waves
@@ -276,7 +365,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             const int e = e0 + tid;
             unsigned n = 0;
             if (e < a.n_here) {
-                const Unit<LIST> u(a, a.first + e, 0, std::false_type());
+                const Unit<FORM> u(a, a.first + e, 0, std::false_type());
                 n = (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
             }
             const unsigned incl = (unsigned)wave_scan_add((int)n);
@@ -294,13 +383,15 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         if (tid == 0) s_before[a.n_here] = total;
         __syncthreads();
     }
+    if constexpr (FORM == kCross)
+        if (a.first == 0) clear_unsourced(a);
     const Pieces pieces(__builtin_amdgcn_readfirstlane(total), gridDim.x, a.whole);
     if (blockIdx.x >= pieces.groups || total == 0) {
         if (tid == 0 && a.notes) a.notes[blockIdx.x].first = -1;
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    MergeNote note = {-1, 0, 0, 0, 0};
+    MergeNote note = {-1, 0, 0, 0, 0, 0};
     int entry = 0;
     if (!even) {  // the last request that begins at or before the piece (of those, the one that is not empty)
         for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
@@ -331,7 +422,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         s = __builtin_amdgcn_readfirstlane(s) + a.first;
         h = __builtin_amdgcn_readfirstlane(h);
         const unsigned stop = min(u1, end);
-        const Unit<LIST> unit(a, s, h, std::true_type());
+        const Unit<FORM> unit(a, s, h, std::true_type());
+        const bool alone = is_alone<FORM>(a, s);
         const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
         if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
             now = stop;
@@ -341,17 +433,32 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         const int q0 = unit.low(a, 0) / Q;
         const PartKeys keys(a, unit, 0, t_last, Q, u0, u1, now, stop);
         const int from = keys.from, to = keys.to;
-        const int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
+        int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
         int low[NT], high[NT];
         u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-            const int row = min(R * x + col_row, n_rows - 1), t = row / a.G;
-            low[x] = max(unit.sees_from(a, t), from);
-            high[x] = min(unit.sees_to(t), to);
-            const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
+            const int row = min(R * x + col_row, n_rows - 1);
+            sees<FORM>(a, unit, FORM == kJoin ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+            const bf16_t *p = query_at<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row) + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
+        }
+        if constexpr (FORM == kJoin) {  // (a source's queries stand in no order)
+            all_low = low[0];
+            all_high = high[0];
+#pragma unroll
+            for (int x = 1; x < NT; ++x) {
+                all_low = max(all_low, low[x]);
+                all_high = min(all_high, high[x]);
+            }
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) {
+                all_low = max(all_low, __shfl_xor(all_low, d));
+                all_high = min(all_high, __shfl_xor(all_high, d));
+            }
+            all_low = __builtin_amdgcn_readfirstlane(all_low);
+            all_high = __builtin_amdgcn_readfirstlane(all_high);
         }
         const int step0 = (q0 + (int)(now - u0)) * W;  // the wave's steps: step0 + wave + W n
         const int n_mine = to > from ? max((to - kStep * (step0 + wave) + Q - 1) / Q, 0) : 0;
@@ -667,7 +774,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                     const int in = in0 + 2 * W * pass, row = R * x + in;
                     if (in >= R || row >= n_rows) continue;
                     if (whole) {
-                        put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum[pass], top[pass], all[pass]);
+                        put_query<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row, d0, sum[pass], top[pass], all[pass], alone);
                     } else {
                         float *r = record + (size_t)row * kRecord;
                         *(f32x4 *)(r + d0) = sum[pass];
@@ -680,7 +787,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             }
             __syncthreads();
         }
-        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows};
+        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows, alone};
         now = stop;
     }
     if (tid == 0 && a.notes) a.notes[blockIdx.x] = note;
@@ -714,13 +821,19 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
     template <typename U> __host__ __device__ static int quanta(const CacheAttend &a, const U &u, int n_rows, int tile) {
         return quanta_of(a, u, kChunkRows * tile / a.G, (min(kChunkRows * (tile + 1), n_rows) - 1) / a.G, kQuantum);
     }
-    template <typename U> __host__ __device__ Chunks(const CacheAttend &a, const U &u) {
+    template <int FORM> __host__ __device__ Chunks(const CacheAttend &a, const Unit<FORM> &u) {
         n_rows = u.queries(a) * a.G;
         tiles = 0;
         pair = single = per_head = 0;
         if (n_rows <= kRows) return;  // (the few-query kernel's, which takes that many where there are requests with more than kFewRows)
         tiles = (n_rows + kChunkRows - 1) / kChunkRows;
         const int middle = quanta(a, u, n_rows, (tiles - 1) / 2);
+        if (gathered(FORM)) {  // all row tiles take the same keys
+            pair = 2 * (unsigned)middle;
+            single = (unsigned)middle;
+            per_head = (unsigned)tiles * single;
+            return;
+        }
         // An estimate for the pairs: with as many keys as queries the tiles' quanta are a line, or with a window concave, and twice the middle covers any
         // pair.  It is no bound: tiles of queries in front of the first key see nothing, and then a pair's first tile alone may need more.
         // So a pair's second tile gets what the first one leaves of it, and that is one quantum at least (see at()); what a unit needs beyond its nominal length its last
@@ -743,7 +856,7 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
     }
 };
 
-template <int SETS>
+template <int SETS, int FORM>
 __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend a) {
     __shared__ u32x4 s_k[2][kWaves][4][64], s_v[2][kRound / kStep][8][64];
     __shared__ unsigned s_before[kEntries + 1], s_wave[kWaves];
@@ -752,7 +865,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     unsigned total = 0;
     for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
         const int e = e0 + tid;
-        const unsigned n = e < a.n_here ? Chunks(a, Unit<false>(a, a.first + e, 0, std::false_type())).per_head * (unsigned)a.c.H : 0u;
+        const unsigned n = e < a.n_here ? Chunks(a, Unit<FORM>(a, a.first + e, 0, std::false_type())).per_head * (unsigned)a.c.H : 0u;
         const unsigned incl = (unsigned)wave_scan_add((int)n);
         if (lane == 63) s_wave[wave] = incl;
         __syncthreads();
@@ -773,7 +886,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    MergeNote note = {-1, 0, 0, 0, 0};
+    MergeNote note = {-1, 0, 0, 0, 0, 0};
     int entry = 0;
     for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
         if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
@@ -785,7 +898,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     for (unsigned now = begin; now < end;) {
         while (s_before[entry + 1] <= now) ++entry;
         const int s = __builtin_amdgcn_readfirstlane(entry) + a.first;
-        const Unit<false> unit(a, s, 0, std::true_type());
+        const Unit<FORM> unit(a, s, 0, std::true_type());
+        const bool alone = is_alone<FORM>(a, s);
         const Chunks ch(a, unit);
         const unsigned first = s_before[entry];
         const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
@@ -797,7 +911,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const int q0 = unit.low(a, t_first) / kQuantum + (int)(now - u0);
         const PartKeys keys(a, unit, t_first, t_last, kQuantum, u0, u1, now, stop);
         const int from = keys.from, to = keys.to;
-        const int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(t_first), to);
+        int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(t_first), to);
+        if (FORM == kJoin) {  // (a source's queries stand in no order: not every one need see these keys)
+            all_low = to;
+            all_high = from;
+        }
         const int key_at = q0 * kQuantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
         // this lane's rows: columns of tiles wave + 4 x
@@ -805,10 +923,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         u32x4 qv[kTiles][4];
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
-            const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1), t = row / a.G;
-            low[x] = max(unit.sees_from(a, t), from);
-            high[x] = min(unit.sees_to(t), to);
-            const bf16_t *p = a.q + (long long)(unit.row0 + t) * a.q_stride + (long long)(h * a.G + row % a.G) * kD + 32 * g;
+            const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1);
+            sees<FORM>(a, unit, FORM == kJoin ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+            const bf16_t *p = query_at<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row) + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
@@ -816,6 +933,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             const int r0 = min(kRows * wave, n_rows - 1), r1 = min(kRows * (kWaves * (kTiles - 1) + wave) + kRows - 1, n_rows - 1);
             wave_low = max(unit.sees_from(a, (base + r1) / a.G), from);
             wave_high = min(unit.sees_to((base + r0) / a.G), to);
+        }
+        if constexpr (FORM == kJoin) {
+            wave_low = max(max(low[0], low[1]), low[2]);
+            wave_high = min(min(high[0], high[1]), high[2]);
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) {
+                wave_low = max(wave_low, __shfl_xor(wave_low, d));
+                wave_high = min(wave_high, __shfl_xor(wave_high, d));
+            }
+            wave_low = __builtin_amdgcn_readfirstlane(wave_low);
+            wave_high = __builtin_amdgcn_readfirstlane(wave_high);
         }
         const int *table = a.table + (size_t)s * a.max_blocks;
         auto places = [&](int n0) __attribute__((always_inline)) -> int {  // this wave's tile of round n0 + l
@@ -1036,7 +1164,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 for (int half = 0; half < 2; ++half) {
                     const int d0 = 32 * g + 8 * i + 4 * half;
                     const f32x4 sum = {acc[x][4 * half][i], acc[x][4 * half + 1][i], acc[x][4 * half + 2][i], acc[x][4 * half + 3][i]};
-                    if (whole) put_row(a, (size_t)(unit.row0 + row / a.G) * a.c.H * a.G + h * a.G + row % a.G, d0, sum, m[x], l[x]);
+                    if (whole) put_query<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row, d0, sum, m[x], l[x], alone);
                     else *(f32x4 *)(record + (size_t)in * kRecord + d0) = sum;
                 }
             if (!whole && g == 0) {
@@ -1044,7 +1172,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 record[(size_t)in * kRecord + kD + 1] = l[x];
             }
         }
-        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, base, all_rows};
+        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, base, all_rows, alone};
         now = stop;
     }
     if (tid == 0) a.notes[blockIdx.x] = note;
@@ -1054,7 +1182,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
 // those behind it up to this one (their first parts).  Groups of 32 threads take a row, four dims each; GROUPS of them share a row's records.
 // Bound by two round trips to memory: the note, the records.
 constexpr int kMergeThreads = 256;
-template <int GROUPS>
+template <int GROUPS, int FORM>
 __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend a) {
     __shared__ float s_sum[kMergeThreads / 32][kRecord];
     const MergeNote note = a.notes[blockIdx.x];
@@ -1065,12 +1193,7 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend 
     const bool mine = in < a.rows && row < note.rows;
     float top = kNoMax, total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    auto join = [&](float m, float l, const f32x4 &v) {
-        const float mn = fmaxf(top, m), f0 = __builtin_amdgcn_exp2f(top - mn), f1 = __builtin_amdgcn_exp2f(m - mn);
-        sum = sum * f0 + v * f1;
-        total = total * f0 + l * f1;
-        top = mn;
-    };
+    auto join = [&](float m, float l, const f32x4 &v) { join_sums(sum, top, total, v, m, l); };
     if (mine) {
         constexpr int kAtOnce = 4;
         for (int k = group; k < n; k += GROUPS * kAtOnce) {
@@ -1101,63 +1224,31 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend 
 #pragma unroll
         for (int w = 1; w < GROUPS; ++w) join(s_sum[all + w][kD], s_sum[all + w][kD + 1], *(const f32x4 *)(s_sum[all + w] + d0));
     }
-    if (mine) put_row(a, (size_t)(note.row0 + row / a.G) * a.c.H * a.G + note.h * a.G + row % a.G, d0, sum, top, total);
+    if (mine) put_query<FORM>(a, token_of<FORM>(a, note.row0, row), note.h, row, d0, sum, top, total, note.alone);
 }
-
-}  // namespace
 
 // Query rows of the launch for few: all of them up to kFewRows, else the requests' with at most 16, and a launch of the many-query
 // kernel serves the others.  768 or (more than 16 rows) 512 workgroups of the first are resident at a time, 512 of the second; there are no
 // more of them than quanta.
 constexpr int kFewRows = 48;
-static int few_rows(const CacheAttend &a) {
+inline int few_rows(const CacheAttend &a) {
     const long long rows = (long long)a.max_query * a.G;
     return rows <= 5 ? 5 : rows <= 8 ? 8 : rows <= 16 || rows > kFewRows ? 16 : rows <= 32 ? 32 : 48;
 }
 // ... and those of a unit of the many-query kernel: a record has room for what a request can have (single tokens of 16 requests whose most queries are not
 // known, 64 rows: 35 MB for 512 workgroups instead of 104).
-static int chunk_rows(const CacheAttend &a) { return (int)std::min<long long>(kChunkRows, (long long)a.max_query * a.G); }
-static size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(MergeNote)); }
+inline int chunk_rows(const CacheAttend &a) { return (int)std::min<long long>(kChunkRows, (long long)a.max_query * a.G); }
+inline size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * rows * kRecord * 4 + sizeof(MergeNote)); }
 
-// Units (request, KV head) that stay whole, one workgroup each, no merge behind it: short ones, where the merge costs more than the cut gains, longer
-// ones too where they are many, and lists of as many units as there are CUs.  Cut and whole, us: dense, 8 units of 512 keys 9.4 and 7.9, of
-// 1024 9.3 and 11.3; 128 units of up to 1024 keys 14.6 and 11.9, of up to 4096 22 and 32; 512 units of up to 2048 keys 30 and 27, of up to 4096 44
-// and 43.  Lists, 8 units of 512 tokens 8.9 and 8.0, of 1024 9.5 and 11.0; 128 units of 1024 15.9 and 14.1, of 2048 22 and 26; 256 units of 2048
-// 36.7 and 34.8, of 4096 62 and 60.
 constexpr int kListWaves = 8;
-static int whole_keys(long long units) { return units >= 512 ? 2048 : units >= 128 ? 1024 : 512; }
-
-size_t plan_cache_attend(CacheAttend &a, bool listed) {
-    const long long units = (long long)std::min(a.S, kEntries) * a.c.H;
-    const int rows = few_rows(a);
-    a.many = (long long)a.max_query * a.G > kFewRows;
-    a.many_groups = 0;
-    if (listed) {
-        const int quantum = kListWaves * kStep;
-        a.per_unit = (a.max_keys + quantum - 1) / quantum;
-        a.whole = a.max_keys <= whole_keys(units) || units >= 256;
-        a.few_groups = (int)(a.whole ? units : std::min<long long>(256, units * a.per_unit));
-        return a.whole ? 0 : attend_bytes(a.few_groups, rows);
-    }
-    a.whole = a.max_keys <= whole_keys(units) && !a.many;
-    a.per_unit = a.whole ? 1 : 0;
-    if (a.whole) {
-        a.few_groups = (int)units;
-        return 0;
-    }
-    const long long quanta = ((long long)a.max_keys + kQuantum - 1) / kQuantum * units;
-    a.few_groups = (int)std::min<long long>(rows > 16 ? 512 : 768, quanta);
-    const long long tiles = ((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows;
-    if (a.many) a.many_groups = (int)std::min<long long>(512, quanta * tiles);
-    return std::max(attend_bytes(a.few_groups, rows), attend_bytes(a.many_groups, chunk_rows(a)));
-}
 
 // The launches of a call, workgroup by workgroup as the kernels take their pieces, from the lengths on the host.
-template <bool LIST, typename F> static void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
+template <int FORM, typename F> inline void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
+    constexpr bool LIST = FORM == kListed;
     const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = few_rows(a);
     const bool even = LIST || a.per_unit > 0;
     const auto unit = [&](int s, int h) {
-        return LIST ? Unit<LIST>(a, s, 1 << 30, len[s * a.c.H + h], 0) : Unit<LIST>(a, s, len[s], start[s], start[s + 1]);
+        return LIST ? Unit<FORM>(a, s, 1 << 30, len[s * a.c.H + h], 0) : Unit<FORM>(a, s, len[s], start[s], start[s + 1]);
     };
     unsigned before[kEntries + 1] = {0};  // quanta before each request
     for (int e = 0; e < a.n_here; ++e)
@@ -1181,8 +1272,8 @@ template <bool LIST, typename F> static void cut_few(const CacheAttend &a, const
                  cut ? (int)record_of(i, now > u0) : -1, now > u0 && stop == u1 ? (int)pieces.owner(u0) : -1});
         }
 }
-template <typename F> static void cut_many(const CacheAttend &a, const int *start, const int *len, F put) {
-    const auto unit = [&](int s) { return Unit<false>(a, s, len[s], start[s], start[s + 1]); };
+template <int FORM, typename F> inline void cut_many(const CacheAttend &a, const int *start, const int *len, F put) {
+    const auto unit = [&](int s) { return Unit<FORM>(a, s, len[s], start[s], start[s + 1]); };
     unsigned before[kEntries + 1] = {0};
     for (int e = 0; e < a.n_here; ++e) before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, unit(a.first + e)).per_head;
     const Pieces pieces(before[a.n_here], a.many_groups, false);
@@ -1202,7 +1293,7 @@ template <typename F> static void cut_many(const CacheAttend &a, const int *star
                  cut ? (int)record_of(i, now > p.u0) : -1, now > p.u0 && stop == p.u1 ? (int)pieces.owner(p.u0) : -1});
         }
 }
-long long cut_cache_attend(CacheAttend a, bool listed, const int *start, const int *len, int *parts, long long most) {
+template <int FORM> inline long long cut_attend(CacheAttend a, const int *start, const int *len, int *parts, long long most) {
     long long n = 0;
     const auto put = [&](const std::array<int, kCutInts> &part) {
         if (n < most) std::copy(part.begin(), part.end(), parts + n * kCutInts);
@@ -1210,52 +1301,56 @@ long long cut_cache_attend(CacheAttend a, bool listed, const int *start, const i
     };
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
         a.n_here = std::min(a.S - a.first, kEntries);
-        if (listed) cut_few<true>(a, start, len, put);
-        else cut_few<false>(a, start, len, put);
-        if (a.many) cut_many(a, start, len, put);
+        cut_few<FORM>(a, start, len, put);
+        if constexpr (FORM != kListed)
+            if (a.many) cut_many<FORM>(a, start, len, put);
     }
     return n;
 }
 
-template <int W, bool LIST>
-static void launch_few(const CacheAttend &a, hipStream_t stream) {
+template <int W, int FORM>
+inline void launch_few(const CacheAttend &a, hipStream_t stream) {
     const dim3 grid(a.whole ? a.n_here * a.c.H : a.few_groups), block(W * 64);
-    if (a.rows == 5) cache_attend_kernel<W, 3, 1, 1, LIST><<<grid, block, 0, stream>>>(a);
-    else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<W, 2, 1, 1, LIST><<<grid, block, 0, stream>>>(a);
-    else if (a.rows == 8) cache_attend_kernel<W, 2, 1, 2, LIST><<<grid, block, 0, stream>>>(a);
-    else if (a.rows == 16 && a.out_bf16) cache_attend_kernel<W, 1, 1, 2, LIST><<<grid, block, 0, stream>>>(a);
-    else if (a.rows == 16) cache_attend_kernel<W, 1, 1, 3, LIST><<<grid, block, 0, stream>>>(a);
-    else if constexpr (!LIST) {
-        if (a.rows == 32 && a.out_bf16) cache_attend_kernel<W, 1, 2, 1, LIST><<<grid, block, 0, stream>>>(a);
-        else if (a.rows == 32) cache_attend_kernel<W, 1, 2, 3, LIST><<<grid, block, 0, stream>>>(a);
-        else if (a.out_bf16) cache_attend_kernel<W, 1, 3, 1, LIST><<<grid, block, 0, stream>>>(a);
-        else cache_attend_kernel<W, 1, 3, 3, LIST><<<grid, block, 0, stream>>>(a);
+    if (a.rows == 5) cache_attend_kernel<W, 3, 1, 1, FORM><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<W, 2, 1, 1, FORM><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 8) cache_attend_kernel<W, 2, 1, 2, FORM><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 16 && a.out_bf16) cache_attend_kernel<W, 1, 1, 2, FORM><<<grid, block, 0, stream>>>(a);
+    else if (a.rows == 16) cache_attend_kernel<W, 1, 1, 3, FORM><<<grid, block, 0, stream>>>(a);
+    else if constexpr (FORM != kListed) {
+        if (a.rows == 32 && a.out_bf16) cache_attend_kernel<W, 1, 2, 1, FORM><<<grid, block, 0, stream>>>(a);
+        else if (a.rows == 32) cache_attend_kernel<W, 1, 2, 3, FORM><<<grid, block, 0, stream>>>(a);
+        else if (a.out_bf16) cache_attend_kernel<W, 1, 3, 1, FORM><<<grid, block, 0, stream>>>(a);
+        else cache_attend_kernel<W, 1, 3, 3, FORM><<<grid, block, 0, stream>>>(a);
     }
     if (a.whole) return;
     // threads for four records of a unit at a time: one trip for most
     const int rows = std::min(a.rows, a.max_query * a.G), per_unit = a.few_groups / std::max(1, a.n_here * a.c.H) + 2;
-    if (per_unit <= 4) cache_merge_kernel<1><<<dim3(a.few_groups, (rows + 7) / 8), kMergeThreads, 0, stream>>>(a);
-    else if (per_unit <= 8) cache_merge_kernel<2><<<dim3(a.few_groups, (rows + 3) / 4), kMergeThreads, 0, stream>>>(a);
-    else cache_merge_kernel<8><<<dim3(a.few_groups, rows), kMergeThreads, 0, stream>>>(a);
+    if (per_unit <= 4) cache_merge_kernel<1, FORM><<<dim3(a.few_groups, (rows + 7) / 8), kMergeThreads, 0, stream>>>(a);
+    else if (per_unit <= 8) cache_merge_kernel<2, FORM><<<dim3(a.few_groups, (rows + 3) / 4), kMergeThreads, 0, stream>>>(a);
+    else cache_merge_kernel<8, FORM><<<dim3(a.few_groups, rows), kMergeThreads, 0, stream>>>(a);
 }
 
-void launch_cache_attend(CacheAttend a, hipStream_t stream) {
+template <int FORM>
+inline void launch_attend(CacheAttend a, hipStream_t stream) {
     float *const part = a.part;
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
         a.n_here = std::min(a.S - a.first, kEntries);
         a.rows = few_rows(a);
         a.notes = a.whole ? nullptr : (MergeNote *)part;
         a.part = a.whole ? nullptr : (float *)(a.notes + a.few_groups);
-        if (a.pos) launch_few<kListWaves, true>(a, stream);
-        else launch_few<kWaves, false>(a, stream);
-        if (!a.many) continue;
-        a.rows = chunk_rows(a);
-        a.notes = (MergeNote *)part;
-        a.part = (float *)(a.notes + a.many_groups);
-        if (a.out_bf16) cache_chunk_kernel<1><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
-        else cache_chunk_kernel<3><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
-        cache_merge_kernel<1><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
+        launch_few<FORM == kListed ? kListWaves : kWaves, FORM>(a, stream);
+        if constexpr (FORM != kListed) {
+            if (!a.many) continue;
+            a.rows = chunk_rows(a);
+            a.notes = (MergeNote *)part;
+            a.part = (float *)(a.notes + a.many_groups);
+            if (a.out_bf16) cache_chunk_kernel<1, FORM><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
+            else cache_chunk_kernel<3, FORM><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
+            cache_merge_kernel<1, FORM><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
+        }
     }
 }
+
+}  // namespace
 
 }  // namespace ice

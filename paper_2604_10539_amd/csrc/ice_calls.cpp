@@ -28,6 +28,12 @@ struct {
     decltype(&ice_cache_attend) attend;
     decltype(&ice_cache_attend_tokens_bytes) tokens_bytes;
     decltype(&ice_cache_attend_tokens) tokens;
+    decltype(&ice_plan_sources) plan_sources;
+    decltype(&ice_cache_append) append;
+    decltype(&ice_cache_attend_cross_bytes) cross_bytes;
+    decltype(&ice_cache_attend_cross) cross;
+    decltype(&ice_cache_attend_shared_bytes) shared_bytes;
+    decltype(&ice_cache_attend_shared) shared;
 } lib = {};
 PyObject *ice_error = nullptr;
 
@@ -304,11 +310,140 @@ PyObject *call_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (stream, source, query_start, seq_len or None, plan, n_rows, n_tokens)
+PyObject *call_plan_sources(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> PyObject * {
+        void *stream = PyLong_AsVoidPtr(a[0]);
+        if (PyErr_Occurred()) throw Refused();
+        const int n_rows = int32_of(a[5], "n_rows"), n_tokens = int32_of(a[6], "n_tokens");
+        const Tensor &source = tensor(a[1], "source");
+        const int64_t requests = source.numel();
+        if (requests > INT32_MAX) refuse_shape("source: too many requests");
+        static const char *const names[4] = {"source", "query_start", "seq_len", "plan"};
+        const int64_t sizes[4] = {requests, requests + 1, requests, 2 * (int64_t)n_rows + 2 + 2 * (int64_t)n_tokens};
+        int32_t *p[4];
+        for (int i = 0; i < 4; ++i) {
+            p[i] = nullptr;
+            if (i == 2 && a[3] == Py_None) continue;
+            const Tensor &t = tensor(a[1 + i], names[i]);
+            if (!(t.scalar_type() == at::kInt && t.numel() == sizes[i] && t.is_contiguous() && t.device() == source.device()))
+                refuse_shape("%s: contiguous int32 of %lld entries on source's device", names[i], (long long)sizes[i]);
+            p[i] = t.data_ptr<int32_t>();
+        }
+        if (!source.is_cuda()) refuse(ICE_ERR_INVALID_ARG, "the arrays must be on a GPU");
+        check(lib.plan_sources((int)requests, n_rows, n_tokens, p[0], p[1], p[2], p[3], stream));
+        Py_RETURN_NONE;
+    });
+}
+
+// (desc, device, stream, k, v, query_start, seq_len, table, q or None, out or None, rope or None, neighbours, source or None)
+PyObject *call_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> PyObject * {
+        const Cache c(a);
+        const Tensor &k = tensor(a[3], "k"), &v = tensor(a[4], "v");
+        int64_t ks = 0, vs = 0, qs = 0, os = 0;
+        const void *kp = c.rows(k, "k", &ks), *vp = c.rows(v, "v", &vs), *qp = nullptr;
+        if (k.sizes() != v.sizes() || k.size(1) != c.c->n_kv_heads || k.size(0) > INT32_MAX) refuse_shape("k and v: [tokens, %d, 128]", c.c->n_kv_heads);
+        const int tokens = (int)k.size(0);
+        const Cache::Table t = c.table(a[6], a[7]);
+        const int32_t *start = c.ints(tensor(a[5], "query_start"), "query_start", {(int64_t)t.n + 1});
+        const int32_t *source = a[12] == Py_None ? nullptr : c.ints(tensor(a[12], "source"), "source", {t.n});
+        const float *rope = nullptr;
+        int positions = 0, rotated = 0, heads = 0;
+        if (a[10] != Py_None) {
+            const Tensor &r = tensor(a[10], "rope");
+            if (!(r.scalar_type() == at::kFloat && r.dim() == 2 && r.is_contiguous() && c.here(r) && r.size(0) <= INT32_MAX && r.size(1) <= 128))
+                refuse_shape("rope: contiguous float32 [positions, up to 128] on the cache's device");
+            rope = r.const_data_ptr<float>();
+            positions = (int)r.size(0);
+            rotated = (int)r.size(1);
+        }
+        Tensor out;
+        void *op = nullptr;
+        if (a[8] == Py_None) {
+            if (a[9] != Py_None) refuse_shape("out: only with q");
+        } else {
+            const Tensor &q = tensor(a[8], "q");
+            qp = c.rows(q, "q", &qs);
+            if (q.size(0) != tokens || q.size(1) < 1 || q.size(1) > 65536) refuse_shape("q: [%d, heads, 128]", tokens);
+            heads = (int)q.size(1);
+            if (a[9] == Py_None) out = at::empty(q.sizes(), c.options(q.scalar_type()));
+            else out = tensor(a[9], "out");
+            op = const_cast<void *>(c.rows(out, "out", &os));
+            if (out.sizes() != q.sizes()) refuse_shape("out: q's shape");
+        }
+        check(lib.append(c.c, qp, qs, heads, op, os, kp, vp, ks, vs, tokens, t.n, start, t.seq_len, source, t.table, t.width, rope, positions, rotated,
+                         a[11] == Py_True, c.stream));
+        if (a[8] == Py_None) Py_RETURN_NONE;
+        if (a[9] == Py_None) return THPVariable_Wrap(out);
+        Py_INCREF(a[9]);
+        return a[9];
+    });
+}
+
+// The sorted list of a step's queries, for a table of `rows` rows and the rows of q.
+const int32_t *list_of(const Cache &c, PyObject *plan, int64_t rows, int64_t tokens) {
+    return c.ints(tensor(plan, "plan"), "plan", {2 * rows + 2 + 2 * tokens});
+}
+// What the host knows of the most queries, or None: `most` then; never more than that.
+int most_of(PyObject *o, const char *name, int most) {
+    const int v = o == Py_None ? most : int32_of(o, name);
+    return v > most ? most : v;
+}
+int longest_of(PyObject *o, const char *name, int64_t cap) { return o == Py_None ? (int)std::min<int64_t>(cap, 1 << 30) : int32_of(o, name); }
+
+// (desc, device, stream, q, plan, seq_len, table, max_shared or None, max_len or None, out or None, bf16, lse or None, with_lse)
+PyObject *call_attend_cross(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> PyObject * {
+        const Cache c(a);
+        const Tensor &q = tensor(a[3], "q");
+        int64_t stride = 0;
+        const void *qp = c.rows(q, "q", &stride);
+        const int group = group_of(c, q), tokens = (int)q.size(0);
+        const Cache::Table t = c.table(a[5], a[6]);
+        const int32_t *plan = list_of(c, a[4], t.n, tokens);
+        const int most = most_of(a[7], "max_shared", tokens), longest = longest_of(a[8], "max_len", (int64_t)t.width * c.c->block_size);
+        const Outputs o(c, q, a[9], a[10] == Py_True, a[11], a[12] == Py_True);
+        if (tokens) {
+            const Scratch w(c, lib.cross_bytes(c.c, group, t.n, most, longest));
+            check(lib.cross(c.c, qp, stride, group, t.n, plan, tokens, most, t.seq_len, longest, t.table, t.width, o.out.data_ptr(), o.kind, o.lse_ptr(), w.ptr(),
+                            w.bytes, c.stream));
+        }
+        return o.result(a[9], a[11]);
+    });
+}
+
+// (desc, device, stream, q, query_start, source, plan, seq_len, table, max_query, max_shared, max_len, max_source (or None each), window, out or None, bf16,
+// lse or None, with_lse)
+PyObject *call_attend_shared(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 18, [&]() -> PyObject * {
+        const Cache c(a);
+        const Tensor &q = tensor(a[3], "q");
+        int64_t stride = 0;
+        const void *qp = c.rows(q, "q", &stride);
+        const int group = group_of(c, q), tokens = (int)q.size(0), window = int32_of(a[13], "window");
+        const Cache::Table t = c.table(a[7], a[8]);
+        const int32_t *start = c.ints(tensor(a[4], "query_start"), "query_start", {(int64_t)t.n + 1}), *source = c.ints(tensor(a[5], "source"), "source", {t.n});
+        const int32_t *plan = list_of(c, a[6], t.n, tokens);
+        const int64_t cap = (int64_t)t.width * c.c->block_size;
+        const int most = most_of(a[9], "max_query", tokens), shared = most_of(a[10], "max_shared", tokens);
+        const int longest = longest_of(a[11], "max_len", cap), longest_source = longest_of(a[12], "max_source", cap);
+        const Outputs o(c, q, a[14], a[15] == Py_True, a[16], a[17] == Py_True);
+        if (tokens) {
+            const Scratch w(c, lib.shared_bytes(c.c, group, t.n, tokens, most, shared, longest, longest_source));
+            check(lib.shared(c.c, qp, stride, group, t.n, start, source, plan, tokens, most, shared, t.seq_len, longest, longest_source, t.table, t.width, window,
+                             o.out.data_ptr(), o.kind, o.lse_ptr(), w.ptr(), w.bytes, c.stream));
+        }
+        return o.result(a[14], a[16]);
+    });
+}
+
 // (IceError, addresses of the entry points in the order of `lib`)
 PyObject *call_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 9, [&]() -> PyObject * {
-        void *p[8];
-        for (int i = 0; i < 8; ++i) p[i] = PyLong_AsVoidPtr(a[1 + i]);
+    constexpr int kEntries = 14;
+    return guarded(n, 1 + kEntries, [&]() -> PyObject * {
+        void *p[kEntries];
+        for (int i = 0; i < kEntries; ++i) p[i] = PyLong_AsVoidPtr(a[1 + i]);
         if (PyErr_Occurred()) throw Refused();
         Py_INCREF(a[0]);
         Py_XDECREF(ice_error);
@@ -321,13 +456,20 @@ PyObject *call_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
         lib.attend = reinterpret_cast<decltype(lib.attend)>(p[5]);
         lib.tokens_bytes = reinterpret_cast<decltype(lib.tokens_bytes)>(p[6]);
         lib.tokens = reinterpret_cast<decltype(lib.tokens)>(p[7]);
+        lib.plan_sources = reinterpret_cast<decltype(lib.plan_sources)>(p[8]);
+        lib.append = reinterpret_cast<decltype(lib.append)>(p[9]);
+        lib.cross_bytes = reinterpret_cast<decltype(lib.cross_bytes)>(p[10]);
+        lib.cross = reinterpret_cast<decltype(lib.cross)>(p[11]);
+        lib.shared_bytes = reinterpret_cast<decltype(lib.shared_bytes)>(p[12]);
+        lib.shared = reinterpret_cast<decltype(lib.shared)>(p[13]);
         Py_RETURN_NONE;
     });
 }
 
 #define ICE_METHOD(name) {#name, (PyCFunction)(void (*)(void))call_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ICE_METHOD(attend), ICE_METHOD(attend_tokens), ICE_METHOD(write), ICE_METHOD(read),
-                         ICE_METHOD(plan),   ICE_METHOD(bind),          {nullptr, nullptr, 0, nullptr}};
+                         ICE_METHOD(plan),   ICE_METHOD(plan_sources),  ICE_METHOD(append), ICE_METHOD(attend_cross),
+                         ICE_METHOD(attend_shared), ICE_METHOD(bind),   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

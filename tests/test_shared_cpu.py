@@ -1,0 +1,146 @@
+"""Sources of the 4-bit cache without a GPU: how attention to them cuts its work, and what the calls refuse."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_cache4_cpu import FAKE, status
+from tests.test_cache4_cut_cpu import CHUNK, FEW, check_units
+
+
+def check(heads, group, lens, counts, max_shared=None, max_keys=None, block=16, width=None):
+    """counts: queries (tokens) of each source."""
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(None, 1, heads, block)
+    start = np.concatenate([[0], np.cumsum(counts), [sum(counts) + 3]])
+    most = max(max(counts), 1) if max_shared is None else max_shared
+    width = width or max(1, -(-max(lens) // block))
+    keys = max(1, max(lens)) if max_keys is None else max_keys
+    parts = b.ice_debug_cross_cut(c, group, len(lens), start, int(start[-1]), most, lens, keys, width)
+    nbytes = p.ice_cache_attend_cross_bytes(c, group, len(lens), most, keys)
+    rows_most = most * group
+    room = next(r for r in (5, 8, 16, 32, FEW, 1 << 30) if rows_most <= r)
+    few = 16 if rows_most > FEW else room
+    expected = {}
+    for s, (length, n) in enumerate(zip(lens, counts)):
+        rows = min(n, most) * group
+        many = rows_most > FEW and rows > 16
+        for base in range(0, rows, CHUNK if many else 1 << 30):
+            expected[int(many), s, base] = (min(rows - base, CHUNK) if many else rows, 0, min(length, width * block))
+    check_units(dict(zip(b.CUT_FIELDS, parts.T)), nbytes, heads, expected, (few, min(CHUNK, rows_most)))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_sources_of_any_shape(seed):
+    rng = np.random.default_rng([seed, 5])
+    for _ in range(50):
+        rows, group = int(rng.choice([1, 2, 7, 40, 130])), int(rng.choice([1, 2, 3, 4, 7, 8, 16]))
+        top = 2500 if rng.random() < 0.5 else max(1, FEW // group)
+        counts = [int(np.exp(rng.uniform(0, np.log(top)))) if rng.random() < 0.6 else 0 for _ in range(rows)]
+        lens = [int(np.exp(rng.uniform(0, np.log(100000 // rows + 2)))) - 1 for _ in range(rows)]
+        most = None if rng.random() < 0.7 else int(rng.integers(1, max(counts) + 2))
+        width = None if rng.random() < 0.8 else max(1, max(lens) // 40)
+        check(int(rng.choice([1, 2, 8])), group, lens, counts, most, None if rng.random() < 0.5 else int(rng.integers(1, 9000)), width=width)
+
+
+def test_one_source_among_many_rows_and_more_rows_than_a_launch_takes():
+    check(8, 4, [32768] + [900] * 32, [32] + [0] * 32, block=64)
+    check(2, 4, [300] * 1030, [3] * 1030)
+    check(1, 2, [300] * 2100, [0, 40, 0] * 700)
+
+
+def test_the_measured_cases():
+    from perf import more_operators
+    for case in more_operators.listed():
+        if case["kind"] not in ("cross", "shared"):
+            continue
+        source, _, gain, lengths = more_operators._batch(case)
+        counts = [0] * len(lengths)
+        for s, g in zip(source, gain):
+            if s >= 0:
+                counts[s] += g
+        check(case["heads"], case["group"], lengths, counts, block=case["block"])
+
+
+def test_the_hook_refuses():
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c, e = p.make_cache_desc(None, 1, 2, 16), np.zeros(4, np.int32)
+    for change in (dict(n_rows=0), dict(n_rows=8193), dict(n_tokens=-1), dict(max_shared=0), dict(max_keys=0), dict(max_blocks=0), dict(max_blocks=2 ** 27)):
+        args = dict(cache=c, group_size=4, n_rows=1, start=e, n_tokens=1, max_shared=1, length=e, max_keys=16, max_blocks=1)
+        assert status(b.ice_debug_cross_cut, **{**args, **change}) == b.ICE_ERR_SHAPE, change
+
+
+# ------------------------------------------------------------------------------------------------------------- what is refused
+def test_sorting_refuses():
+    from paper_2604_10539_amd import binding as b
+    good = dict(n=4, rows=4, tokens=10, source=FAKE, start=FAKE, seq_len=FAKE, plan=FAKE)
+
+    def call(**change):
+        return b.lib().ice_plan_sources(*{**good, **change}.values(), None)
+    for name in ("source", "start", "plan"):
+        assert call(**{name: None}) == b.ICE_ERR_INVALID_ARG
+    for change in (dict(n=0), dict(n=8193), dict(rows=0), dict(rows=8193), dict(tokens=-1), dict(tokens=2 ** 30 + 1)):
+        assert call(**change) == b.ICE_ERR_SHAPE, change
+
+
+def test_appending_refuses():
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(FAKE, 10, 2, 16)
+    good = dict(q=FAKE, qs=1024, qh=8, out=FAKE, os=1024, k=FAKE, v=FAKE, ks=256, vs=256, tokens=4, n=2, start=FAKE, sl=FAKE, source=FAKE, table=FAKE, mb=4,
+                rope=FAKE, positions=100, rotated=128, neighbours=0)
+    go = lambda **change: status(p.ice_cache_append, c, *{**good, **change}.values())  # noqa: E731
+    for name in ("out", "k", "v", "start", "sl", "table", "rope"):
+        assert go(**{name: None}) == b.ICE_ERR_INVALID_ARG, name
+    for name in ("q", "out", "k", "v", "rope"):
+        assert go(**{name: FAKE + 8}) == b.ICE_ERR_INVALID_ARG, name
+    for change in (dict(qs=1028), dict(qs=1016), dict(os=1028), dict(os=1016), dict(ks=252), dict(ks=248), dict(vs=260), dict(vs=0), dict(tokens=-1), dict(n=0),
+                   dict(n=65536), dict(mb=0), dict(mb=2 ** 27), dict(positions=0), dict(qh=0)):
+        assert go(**change) == b.ICE_ERR_SHAPE, change
+    for rotated in (0, 8, 24, 144, -16):
+        assert go(rotated=rotated) == b.ICE_ERR_UNSUPPORTED
+    assert go(neighbours=2) == b.ICE_ERR_INVALID_ARG
+    assert go(tokens=2 ** 30) == b.ICE_ERR_UNSUPPORTED
+    p.ice_cache_append(c, *{**good, "tokens": 0, "k": None, "v": None, "out": None}.values())  # nothing to do
+    assert b.lib().ice_cache_append(None, *good.values(), None) == b.ICE_ERR_INVALID_ARG
+
+
+def test_attention_to_sources_refuses():
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(FAKE, 1000, 2, 16)
+    cross = dict(q=FAKE, qs=1024, G=4, rows=2, plan=FAKE, tokens=2, shared=1, sl=FAKE, keys=4096, table=FAKE, mb=256, out=FAKE, ot=0, lse=None, ws=FAKE, wb=1 << 30)
+    both = dict(q=FAKE, qs=1024, G=4, n=2, start=FAKE, source=FAKE, plan=FAKE, tokens=2, query=1, shared=2, sl=FAKE, keys=64, source_keys=4096, table=FAKE, mb=256,
+                window=0, out=FAKE, ot=0, lse=None, ws=FAKE, wb=1 << 30)
+    need = {p.ice_cache_attend_cross: p.ice_cache_attend_cross_bytes(c, 4, 2, 1, 4096),
+            p.ice_cache_attend_shared: p.ice_cache_attend_shared_bytes(c, 4, 2, 2, 1, 2, 64, 4096)}
+    assert need[p.ice_cache_attend_shared] > 2 * 8 * 528  # (every row's sums, and scratch)
+    for call, good, count in ((p.ice_cache_attend_cross, cross, "rows"), (p.ice_cache_attend_shared, both, "n")):
+        go = lambda **change: status(call, c, *{**good, **change}.values())  # noqa: E731, B023
+        for name in [x for x in ("q", "start", "source", "plan", "sl", "table", "out", "ws") if x in good]:
+            assert go(**{name: None}) == b.ICE_ERR_INVALID_ARG, name
+        for change in (dict(q=FAKE + 8), dict(out=FAKE + 8), dict(ws=FAKE + 8), dict(ot=2)):
+            assert go(**change) == b.ICE_ERR_INVALID_ARG
+        for name, values in ((count, (0, 8193)), ("tokens", (-1,)), ("shared", (0, 2 ** 24 + 1)), ("keys", (0, 2 ** 30 + 1)), ("mb", (0, 2 ** 27)), ("qs", (1020, 1016)),
+                             ("query", (0, 2 ** 24 + 1)), ("source_keys", (0,)), ("window", (-1,))):
+            for v in values if name in good else ():
+                assert go(**{name: v}) == b.ICE_ERR_SHAPE, (name, v)
+        for G in (0, -1, 17):
+            assert go(G=G) == b.ICE_ERR_UNSUPPORTED
+        assert go(wb=need[call] - 1) == b.ICE_ERR_CAPACITY and "workspace" in p.ice_last_error()
+        assert go(**{count: 8192, "shared": 2 ** 24}) == b.ICE_ERR_UNSUPPORTED
+        call(c, *{**good, "tokens": 0}.values())
+    for args in ((c, 17, 2, 1, 4096), (c, 4, 0, 1, 4096), (c, 4, 8193, 1, 4096), (c, 4, 2, 0, 4096)):
+        assert p.ice_cache_attend_cross_bytes(*args) == 0
+    assert p.ice_cache_attend_shared_bytes(c, 4, 2, -1, 1, 2, 64, 4096) == 0 and p.ice_cache_attend_shared_bytes(c, 4, 8193, 2, 1, 2, 64, 4096) == 0
+
+
+def test_sorting_takes_arrays_on_a_gpu_only():
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    e = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    args = [e(2), e(3), e(2), e(2 * 2 + 2 + 2 * 5), 2, 5]
+    assert status(p.ice_plan_sources, *args) == b.ICE_ERR_INVALID_ARG
+    for i, bad in ((0, e(3)), (1, e(2)), (2, e(1)), (3, e(15)), (0, torch.zeros(2)), (1, None), (3, torch.zeros(32, dtype=torch.int32)[::2])):
+        assert status(p.ice_plan_sources, *[bad if j == i else x for j, x in enumerate(args)]) == b.ICE_ERR_SHAPE, i
