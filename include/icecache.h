@@ -426,8 +426,8 @@ ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_toke
  *   plan: as ice_plan_sources wrote it for the same n_rows and n_tokens, and query_start and source of this step.
  *   seq_len [n_rows], block_table [n_rows][max_blocks]: those of the sources.  max_keys: about the longest of them, a hint.
  *   max_shared: no source has more queries (tokens; those beyond are left out), in [1, 2^24].
- *   q, out, out_type, lse, Precision: as for ice_cache_attend, with max_shared in the place of max_query, and a source's queries in the place of a
- *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
+ *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with max_shared in the place of max_query and a source's queries in the place of a
+ *     request's; where max_shared * group_size is above 48, a bf16 output's weights are rounded to bf16 once whatever its source's queries are.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
  *   workspace: ice_cache_attend_cross_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
  * SHAPE for n_rows > 8192; UNSUPPORTED as for ice_cache_attend. */
 size_t ice_cache_attend_cross_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, int32_t max_shared, int32_t max_keys);
@@ -443,10 +443,10 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int
  *   source, plan: as given to and written by ice_plan_sources for this step, n_rows = n_requests, with seq_len.
  *   max_query, max_keys: of the requests' own queries and tokens, as for ice_cache_attend; max_shared: no source has more queries (tokens of all its requests;
  *     those beyond are left out, their outputs as they were), in [1, 2^24]; max_source_keys: about the longest source, a hint.
- *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there; a bf16 output's weights on its own tokens follow max_query, those on the source
- *     max_shared.
- *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 528 for every row of out, and scratch.
- * SHAPE for n_requests > 8192; UNSUPPORTED as for ice_cache_attend. */
+ *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as for ice_cache_attend_cross, with the larger of max_query and max_shared.
+ *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 1056 for every row of out, and scratch.
+ * SHAPE for n_requests > 8192; UNSUPPORTED where (tokens of a table row / 128 + 3) * ((max_query + max_shared) / (192 / group_size) + 4) * 2 * n_requests *
+ * n_kv_heads, or n_tokens * n_kv_heads, reaches 2^31. */
 size_t ice_cache_attend_shared_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t n_tokens, int32_t max_query,
                                      int32_t max_shared, int32_t max_keys, int32_t max_source_keys);
 ice_status_t ice_cache_attend_shared(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,
@@ -511,10 +511,15 @@ ice_status_t ice_debug_cache_cut(const ice_cache_t *cache, int32_t group_size, i
                                  int32_t max_query, const int32_t *len, int32_t max_keys, int32_t max_blocks, int32_t window, int32_t *parts,
                                  int64_t max_parts, int64_t *n_parts);
 
-/* Test hook: ice_debug_cache_cut for ice_cache_attend_cross (and the sources' half of ice_cache_attend_shared without a window).  start: the list's start
- * [n_rows + 2], seq_len [n_rows], HOST arrays; a part's request is its source, its first row counts the source's queries. */
+/* Test hooks: ice_debug_cache_cut for ice_cache_attend_cross and ice_cache_attend_shared, all arrays on the HOST.  Cross: start, the list's [n_rows + 2]; a part's
+ * request is its source, its first row counts the source's queries.  Shared: query_start [n_requests + 1] and the whole plan; the parts of sources 0 ..
+ * n_requests - 1 come first, then those of requests, numbered from n_requests on; notes are by query there, so a part's last word says what its first workgroup is. */
 ice_status_t ice_debug_cross_cut(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, const int32_t *start, int32_t n_tokens, int32_t max_shared,
                                  const int32_t *seq_len, int32_t max_keys, int32_t max_blocks, int32_t *parts, int64_t max_parts, int64_t *n_parts);
+
+ice_status_t ice_debug_shared_cut(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, const int32_t *query_start, const int32_t *plan, int32_t n_tokens,
+                                  int32_t max_query, int32_t max_shared, const int32_t *seq_len, int32_t max_keys, int32_t max_source_keys, int32_t max_blocks,
+                                  int32_t window, int32_t *parts, int64_t max_parts, int64_t *n_parts);
 
 /* Test hook for the failure path of ice_select / ice_select_attend when a unit is served by several
  * workgroups (fewer than 256 units): those workgroups hand their page scores to the last one of

@@ -24,7 +24,7 @@ SYMBOLS = ["ice_workspace_bytes", "ice_create", "ice_destroy", "ice_build_index"
            "ice_cache_bytes", "ice_plan_blocks", "ice_cache_write", "ice_cache_read", "ice_cache_attend_bytes", "ice_cache_attend",
            "ice_cache_attend_tokens", "ice_cache_attend_tokens_bytes", "ice_debug_cache_cut",
            "ice_plan_sources", "ice_cache_append", "ice_cache_attend_cross_bytes", "ice_cache_attend_cross", "ice_cache_attend_shared_bytes",
-           "ice_cache_attend_shared", "ice_debug_cross_cut"]
+           "ice_cache_attend_shared", "ice_debug_cross_cut", "ice_debug_shared_cut"]
 
 
 class IceConfig(C.Structure):
@@ -137,6 +137,7 @@ def lib() -> C.CDLL:
         L.ice_cache_attend_shared_bytes.argtypes = [desc] + [i32] * 7
         L.ice_cache_attend_shared.argtypes = [desc, ptr, i64, i32, i32, ptr, ptr, ptr, i32, i32, i32, ptr, i32, i32, ptr, i32, i32, ptr, i32, ptr, ptr,
                                               C.c_size_t, ptr]
+        L.ice_debug_shared_cut.argtypes = [desc, i32, i32, ptr, ptr, i32, i32, i32, ptr, i32, i32, i32, i32, ptr, i64, C.POINTER(C.c_int64)]
         L.ice_debug_cross_cut.argtypes = [desc, i32, i32, ptr, i32, i32, ptr, i32, i32, ptr, i64, C.POINTER(C.c_int64)]
         for name in SYMBOLS:
             if name not in ("ice_last_error", "ice_cache_attend_cross_bytes", "ice_cache_attend_shared_bytes", "ice_workspace_bytes", "ice_cache_bytes", "ice_cache_attend_bytes",
@@ -706,6 +707,21 @@ def ice_debug_cross_cut(cache: IceCacheDesc, group_size, n_rows, start, n_tokens
     while True:
         _check(lib().ice_debug_cross_cut(C.byref(cache), group_size, n_rows, start.ctypes.data, n_tokens, max_shared, length.ctypes.data, max_keys, max_blocks,
                                          parts.ctypes.data, len(parts), C.byref(n)))
+        if n.value <= len(parts):
+            return parts[: n.value]
+        parts = np.empty((n.value, len(CUT_FIELDS)), dtype=np.int32)
+
+
+def ice_debug_shared_cut(cache: IceCacheDesc, group_size, n_requests, query_start, plan, n_tokens, max_query, max_shared, length, max_keys, max_source_keys,
+                         max_blocks, window=0):
+    """numpy arrays on the host, int32 -> the parts, int32 [n, 15] in the order of CUT_FIELDS."""
+    import numpy as np
+    start, plan, length = (np.ascontiguousarray(x, dtype=np.int32) for x in (query_start, plan, length))
+    n = C.c_int64(0)
+    parts = np.empty((1 << 12, len(CUT_FIELDS)), dtype=np.int32)
+    while True:
+        _check(lib().ice_debug_shared_cut(C.byref(cache), group_size, n_requests, start.ctypes.data, plan.ctypes.data, n_tokens, max_query, max_shared,
+                                          length.ctypes.data, max_keys, max_source_keys, max_blocks, window, parts.ctypes.data, len(parts), C.byref(n)))
         if n.value <= len(parts):
             return parts[: n.value]
         parts = np.empty((n.value, len(CUT_FIELDS)), dtype=np.int32)

@@ -641,7 +641,7 @@ static ice_status_t check_rows(int32_t n_rows) {
 
 // where a list's parts lie (ice_plan_sources)
 static void set_list(CacheAttend &a, const int32_t *plan) {
-    a.query_start = plan;
+    a.list_start = plan;
     a.lowest = plan + a.S + 2;
     a.token = plan + 2 * (size_t)a.S + 2;
     a.place = a.token + a.T;
@@ -668,6 +668,7 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *c, const void *q, int64_t
     if (n_tokens == 0) return ICE_OK;
     a.T = n_tokens;
     set_list(a, plan);
+    a.query_start = plan;
     a.seq_len = seq_len;
     a.table = table;
     a.max_blocks = max_blocks;
@@ -676,24 +677,34 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *c, const void *q, int64_t
     return device_status("ice_cache_attend_cross");
 }
 
-// the two halves of a call, and what it needs: the rows' sums, and behind them the scratch that the halves use one after the other
 static ice_status_t plan_shared(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t n_tokens, int32_t max_query, int32_t max_shared,
-                                int32_t max_keys, int32_t max_source_keys, CacheAttend &own, CacheAttend &join, size_t *bytes) {
+                                int32_t max_keys, int32_t max_source_keys, CacheAttend &a, size_t *bytes) {
     if (ice_status_t st = check_rows(n_requests)) return st;
     if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_tokens %d is outside [0, 2^30]", n_tokens);
-    size_t first = 0, second = 0;
-    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, false, own, &first)) return st;
-    if (ice_status_t st = plan_attend(c, G, n_requests, max_shared, max_source_keys, false, join, &second)) return st;
-    own.T = join.T = n_tokens;
-    *bytes = cache_state_bytes(own) + std::max(first, second);
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_shared, max_source_keys, false, a, bytes)) return st;  // (its checks of these two)
+    if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, false, a, bytes)) return st;
+    if ((double)n_tokens * c->n_kv_heads >= 2147483648.0) return fail(ICE_ERR_UNSUPPORTED, "%d tokens for %d KV heads: too many for one call", n_tokens, c->n_kv_heads);
+    a.T = n_tokens;
+    a.max_shared = max_shared;
+    a.whole = false;
+    *bytes = plan_cache_shared(a, max_source_keys);
+    return ICE_OK;
+}
+
+// (both sides' quanta are counted together, all requests in one launch)
+static ice_status_t check_shared_count(const ice_cache_t *c, const CacheAttend &a) {
+    const double keys = (double)a.max_blocks * c->block_size / 128 + 3, tile = 192 / a.G;
+    if (keys * (a.max_query / tile + a.max_shared / tile + 4) * 2 * a.S * c->n_kv_heads >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %d blocks x %d and %d queries: too many for one call", a.S, c->n_kv_heads, a.max_blocks,
+                    a.max_query, a.max_shared);
     return ICE_OK;
 }
 
 size_t ice_cache_attend_shared_bytes(const ice_cache_t *c, int32_t G, int32_t n_requests, int32_t n_tokens, int32_t max_query, int32_t max_shared,
                                      int32_t max_keys, int32_t max_source_keys) {
-    CacheAttend own{}, join{};
+    CacheAttend a{};
     size_t bytes = 0;
-    return plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, own, join, &bytes) == ICE_OK ? bytes : 0;
+    return plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, a, &bytes) == ICE_OK ? bytes : 0;
 }
 
 ice_status_t ice_cache_attend_shared(const ice_cache_t *c, const void *q, int64_t q_stride, int32_t G, int32_t n_requests, const int32_t *query_start,
@@ -705,26 +716,41 @@ ice_status_t ice_cache_attend_shared(const ice_cache_t *c, const void *q, int64_
     if (ice_status_t st = check_table(c, n_requests, seq_len, table, max_blocks)) return st;
     if (!query_start || !source || !plan) return fail(ICE_ERR_INVALID_ARG, "query_start, source or plan is null");
     if (window < 0) return fail(ICE_ERR_SHAPE, "window must be >= 0 (0: no window)");
-    CacheAttend own{}, join{};
+    CacheAttend a{};
     size_t need = 0;
-    if (ice_status_t st = plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, own, join, &need)) return st;
+    if (ice_status_t st = plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, a, &need)) return st;
     if (n_tokens == 0) return ICE_OK;
-    for (CacheAttend *a : {&own, &join}) {
-        a->seq_len = seq_len;
-        a->table = table;
-        a->max_blocks = max_blocks;
-        a->window = window;
-        a->source = source;
-    }
-    own.query_start = query_start;
-    set_list(join, plan);
-    for (CacheAttend *a : {&own, &join}) {
-        if (ice_status_t st = set_attend(c, *a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
-        a->state = static_cast<float *>(ws);
-        a->part = a->state + cache_state_bytes(own) / sizeof(float);
-    }
-    launch_cache_shared(own, join, static_cast<hipStream_t>(stream));
+    a.seq_len = seq_len;
+    a.table = table;
+    a.max_blocks = max_blocks;
+    a.window = window;
+    a.source = source;
+    a.query_start = query_start;
+    set_list(a, plan);
+    if (ice_status_t st = check_shared_count(c, a)) return st;
+    if (ice_status_t st = set_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
+    launch_cache_shared(a, ws, static_cast<hipStream_t>(stream));
     return device_status("ice_cache_attend_shared");
+}
+
+ice_status_t ice_debug_shared_cut(const ice_cache_t *c, int32_t G, int32_t n_requests, const int32_t *query_start, const int32_t *plan, int32_t n_tokens,
+                                  int32_t max_query, int32_t max_shared, const int32_t *seq_len, int32_t max_keys, int32_t max_source_keys, int32_t max_blocks,
+                                  int32_t window, int32_t *parts, int64_t max_parts, int64_t *n_parts) {
+    if (ice_status_t st = check_cache(c)) return st;
+    if (!query_start || !plan || !seq_len || !parts || !n_parts) return fail(ICE_ERR_INVALID_ARG, "a pointer is null");
+    if (max_blocks < 1 || (long long)max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: at least 1, at most 2^30 tokens", max_blocks);
+    if (window < 0 || max_parts < 0) return fail(ICE_ERR_SHAPE, "window and max_parts must be >= 0");
+    CacheAttend a{};
+    size_t need = 0;
+    if (ice_status_t st = plan_shared(c, G, n_requests, n_tokens, max_query, max_shared, max_keys, max_source_keys, a, &need)) return st;
+    a.max_blocks = max_blocks;
+    a.window = window;
+    a.seq_len = seq_len;
+    a.query_start = query_start;
+    set_list(a, plan);
+    if (ice_status_t st = check_shared_count(c, a)) return st;
+    *n_parts = cut_cache_shared(a, parts, max_parts);
+    return ICE_OK;
 }
 
 ice_status_t ice_debug_cross_cut(const ice_cache_t *c, int32_t G, int32_t n_rows, const int32_t *start, int32_t n_tokens, int32_t max_shared,

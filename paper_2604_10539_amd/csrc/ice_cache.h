@@ -38,9 +38,14 @@ void launch_cache_read(const CacheDims &c, int n_requests, const int *seq_len, c
                        int n_rows, bf16_t *k, bf16_t *v, hipStream_t stream);
 
 // A (request, KV head) that was cut between workgroups: the first one of them, the KV head, the request's first query row, the first of the
-// unit's rows and the number of the request's rows (query, head of the group); of Own, whether the request has no source.
+// unit's rows and the number of the request's rows (query, head of the group).
 struct alignas(16) MergeNote {
-    int first, h, row0, base, rows, alone;
+    int first, h, row0, base, rows;
+};
+// Where a query's sums over one side's tokens are, of a KV head: the first workgroup of the records and their number, the query's first row in them; or a whole
+// unit's state (first < 0).
+struct alignas(16) TokenNote {
+    int first, count, row, flags;
 };
 
 struct CacheAttend {
@@ -61,22 +66,28 @@ struct CacheAttend {
     int first, n_here;  // the launch's requests
     float scale_log2;
     bool out_bf16;
-    // of queries that are gathered by source (ice_plan_sources): the sorted list's tokens and places, each source's lowest place; the requests' sources;
-    // the sums of the queries over their own tokens, a record each
-    const int *token, *place, *lowest, *source;
+    // of queries that are gathered by source (ice_plan_sources): the sorted list's tokens
+    const int *token;
+    // of attention behind a source: the list's starts, places and each source's lowest place, the requests' sources; the sums of whole units, a record for each row
+    // over its own tokens and one over its source's; notes likewise; workgroups, and the most queries of a source
+    const int *list_start, *place, *lowest, *source;
     float *state;
+    TokenNote *token_notes;
+    int groups, max_shared;
 };
 // How a call is cut, from the sizes: fills few_groups, many_groups, many, per_unit and whole; returns the bytes of workspace.
 size_t plan_cache_attend(CacheAttend &a, bool listed);
 void launch_cache_attend(CacheAttend a, hipStream_t stream);
 void launch_cache_cross(const CacheAttend &a, hipStream_t stream);
-void launch_cache_shared(const CacheAttend &own, const CacheAttend &join, hipStream_t stream);
+// ... and of attention behind a source, whose longest has about max_source tokens: fills rows, many and groups; returns the bytes of workspace.
+size_t plan_cache_shared(CacheAttend &a, int max_source);
+void launch_cache_shared(CacheAttend a, void *workspace, hipStream_t stream);
 // The parts that the workgroups of a planned call take, from lengths on the host (query_start and seq_len, or n_tok): their number, the first `most` of
 // them in parts, kCutInts words each (see ice_debug_cache_cut).
 constexpr int kCutInts = 15;
 long long cut_cache_attend(CacheAttend a, bool listed, const int *query_start, const int *len, int *parts, long long most);
 long long cut_cache_cross(CacheAttend a, const int *start, const int *len, int *parts, long long most);
-size_t cache_state_bytes(const CacheAttend &a);
+long long cut_cache_shared(const CacheAttend &a, int *parts, long long most);  // (a's arrays on the host)
 
 // The queries of a step sorted by the row of the table that their requests name.
 struct CacheSources {

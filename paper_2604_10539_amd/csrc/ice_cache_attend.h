@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <array>
 #include <type_traits>
+#include <vector>
 
 #include "ice_cache.h"
 
@@ -23,6 +24,7 @@ constexpr int kRecord = 132;   // floats per row of a partial result: 128 sums, 
 constexpr int kEntries = 1024; // requests of one launch at most
 constexpr int kFar = 0x7FFFFFF0; // positions of gathered queries end here
 constexpr float kNoMax = -3.402823466e38f;  // maximum of a row that has seen no key: below every finite score
+constexpr int kNoteAlone = 1, kNoteDone = 2, kNoteLeft = 4;  // of a TokenNote: no source; no source and the output is written; nothing is to be written
 constexpr float kSlack = 8.f;  // a row's reference may lie this far (in powers of two) below its maximum before sums are rescaled
 
 __device__ inline f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
@@ -44,10 +46,9 @@ __device__ inline float cut(float v, uint32_t mask) { return v - __uint_as_float
 
 // What a launch computes.  Causal: a step's queries over their requests' tokens.  Listed: one query of a request over listed tokens.
 // Cross: the queries of all requests that name a source, a row of the table, over all of its tokens; an entry of the launch is a row of the table and
-// its queries are gathered through the sorted list (ice_plan_sources).  Own and Join are the halves of attention behind a shared source: Own is Causal
-// with its rows' sums left in a.state, Join is Cross whose rows then take these sums along and become outputs.
-enum Form { kCausal, kListed, kCross, kOwn, kJoin };
-constexpr bool gathered(int form) { return form == kCross || form == kJoin; }
+// its queries are gathered through the sorted list (ice_plan_sources).  Both: attention behind a source, the entries of Cross and then those of
+// Causal in one launch.
+enum Form { kCausal, kListed, kCross, kBoth };
 
 // A request's query rows and the keys they see; for listed tokens, those of one KV head; for gathered queries, those of a source.
 template <int FORM>
@@ -56,24 +57,32 @@ struct Unit {
     int row0, n_query, first;  // first query row, queries, the position behind the first one's own (listed: entries of the list; gathered: the
                              // position behind the lowest one's own)
     int tokens;              // the length, or what the table has room for if that is less: the queries' positions follow the length all the same
+    bool side;               // of Both: gathered
     // t: the request's length; x, y: its entry of query_start and the next one, or x the length of its list.
-    __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y) { set(a, s, t, x, y); }
+    __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y, int lowest = 0) : side(FORM == kBoth && s < a.S) { set(a, s, t, x, y, lowest); }
     // UNIFORM: the same on all lanes.  A request's words are asked for before one is looked at: left to the compiler, the length was asked for
     // once the request was known to have queries, a trip more (0.1 to 1 us a call).
     template <bool UNIFORM>
-    __device__ Unit(const CacheAttend &a, int s, int h, std::integral_constant<bool, UNIFORM>) {
-        int t = a.seq_len[s], x = LIST ? a.n_tok[s * a.c.H + h] : a.query_start[s], y = LIST ? 0 : a.query_start[s + 1];
+    __device__ Unit(const CacheAttend &a, int s, int h, std::integral_constant<bool, UNIFORM>) : side(FORM == kBoth && s < a.S) {
+        const int row = FORM == kBoth && !side ? s - a.S : s;
+        const int *start = FORM == kBoth && side ? a.list_start : a.query_start;
+        int t = a.seq_len[row], x = LIST ? a.n_tok[s * a.c.H + h] : start[row], y = LIST ? 0 : start[row + 1];
+        int lowest = 0;
+        if constexpr (FORM == kBoth)
+            if (side) lowest = a.lowest[row];
         if constexpr (LIST) {
         } else if constexpr (UNIFORM) {
             t = __builtin_amdgcn_readfirstlane(t);
             x = __builtin_amdgcn_readfirstlane(x);
             y = __builtin_amdgcn_readfirstlane(y);
+            if constexpr (FORM == kBoth) lowest = __builtin_amdgcn_readfirstlane(lowest);
             asm volatile("" : "+s"(t), "+s"(x), "+s"(y));
         } else {
             asm volatile("" : "+v"(t), "+v"(x), "+v"(y));
         }
-        set(a, s, t, x, y, FORM == kJoin && a.window > 0 ? a.lowest[s] : 0);
+        set(a, s, t, x, y, lowest);
     }
+    __host__ __device__ bool gathered() const { return FORM == kCross || (FORM == kBoth && side); }
     // A gathered query's position: its place behind the source's tokens.
     static __host__ __device__ int position(int length, int place) {
         return (int)min(max((long long)max(length, 0) + place, -1ll), (long long)kFar);
@@ -87,16 +96,16 @@ struct Unit {
         } else {
             row0 = min(max(x, 0), a.T);
             n_query = min(max(y, row0), a.T) - row0;
-            if constexpr (gathered(FORM)) first = position(t, lowest) + 1;
+            if (gathered()) first = position(t, lowest) + 1;
             else first = (int)((unsigned)max(t, 0) - (unsigned)n_query + 1u);  // (of a request without queries it may wrap)
         }
     }
-    __host__ __device__ int queries(const CacheAttend &a) const { return min(n_query, a.max_query); }
+    __host__ __device__ int queries(const CacheAttend &a) const { return min(n_query, FORM == kBoth && side ? a.max_shared : a.max_query); }
     // Keys [low, high) that query t sees; sees_from and sees_to: the same for who keeps to keys that some query sees.
     // (of gathered queries every one may see all tokens but those that the lowest one's window leaves out)
-    __host__ __device__ int sees_to(int t) const { return LIST ? first : gathered(FORM) ? tokens : first + t; }
+    __host__ __device__ int sees_to(int t) const { return LIST ? first : gathered() ? tokens : first + t; }
     __host__ __device__ int sees_from(const CacheAttend &a, int t) const {
-        return !LIST && FORM != kCross && a.window > 0 ? max(first + (gathered(FORM) ? 0 : t), 0) - a.window : 0;
+        return !LIST && FORM != kCross && a.window > 0 ? max(first + (gathered() ? 0 : t), 0) - a.window : 0;
     }
     __host__ __device__ int high(int t) const { return LIST ? first : min(max(sees_to(t), 0), tokens); }
     __host__ __device__ int low(const CacheAttend &a, int t) const { return !LIST && a.window > 0 ? min(max(sees_from(a, t), 0), tokens) : 0; }
@@ -106,8 +115,12 @@ struct Unit {
 template <typename U> __host__ __device__ inline int quanta_of(const CacheAttend &a, const U &u, int t0, int t1, int quantum) {
     return max((u.high(t1) + quantum - 1) / quantum - u.low(a, t0) / quantum, 1);
 }
-// The same of a request in the kernel for few queries, if it takes that many rows.
-template <typename U> __host__ __device__ inline int few_quanta(const CacheAttend &a, const U &u, int most_rows, int quantum) {
+// What a unit costs beside its keys, in quanta of the kernel for many queries: it is that much longer in the flat work, behind its keys.  (Of Causal
+// nothing: its units are long there.  Six chunks of 250 to 500 queries on 500 to 1500 keys of their own and 32 K of a source, us: 0 1990, 2 1340, 3 1260, 4 1270; 48 times
+// four drafted tokens on up to 2 K and 8 K: 98, 89, 100, 105.)
+constexpr int chunk_setup(int form) { return form == kCross || form == kBoth ? 2 : 0; }
+// The quanta of a request in the kernel for few queries, if it takes that many rows.
+template <int FORM> __host__ __device__ inline int few_quanta(const CacheAttend &a, const Unit<FORM> &u, int most_rows, int quantum) {
     const int q = u.queries(a);
     return q > 0 && q * a.G <= most_rows ? quanta_of(a, u, 0, q - 1, quantum) : 0;
 }
@@ -134,18 +147,7 @@ __device__ inline void join_sums(f32x4 &sum, float &top, float &total, const f32
     top = mn;
 }
 // Writes four dims of a row from its sums relative to 2^top, and the logarithm of its denominator.
-template <int FORM>
 __device__ inline void put_row(const CacheAttend &a, size_t row, int d0, f32x4 sum, float top, float total) {
-    if constexpr (FORM == kOwn || FORM == kJoin) {
-        float *r = a.state + row * kRecord;
-        if constexpr (FORM == kOwn) {
-            *(f32x4 *)(r + d0) = sum;
-            if (d0 == 0) *(float2 *)(r + kD) = make_float2(top, total);
-            return;
-        }
-        const float2 ml = *(const float2 *)(r + kD);
-        join_sums(sum, top, total, *(const f32x4 *)(r + d0), ml.x, ml.y);
-    }
     const bool none = total == 0.f;  // no key at all: the largest of any weights is 2^-kSlack or more
     sum = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total);
     if (a.out_bf16) *(uint2 *)((bf16_t *)a.out + row * kD + d0) = make_uint2(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]));
@@ -153,34 +155,59 @@ __device__ inline void put_row(const CacheAttend &a, size_t row, int d0, f32x4 s
     if (a.lse && d0 == 0) a.lse[row] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
-// The token whose query is row `row` of a unit that begins at `row0` of the step's queries, or of the sorted list: -1 where the list names none.
-template <int FORM> __device__ inline int token_of(const CacheAttend &a, int row0, int row) {
-    if constexpr (!gathered(FORM)) return row0 + row / a.G;
-    const int t = a.token[row0 + row / a.G];
+// The token whose query is row `row` of a unit: -1 where the sorted list names none.
+template <int FORM> __device__ inline int token_of(const CacheAttend &a, bool side, int row0, int row) {
+    const int at = row0 + row / a.G;
+    if (!(FORM == kCross || (FORM == kBoth && side))) return at;
+    const int t = a.token[at];
     return (unsigned)t < (unsigned)a.T ? t : -1;
 }
-template <int FORM> __device__ inline const bf16_t *query_at(const CacheAttend &a, int token, int h, int row) {
-    return a.q + (long long)(gathered(FORM) ? max(token, 0) : token) * a.q_stride + (long long)(h * a.G + row % a.G) * kD;
+template <int FORM> __device__ inline const bf16_t *query_at(const CacheAttend &a, bool side, int row0, int h, int row) {
+    int token = token_of<FORM>(a, side, row0, row);
+    if (FORM == kCross || FORM == kBoth) token = max(token, 0);
+    return a.q + (long long)token * a.q_stride + (long long)(h * a.G + row % a.G) * kD;
 }
-// alone: of Own, the request has no source, its sums are its output.
+// A whole unit's row.  alone: of Both, the request has no source, its sums are its output; else they wait for the others in their side's state.
 template <int FORM>
-__device__ inline void put_query(const CacheAttend &a, int token, int h, int row, int d0, const f32x4 &sum, float top, float total, bool alone) {
-    if (gathered(FORM) && token < 0) return;
+__device__ inline void put_query(const CacheAttend &a, bool side, int row0, int h, int row, int d0, const f32x4 &sum, float top, float total, bool alone) {
+    const int token = token_of<FORM>(a, side, row0, row);
+    if ((FORM == kCross || FORM == kBoth) && token < 0) return;
     const size_t at = (size_t)token * a.c.H * a.G + h * a.G + row % a.G;
-    if (FORM == kOwn && alone) put_row<kCausal>(a, at, d0, sum, top, total);
-    else put_row<FORM>(a, at, d0, sum, top, total);
+    if (FORM == kBoth && !alone) {
+        float *r = a.state + ((side ? (size_t)a.T * a.c.H * a.G : 0) + at) * kRecord;
+        *(f32x4 *)(r + d0) = sum;
+        if (d0 == 0) *(float2 *)(r + kD) = make_float2(top, total);
+    } else {
+        put_row(a, at, d0, sum, top, total);
+    }
 }
-// What counts as a source: a row of the table, not the request's own.
-template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, int s) {
-    if constexpr (FORM != kOwn) return false;
+// Of Both: a request without a source, that is a row of the table, not its own.
+template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, bool side, int s) {
+    if constexpr (FORM != kBoth) return false;
+    if (side) return false;
     const int to = __builtin_amdgcn_readfirstlane(a.source[s]);
     return (unsigned)to >= (unsigned)a.S || to == s;
+}
+// Of Both, by the workgroup that a unit ends in: where each query's sums are.  rows: of the unit, from the request's row `base` on.
+__device__ inline void put_notes(const CacheAttend &a, const Unit<kBoth> &u, int h, int base, int rows, int first, bool alone) {
+    const int side = u.side ? 1 : 0, t0 = base / a.G, n = rows / a.G, all = u.queries(a);
+    for (int i = threadIdx.x; i < n; i += (int)blockDim.x) {
+        const int token = token_of<kBoth>(a, u.side, u.row0, base + i * a.G);
+        if (token < 0) continue;
+        a.token_notes[((size_t)side * a.T + token) * a.c.H + h] =
+            TokenNote{first, first < 0 ? 1 : (int)blockIdx.x - first + 1, i * a.G, alone ? (first < 0 ? kNoteDone : kNoteAlone) : 0};
+    }
+    if (t0 + n == all)  // queries beyond the most that there may be
+        for (int i = all + (int)threadIdx.x; i < u.n_query; i += (int)blockDim.x) {
+            const int token = token_of<kBoth>(a, u.side, u.row0, i * a.G);
+            if (token >= 0) a.token_notes[((size_t)side * a.T + token) * a.c.H + h] = TokenNote{-1, 1, 0, kNoteLeft};
+        }
 }
 // Keys [low, high) of the part [from, to) that row `row` of the unit sees.
 template <int FORM>
 __device__ inline void sees(const CacheAttend &a, const Unit<FORM> &u, int length, int row, int from, int to, int &low, int &high) {
     const int t = row / a.G;
-    if constexpr (FORM == kJoin) {
+    if (FORM == kBoth && u.side) {
         const int behind = Unit<FORM>::position(length, a.place[u.row0 + t]) + 1;
         low = a.window > 0 ? max(behind - a.window, from) : from;
         high = min(behind, to);
@@ -188,6 +215,23 @@ __device__ inline void sees(const CacheAttend &a, const Unit<FORM> &u, int lengt
         low = max(u.sees_from(a, t), from);
         high = min(u.sees_to(t), to);
     }
+}
+// The entries of a launch: of Both, the rows of the table as sources and then as requests, all in one launch, several to a place of the table of sums
+// where there are more of them than places.
+template <int FORM> struct Entries {
+    int n, each, slots;
+    __host__ __device__ Entries(const CacheAttend &a) : n(FORM == kBoth ? 2 * a.S : a.n_here), each(FORM == kBoth ? (n + kEntries - 1) / kEntries : 1),
+                                                        slots(FORM == kBoth ? (n + each - 1) / each : n) {}
+};
+// Of Both: the entry that the flat work's quantum `now` lies in, from its place of the table; quanta(e): those of an entry.  first: where the entry begins.
+template <typename F> __host__ __device__ inline int entry_at(const Entries<kBoth> &x, int slot, unsigned now, unsigned &first, unsigned &n, F quanta) {
+    int e = slot * x.each;
+    n = quanta(e);
+    while (now >= first + n && e + 1 < x.n) {
+        first += n;
+        n = quanta(++e);
+    }
+    return e;
 }
 
 // ------------------------------------------------------------------------------------------------------------- few queries
@@ -313,7 +357,7 @@ __device__ inline void clear_unsourced(const CacheAttend &a) {
         for (int i = threadIdx.x; i < heads * (kD / 4); i += (int)blockDim.x) {
             const size_t row = (size_t)t * heads + i / (kD / 4);
             const int d0 = 4 * (i % (kD / 4));
-            put_row<kCross>(a, row, d0, f32x4{0.f, 0.f, 0.f, 0.f}, kNoMax, 0.f);
+            put_row(a, row, d0, f32x4{0.f, 0.f, 0.f, 0.f}, kNoMax, 0.f);
         }
     }
 }
@@ -357,16 +401,22 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
     const int term = PACK == 1 ? 0 : c / R, col_row = PACK == 1 ? c : c % R;
 
     unsigned total = 0;
-    const bool even = LIST || a.per_unit > 0;  // units of equal nominal length: no need to look at the lengths
+    const Entries<FORM> entries(a);
+    auto quanta_at = [&](int e, auto uniform) -> unsigned {
+        const Unit<FORM> u(a, a.first + e, 0, uniform);
+        return (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
+    };
+    const bool even = FORM != kBoth && (LIST || a.per_unit > 0);  // units of equal nominal length: no need to look at the lengths
     if (even) {
         total = (unsigned)a.n_here * a.c.H * (unsigned)a.per_unit;
     } else {
-        for (int e0 = 0; e0 < a.n_here; e0 += W * 64) {
+        for (int e0 = 0; e0 < entries.slots; e0 += W * 64) {
             const int e = e0 + tid;
             unsigned n = 0;
-            if (e < a.n_here) {
-                const Unit<FORM> u(a, a.first + e, 0, std::false_type());
-                n = (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
+            if constexpr (FORM == kBoth) {
+                for (int k = e * entries.each; k < min((e + 1) * entries.each, entries.n); ++k) n += quanta_at(k, std::false_type());
+            } else if (e < a.n_here) {
+                n = quanta_at(e, std::false_type());
             }
             const unsigned incl = (unsigned)wave_scan_add((int)n);
             if (lane == 63) s_wave[wave] = incl;
@@ -377,10 +427,10 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                 if (w < wave) before += s_wave[w];
                 total += s_wave[w];
             }
-            if (e < a.n_here) s_before[e] = before + incl - n;
+            if (e < entries.slots) s_before[e] = before + incl - n;
             __syncthreads();
         }
-        if (tid == 0) s_before[a.n_here] = total;
+        if (tid == 0) s_before[entries.slots] = total;
         __syncthreads();
     }
     if constexpr (FORM == kCross)
@@ -391,11 +441,11 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    MergeNote note = {-1, 0, 0, 0, 0, 0};
+    MergeNote note = {-1, 0, 0, 0, 0};
     int entry = 0;
     if (!even) {  // the last request that begins at or before the piece (of those, the one that is not empty)
-        for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
-            if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
+        for (int width = 1 << (31 - __builtin_clz(entries.slots)); width; width >>= 1)
+            if (entry + width < entries.slots && s_before[entry + width] <= begin) entry += width;
     }
     const int tiles_mask = (1 << a.c.tile_shift) - 1;
     const int k_row = 4 * (c & 3) + (c >> 2);  // token that is row c of the key operand: row 4 g + i is token 4 i + g
@@ -413,8 +463,14 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             u1 = u0 + (unsigned)a.per_unit;
         } else {
             while (s_before[entry + 1] <= now) ++entry;
-            const unsigned first = s_before[entry], per = (s_before[entry + 1] - first) / (unsigned)a.c.H;
+            unsigned first = s_before[entry], quanta = s_before[entry + 1] - first;
             s = entry;
+            if constexpr (FORM == kBoth)
+                if (entries.each > 1) {
+                    const unsigned at = (unsigned)__builtin_amdgcn_readfirstlane((int)now);
+                    s = entry_at(entries, __builtin_amdgcn_readfirstlane(entry), at, first, quanta, [&](int e) { return quanta_at(e, std::true_type()); });
+                }
+            const unsigned per = quanta / (unsigned)a.c.H;
             h = (int)((now - first) / per);
             u0 = first + (unsigned)h * per;
             u1 = u0 + per;
@@ -423,7 +479,8 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         h = __builtin_amdgcn_readfirstlane(h);
         const unsigned stop = min(u1, end);
         const Unit<FORM> unit(a, s, h, std::true_type());
-        const bool alone = is_alone<FORM>(a, s);
+        if constexpr (FORM == kBoth) s = unit.side ? s : s - a.S;  // (from here on: the row of the table)
+        const bool alone = is_alone<FORM>(a, unit.side, s);
         const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
         if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
             now = stop;
@@ -439,12 +496,12 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             const int row = min(R * x + col_row, n_rows - 1);
-            sees<FORM>(a, unit, FORM == kJoin ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
-            const bf16_t *p = query_at<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row) + 32 * g;
+            sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+            const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
-        if constexpr (FORM == kJoin) {  // (a source's queries stand in no order)
+        if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order)
             all_low = low[0];
             all_high = high[0];
 #pragma unroll
@@ -774,7 +831,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                     const int in = in0 + 2 * W * pass, row = R * x + in;
                     if (in >= R || row >= n_rows) continue;
                     if (whole) {
-                        put_query<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row, d0, sum[pass], top[pass], all[pass], alone);
+                        put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum[pass], top[pass], all[pass], alone);
                     } else {
                         float *r = record + (size_t)row * kRecord;
                         *(f32x4 *)(r + d0) = sum[pass];
@@ -787,7 +844,11 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
             }
             __syncthreads();
         }
-        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows, alone};
+        if constexpr (FORM == kBoth) {
+            if (stop == u1) put_notes(a, unit, h, 0, n_rows, whole ? -1 : (int)pieces.owner(u0), alone);
+        } else if (now > u0 && stop == u1) {
+            note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows};
+        }
         now = stop;
     }
     if (tid == 0 && a.notes) a.notes[blockIdx.x] = note;
@@ -816,19 +877,26 @@ constexpr int kVector = 0x002, kMatrix = 0x008, kLdsRead = 0x100;
 constexpr int kAhead = 2, kWeightOps = 28, kBeside = 2;
 
 struct Chunks {  // how a request's row tiles lie in the flat work of one KV head
-    int n_rows, tiles;
-    unsigned pair, single, per_head;  // quanta of a pair, of the middle tile of an odd number, of all
-    template <typename U> __host__ __device__ static int quanta(const CacheAttend &a, const U &u, int n_rows, int tile) {
-        return quanta_of(a, u, kChunkRows * tile / a.G, (min(kChunkRows * (tile + 1), n_rows) - 1) / a.G, kQuantum);
+    int n_rows, tiles, step, quantum;  // step: rows of a tile
+    unsigned pair, single, per_head;   // quanta of a pair, of the middle tile of an odd number, of all
+    template <int FORM> __host__ __device__ int quanta(const CacheAttend &a, const Unit<FORM> &u, int tile) const {
+        return quanta_of(a, u, step * tile / a.G, (min(step * (tile + 1), n_rows) - 1) / a.G, quantum) + chunk_setup(FORM);
     }
-    template <int FORM> __host__ __device__ Chunks(const CacheAttend &a, const Unit<FORM> &u) {
+    template <int FORM> __host__ __device__ Chunks(const CacheAttend &a, const Unit<FORM> &u) : step(kChunkRows), quantum(kQuantum) {
         n_rows = u.queries(a) * a.G;
         tiles = 0;
         pair = single = per_head = 0;
-        if (n_rows <= kRows) return;  // (the few-query kernel's, which takes that many where there are requests with more than kFewRows)
-        tiles = (n_rows + kChunkRows - 1) / kChunkRows;
-        const int middle = quanta(a, u, n_rows, (tiles - 1) / 2);
-        if (gathered(FORM)) {  // all row tiles take the same keys
+        // (up to kRows rows are the few-query kernel's, which takes that many where there are requests with more than kFewRows)
+        if (n_rows <= (FORM == kCausal ? kRows : 0)) return;
+        if constexpr (FORM != kCausal) {  // whole tokens, as evenly as they go; a quantum of few rows is longer, since its keys cost less
+            const int most = kChunkRows / a.G, n = n_rows / a.G;
+            tiles = (n + most - 1) / most;
+            step = (n + tiles - 1) / tiles * a.G;
+            if (step <= kRows * kWaves) quantum = 2 * kQuantum;
+        }
+        tiles = (n_rows + step - 1) / step;
+        const int middle = quanta(a, u, (tiles - 1) / 2);
+        if (u.gathered()) {  // all row tiles take the same keys
             pair = 2 * (unsigned)middle;
             single = (unsigned)middle;
             per_head = (unsigned)tiles * single;
@@ -838,7 +906,7 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
         // pair.  It is no bound: tiles of queries in front of the first key see nothing, and then a pair's first tile alone may need more.
         // So a pair's second tile gets what the first one leaves of it, and that is one quantum at least (see at()); what a unit needs beyond its nominal length its last
         // part takes along (PartKeys).
-        if (tiles > 1) pair = (unsigned)max(2 * middle + 2, quanta(a, u, n_rows, tiles - 1) + 1);
+        if (tiles > 1) pair = (unsigned)max(2 * middle + 2, quanta(a, u, tiles - 1) + 1);
         if (tiles & 1) single = (unsigned)middle;
         per_head = (unsigned)(tiles / 2) * pair + single;
     }
@@ -851,7 +919,7 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
         const unsigned paired = head0 + (unsigned)(tiles / 2) * pair;
         if (now >= paired) return {tiles / 2, paired, paired + single};
         const int p = (int)((now - head0) / pair);
-        const unsigned p0 = head0 + (unsigned)p * pair, split = p0 + (unsigned)min(quanta(a, u, n_rows, tiles - 1 - p), (int)pair - 1);
+        const unsigned p0 = head0 + (unsigned)p * pair, split = p0 + (unsigned)min(quanta(a, u, tiles - 1 - p), (int)pair - 1);
         return now >= split ? Tile{p, split, p0 + pair} : Tile{tiles - 1 - p, p0, split};
     }
 };
@@ -863,9 +931,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     __shared__ uint32_t s_flags[2][kWaves];  // of a tile of keys: bit 0: in no block, bit 1: values held as NaN were taken out
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
     unsigned total = 0;
-    for (int e0 = 0; e0 < a.n_here; e0 += kWaves * 64) {
+    const Entries<FORM> entries(a);
+    auto quanta_at = [&](int e, auto uniform) -> unsigned { return Chunks(a, Unit<FORM>(a, a.first + e, 0, uniform)).per_head * (unsigned)a.c.H; };
+    for (int e0 = 0; e0 < entries.slots; e0 += kWaves * 64) {
         const int e = e0 + tid;
-        const unsigned n = e < a.n_here ? Chunks(a, Unit<FORM>(a, a.first + e, 0, std::false_type())).per_head * (unsigned)a.c.H : 0u;
+        unsigned n = 0;
+        if constexpr (FORM == kBoth) {
+            for (int k = e * entries.each; k < min((e + 1) * entries.each, entries.n); ++k) n += quanta_at(k, std::false_type());
+        } else {
+            n = e < a.n_here ? quanta_at(e, std::false_type()) : 0u;
+        }
         const unsigned incl = (unsigned)wave_scan_add((int)n);
         if (lane == 63) s_wave[wave] = incl;
         __syncthreads();
@@ -875,21 +950,23 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             if (w < wave) before += s_wave[w];
             total += s_wave[w];
         }
-        if (e < a.n_here) s_before[e] = before + incl - n;
+        if (e < entries.slots) s_before[e] = before + incl - n;
         __syncthreads();
     }
-    if (tid == 0) s_before[a.n_here] = total;
+    if (tid == 0) s_before[entries.slots] = total;
     __syncthreads();
+    if constexpr (FORM == kCross)
+        if (a.first == 0) clear_unsourced(a);
     const Pieces pieces(__builtin_amdgcn_readfirstlane(total), gridDim.x, false);
     if (blockIdx.x >= pieces.groups || total == 0) {
-        if (tid == 0) a.notes[blockIdx.x].first = -1;
+        if (FORM != kBoth && tid == 0) a.notes[blockIdx.x].first = -1;
         return;
     }
     const unsigned begin = pieces.begin(blockIdx.x), end = pieces.begin(blockIdx.x + 1);
-    MergeNote note = {-1, 0, 0, 0, 0, 0};
+    MergeNote note = {-1, 0, 0, 0, 0};
     int entry = 0;
-    for (int width = 1 << (31 - __builtin_clz(a.n_here)); width; width >>= 1)
-        if (entry + width < a.n_here && s_before[entry + width] <= begin) entry += width;
+    for (int width = 1 << (31 - __builtin_clz(entries.slots)); width; width >>= 1)
+        if (entry + width < entries.slots && s_before[entry + width] <= begin) entry += width;
     const int tiles_mask = (1 << a.c.tile_shift) - 1;
     const int k_row = 4 * (c & 3) + (c >> 2);
     const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
@@ -897,26 +974,33 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
 
     for (unsigned now = begin; now < end;) {
         while (s_before[entry + 1] <= now) ++entry;
-        const int s = __builtin_amdgcn_readfirstlane(entry) + a.first;
+        unsigned first = s_before[entry];
+        int s = __builtin_amdgcn_readfirstlane(entry) + a.first;
+        if constexpr (FORM == kBoth)
+            if (entries.each > 1) {
+                unsigned quanta;
+                first = (unsigned)__builtin_amdgcn_readfirstlane((int)first);
+                s = entry_at(entries, s, (unsigned)__builtin_amdgcn_readfirstlane((int)now), first, quanta, [&](int e) { return quanta_at(e, std::true_type()); });
+            }
         const Unit<FORM> unit(a, s, 0, std::true_type());
-        const bool alone = is_alone<FORM>(a, s);
+        if constexpr (FORM == kBoth) s = unit.side ? s : s - a.S;  // (from here on: the row of the table)
+        const bool alone = is_alone<FORM>(a, unit.side, s);
         const Chunks ch(a, unit);
-        const unsigned first = s_before[entry];
         const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
         const Chunks::Tile place = ch.at(a, unit, first + (unsigned)h * ch.per_head, now);
         const int all_rows = ch.n_rows, tile = __builtin_amdgcn_readfirstlane(place.tile);
         const unsigned u0 = place.u0, u1 = place.u1, stop = min(u1, end);
-        const int base = kChunkRows * tile, n_rows = min(all_rows - base, kChunkRows);
+        const int base = ch.step * tile, n_rows = min(all_rows - base, ch.step);
         const int t_first = base / a.G, t_last = (base + n_rows - 1) / a.G;
-        const int q0 = unit.low(a, t_first) / kQuantum + (int)(now - u0);
-        const PartKeys keys(a, unit, t_first, t_last, kQuantum, u0, u1, now, stop);
+        const int q0 = unit.low(a, t_first) / ch.quantum + (int)(now - u0);
+        const PartKeys keys(a, unit, t_first, t_last, ch.quantum, u0, u1, now, stop);
         const int from = keys.from, to = keys.to;
         int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(t_first), to);
-        if (FORM == kJoin) {  // (a source's queries stand in no order: not every one need see these keys)
-            all_low = to;
-            all_high = from;
+        if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order: only of the lowest one the position is known)
+            all_low = a.window > 0 ? to : from;
+            all_high = min(unit.first, to);
         }
-        const int key_at = q0 * kQuantum;  // of the first round
+        const int key_at = q0 * ch.quantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
         // this lane's rows: columns of tiles wave + 4 x
         int low[kTiles], high[kTiles], wave_low = 0, wave_high = to;
@@ -924,8 +1008,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
             const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1);
-            sees<FORM>(a, unit, FORM == kJoin ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
-            const bf16_t *p = query_at<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row) + 32 * g;
+            sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+            const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
@@ -934,7 +1018,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             wave_low = max(unit.sees_from(a, (base + r1) / a.G), from);
             wave_high = min(unit.sees_to((base + r0) / a.G), to);
         }
-        if constexpr (FORM == kJoin) {
+        if (FORM == kBoth && unit.side) {
             wave_low = max(max(low[0], low[1]), low[2]);
             wave_high = min(min(high[0], high[1]), high[2]);
 #pragma unroll
@@ -1147,8 +1231,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             }
         };
         // (a wave without rows converts all the same; its one tile is not written)
-        if (n_tiles > 1) run(std::integral_constant<int, kTiles>());
-        else run(std::integral_constant<int, 1>());
+        if constexpr (FORM == kCausal) {
+            if (n_tiles > 1) run(std::integral_constant<int, kTiles>());
+            else run(std::integral_constant<int, 1>());
+        } else {
+            if (n_tiles > 2) run(std::integral_constant<int, kTiles>());
+            else if (n_tiles > 1) run(std::integral_constant<int, 2>());
+            else run(std::integral_constant<int, 1>());
+        }
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1;
         float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
@@ -1164,7 +1254,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 for (int half = 0; half < 2; ++half) {
                     const int d0 = 32 * g + 8 * i + 4 * half;
                     const f32x4 sum = {acc[x][4 * half][i], acc[x][4 * half + 1][i], acc[x][4 * half + 2][i], acc[x][4 * half + 3][i]};
-                    if (whole) put_query<FORM>(a, token_of<FORM>(a, unit.row0, row), h, row, d0, sum, m[x], l[x], alone);
+                    if (whole) put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum, m[x], l[x], alone);
                     else *(f32x4 *)(record + (size_t)in * kRecord + d0) = sum;
                 }
             if (!whole && g == 0) {
@@ -1172,10 +1262,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 record[(size_t)in * kRecord + kD + 1] = l[x];
             }
         }
-        if (now > u0 && stop == u1) note = {(int)pieces.owner(u0), h, unit.row0, base, all_rows, alone};
+        if constexpr (FORM == kBoth) {
+            if (stop == u1) put_notes(a, unit, h, base, n_rows, whole ? -1 : (int)pieces.owner(u0), alone);
+        } else if (now > u0 && stop == u1) {
+            note = {(int)pieces.owner(u0), h, unit.row0, base, FORM == kCausal ? all_rows : min(all_rows, base + n_rows)};
+        }
         now = stop;
     }
-    if (tid == 0) a.notes[blockIdx.x] = note;
+    if (FORM != kBoth && tid == 0) a.notes[blockIdx.x] = note;
 }
 
 // Joins the records of the unit whose end workgroup blockIdx.x noted, if it did: one of workgroup `first` (its last part), one each of
@@ -1224,7 +1318,62 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend 
 #pragma unroll
         for (int w = 1; w < GROUPS; ++w) join(s_sum[all + w][kD], s_sum[all + w][kD + 1], *(const f32x4 *)(s_sum[all + w] + d0));
     }
-    if (mine) put_query<FORM>(a, token_of<FORM>(a, note.row0, row), note.h, row, d0, sum, top, total, note.alone);
+    if (mine) put_query<FORM>(a, false, note.row0, note.h, row, d0, sum, top, total, false);
+}
+
+// Of Both: a (token, KV head)'s sums over its own tokens and over its source's, records or a whole unit's state each, become its output.  Groups of 32 threads
+// take a row, four dims each; GROUPS of them share a row's sums.  Bound by its trips: the notes, the records.
+template <int GROUPS>
+__global__ __launch_bounds__(kMergeThreads) void cache_join_kernel(CacheAttend a) {
+    __shared__ float s_sum[kMergeThreads / 32][kRecord];
+    constexpr int kAtOnceRows = kMergeThreads / 32 / GROUPS, kAtOnce = 4;
+    const int t = (int)(blockIdx.x / (unsigned)a.c.H), h = (int)(blockIdx.x % (unsigned)a.c.H);
+    const int all_tokens = a.query_start[a.S];
+    const TokenNote note[2] = {a.token_notes[(size_t)t * a.c.H + h], a.token_notes[((size_t)a.T + t) * a.c.H + h]};
+    if (t >= all_tokens || (note[0].flags & (kNoteLeft | kNoteDone))) return;
+    const bool alone = note[0].flags & kNoteAlone;
+    if (!alone && (note[1].flags & kNoteLeft)) return;
+    int n[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        n[k] = k == 1 && alone ? 0 : note[k].first < 0 ? 1 : note[k].count;
+        // (what no kernel of this call wrote would name records that there are not)
+        if (n[k] && note[k].first >= 0 && (note[k].count < 1 || note[k].count > a.groups || note[k].first > a.groups - note[k].count || note[k].row < 0 || note[k].row > a.rows - a.G)) return;
+    }
+    const int all = threadIdx.x >> 5, group = all % GROUPS, d0 = 4 * (threadIdx.x & 31), total_n = n[0] + n[1];
+    const int j = (int)blockIdx.y * kAtOnceRows + all / GROUPS;
+    const size_t row = (size_t)t * a.c.H * a.G + h * a.G + min(j, a.G - 1);
+    float top = kNoMax, total = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int k = group; k < total_n; k += GROUPS * kAtOnce) {
+        float2 ml[kAtOnce];
+        f32x4 v[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int kk = min(k + GROUPS * i, total_n - 1), side = kk >= n[0] ? 1 : 0, at = kk - (side ? n[0] : 0);
+            const int first = side ? note[1].first : note[0].first, in = side ? note[1].row : note[0].row;
+            const float *x = first < 0 ? a.state + ((side ? (size_t)a.T * a.c.H * a.G : 0) + row) * kRecord
+                                       : a.part + ((size_t)record_of(first + at, at > 0) * a.rows + in + min(j, a.G - 1)) * kRecord;
+            v[i] = *(const f32x4 *)(x + d0);
+            ml[i] = *(const float2 *)(x + kD);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (k + GROUPS * i < total_n) join_sums(sum, top, total, v[i], ml[i].x, ml[i].y);
+    }
+    if constexpr (GROUPS > 1) {
+        float *r = s_sum[all];
+        *(f32x4 *)(r + d0) = sum;
+        if (d0 == 0) {
+            r[kD] = top;
+            r[kD + 1] = total;
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int w = 1; w < GROUPS; ++w) join_sums(sum, top, total, *(const f32x4 *)(s_sum[all + w] + d0), s_sum[all + w][kD], s_sum[all + w][kD + 1]);
+    }
+    if (j < a.G) put_row(a, row, d0, sum, top, total);
 }
 
 // Query rows of the launch for few: all of them up to kFewRows, else the requests' with at most 16, and a launch of the many-query
@@ -1242,28 +1391,34 @@ inline size_t attend_bytes(int groups, int rows) { return (size_t)groups * (2 * 
 
 constexpr int kListWaves = 8;
 
-// The launches of a call, workgroup by workgroup as the kernels take their pieces, from the lengths on the host.
+template <int FORM> inline Unit<FORM> host_unit(const CacheAttend &a, int entry, int h, const int *start, const int *len) {
+    if constexpr (FORM == kBoth) {  // (the call's own arrays, on the host)
+        const bool side = entry < a.S;
+        const int row = side ? entry : entry - a.S, *from = side ? a.list_start : a.query_start;
+        return Unit<FORM>(a, entry, a.seq_len[row], from[row], from[row + 1], side ? a.lowest[row] : 0);
+    }
+    if constexpr (FORM == kListed) return Unit<FORM>(a, entry, 1 << 30, len[entry * a.c.H + h], 0);
+    else return Unit<FORM>(a, entry, len[entry], start[entry], start[entry + 1]);
+}
 template <int FORM, typename F> inline void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
     constexpr bool LIST = FORM == kListed;
-    const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = few_rows(a);
+    const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = FORM == kBoth ? a.rows : few_rows(a);
     const bool even = LIST || a.per_unit > 0;
-    const auto unit = [&](int s, int h) {
-        return LIST ? Unit<FORM>(a, s, 1 << 30, len[s * a.c.H + h], 0) : Unit<FORM>(a, s, len[s], start[s], start[s + 1]);
-    };
-    unsigned before[kEntries + 1] = {0};  // quanta before each request
-    for (int e = 0; e < a.n_here; ++e)
-        before[e + 1] = before[e] + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, unit(a.first + e, 0), rows, quantum));
-    const unsigned total = before[a.n_here];
-    const unsigned launched = a.whole ? a.n_here * a.c.H : a.few_groups;
+    const int n = Entries<FORM>(a).n;
+    std::vector<unsigned> before(n + 1, 0);  // quanta before each request
+    for (int e = 0; e < n; ++e)
+        before[e + 1] = before[e] + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, host_unit<FORM>(a, a.first + e, 0, start, len), rows, quantum));
+    const unsigned total = before[n];
+    const unsigned launched = a.whole ? a.n_here * a.c.H : FORM == kBoth ? a.groups : a.few_groups;
     const Pieces pieces(total, launched, a.whole);
     if (total == 0) return;
     for (unsigned i = 0; i < pieces.groups && i < launched; ++i)
         for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
-            const int entry = (int)(std::upper_bound(before, before + a.n_here + 1, now) - before) - 1;
+            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
             const unsigned per = (before[entry + 1] - before[entry]) / a.c.H, h = (now - before[entry]) / per;
             const unsigned u0 = before[entry] + h * per, u1 = u0 + per;
             stop = std::min(u1, end);
-            const auto u = unit(a.first + entry, (int)h);
+            const auto u = host_unit<FORM>(a, a.first + entry, (int)h, start, len);
             const int n_rows = u.queries(a) * a.G;
             if (n_rows <= 0 || n_rows > rows) continue;
             const PartKeys keys(a, u, 0, (n_rows - 1) / a.G, quantum, u0, u1, now, stop);
@@ -1273,35 +1428,42 @@ template <int FORM, typename F> inline void cut_few(const CacheAttend &a, const 
         }
 }
 template <int FORM, typename F> inline void cut_many(const CacheAttend &a, const int *start, const int *len, F put) {
-    const auto unit = [&](int s) { return Unit<FORM>(a, s, len[s], start[s], start[s + 1]); };
-    unsigned before[kEntries + 1] = {0};
-    for (int e = 0; e < a.n_here; ++e) before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, unit(a.first + e)).per_head;
-    const Pieces pieces(before[a.n_here], a.many_groups, false);
-    if (before[a.n_here] == 0) return;
-    for (unsigned i = 0; i < pieces.groups && i < (unsigned)a.many_groups; ++i)
+    const int n = Entries<FORM>(a).n;
+    const unsigned launched = FORM == kBoth ? a.groups : a.many_groups;
+    std::vector<unsigned> before(n + 1, 0);
+    for (int e = 0; e < n; ++e) before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, host_unit<FORM>(a, a.first + e, 0, start, len)).per_head;
+    const Pieces pieces(before[n], launched, false);
+    if (before[n] == 0) return;
+    for (unsigned i = 0; i < pieces.groups && i < launched; ++i)
         for (unsigned now = pieces.begin(i), end = pieces.begin(i + 1), stop; now < end; now = stop) {
-            const int entry = (int)(std::upper_bound(before, before + a.n_here + 1, now) - before) - 1;
-            const auto u = unit(a.first + entry);
+            const int entry = (int)(std::upper_bound(before.begin(), before.end(), now) - before.begin()) - 1;
+            const auto u = host_unit<FORM>(a, a.first + entry, 0, start, len);
             const Chunks ch(a, u);
             const unsigned h = (now - before[entry]) / ch.per_head;
             const Chunks::Tile p = ch.at(a, u, before[entry] + h * ch.per_head, now);
             stop = std::min(p.u1, end);
-            const int base = kChunkRows * p.tile, n_rows = std::min(ch.n_rows - base, kChunkRows);
-            const PartKeys keys(a, u, base / a.G, (base + n_rows - 1) / a.G, kQuantum, p.u0, p.u1, now, stop);
+            const int base = ch.step * p.tile, n_rows = std::min(ch.n_rows - base, ch.step);
+            const PartKeys keys(a, u, base / a.G, (base + n_rows - 1) / a.G, ch.quantum, p.u0, p.u1, now, stop);
             const bool cut = now > p.u0 || stop < p.u1;
             put({a.first, 1, (int)i, a.first + entry, (int)h, base, n_rows, keys.from, keys.to, (int)p.u0, (int)p.u1, (int)now, (int)stop,
                  cut ? (int)record_of(i, now > p.u0) : -1, now > p.u0 && stop == p.u1 ? (int)pieces.owner(p.u0) : -1});
         }
 }
+// The launches of a call, workgroup by workgroup as the kernels take their pieces, from the lengths on the host.
 template <int FORM> inline long long cut_attend(CacheAttend a, const int *start, const int *len, int *parts, long long most) {
     long long n = 0;
     const auto put = [&](const std::array<int, kCutInts> &part) {
         if (n < most) std::copy(part.begin(), part.end(), parts + n * kCutInts);
         ++n;
     };
+    if constexpr (FORM == kBoth) {
+        if (a.many) cut_many<FORM>(a, start, len, put);
+        else cut_few<FORM>(a, start, len, put);
+        return n;
+    }
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
         a.n_here = std::min(a.S - a.first, kEntries);
-        cut_few<FORM>(a, start, len, put);
+        if (FORM != kCross || !a.many) cut_few<FORM>(a, start, len, put);
         if constexpr (FORM != kListed)
             if (a.many) cut_many<FORM>(a, start, len, put);
     }
@@ -1310,7 +1472,7 @@ template <int FORM> inline long long cut_attend(CacheAttend a, const int *start,
 
 template <int W, int FORM>
 inline void launch_few(const CacheAttend &a, hipStream_t stream) {
-    const dim3 grid(a.whole ? a.n_here * a.c.H : a.few_groups), block(W * 64);
+    const dim3 grid(FORM == kBoth ? a.groups : a.whole ? a.n_here * a.c.H : a.few_groups), block(W * 64);
     if (a.rows == 5) cache_attend_kernel<W, 3, 1, 1, FORM><<<grid, block, 0, stream>>>(a);
     else if (a.rows == 8 && a.out_bf16) cache_attend_kernel<W, 2, 1, 1, FORM><<<grid, block, 0, stream>>>(a);
     else if (a.rows == 8) cache_attend_kernel<W, 2, 1, 2, FORM><<<grid, block, 0, stream>>>(a);
@@ -1322,6 +1484,9 @@ inline void launch_few(const CacheAttend &a, hipStream_t stream) {
         else if (a.out_bf16) cache_attend_kernel<W, 1, 3, 1, FORM><<<grid, block, 0, stream>>>(a);
         else cache_attend_kernel<W, 1, 3, 3, FORM><<<grid, block, 0, stream>>>(a);
     }
+}
+template <int FORM>
+inline void launch_few_merge(const CacheAttend &a, hipStream_t stream) {
     if (a.whole) return;
     // threads for four records of a unit at a time: one trip for most
     const int rows = std::min(a.rows, a.max_query * a.G), per_unit = a.few_groups / std::max(1, a.n_here * a.c.H) + 2;
@@ -1335,10 +1500,13 @@ inline void launch_attend(CacheAttend a, hipStream_t stream) {
     float *const part = a.part;
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
         a.n_here = std::min(a.S - a.first, kEntries);
-        a.rows = few_rows(a);
-        a.notes = a.whole ? nullptr : (MergeNote *)part;
-        a.part = a.whole ? nullptr : (float *)(a.notes + a.few_groups);
-        launch_few<FORM == kListed ? kListWaves : kWaves, FORM>(a, stream);
+        if (FORM != kCross || !a.many) {  // (of Cross the one kernel or the other takes all)
+            a.rows = few_rows(a);
+            a.notes = a.whole ? nullptr : (MergeNote *)part;
+            a.part = a.whole ? nullptr : (float *)(a.notes + a.few_groups);
+            launch_few<FORM == kListed ? kListWaves : kWaves, FORM>(a, stream);
+            launch_few_merge<FORM>(a, stream);
+        }
         if constexpr (FORM != kListed) {
             if (!a.many) continue;
             a.rows = chunk_rows(a);
@@ -1349,6 +1517,16 @@ inline void launch_attend(CacheAttend a, hipStream_t stream) {
             cache_merge_kernel<1, FORM><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
         }
     }
+}
+
+constexpr long long kJoinRows = 4096;  // rows whose sums are joined by many threads each: few rows have many records
+inline void launch_both(const CacheAttend &a, hipStream_t stream) {
+    if (!a.many) launch_few<kWaves, kBoth>(a, stream);
+    else if (a.out_bf16) cache_chunk_kernel<1, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
+    else cache_chunk_kernel<3, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
+    const unsigned units = (unsigned)a.T * (unsigned)a.c.H;
+    if ((long long)units * a.G <= kJoinRows) cache_join_kernel<8><<<dim3(units, a.G), kMergeThreads, 0, stream>>>(a);
+    else cache_join_kernel<2><<<dim3(units, (a.G + 3) / 4), kMergeThreads, 0, stream>>>(a);
 }
 
 }  // namespace

@@ -80,16 +80,31 @@ void launch_plan_sources(const CacheSources &p, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------ attention
-size_t cache_state_bytes(const CacheAttend &a) { return (size_t)a.T * a.c.H * a.G * kRecord * sizeof(float); }
+static size_t note_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H * sizeof(TokenNote); }
+static size_t state_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H * a.G * kRecord * sizeof(float); }
+
+size_t plan_cache_shared(CacheAttend &a, int max_source) {
+    const long long most = std::max(a.max_query, a.max_shared), tile = kChunkRows / a.G;
+    a.many = most * a.G > kFewRows;
+    CacheAttend rows = a;
+    rows.max_query = (int)most;
+    a.rows = a.many ? (int)std::min<long long>(tile, most) * a.G : few_rows(rows);
+    const auto quanta = [&](int keys, long long queries) { return ((long long)keys + kQuantum - 1) / kQuantum * (a.many ? (queries + tile - 1) / tile : 1); };
+    const double all = (double)a.c.H * ((double)a.S * quanta(a.max_keys, a.max_query) + quanta(max_source, a.max_shared));
+    a.groups = (int)std::min<double>(a.rows > kRows ? 512 : 768, all);
+    return note_bytes(a) + state_bytes(a) + (size_t)a.groups * 2 * a.rows * kRecord * sizeof(float);
+}
 
 long long cut_cache_cross(CacheAttend a, const int *start, const int *len, int *parts, long long most) { return cut_attend<kCross>(a, start, len, parts, most); }
+long long cut_cache_shared(const CacheAttend &a, int *parts, long long most) { return cut_attend<kBoth>(a, nullptr, nullptr, parts, most); }
 
 void launch_cache_cross(const CacheAttend &a, hipStream_t stream) { launch_attend<kCross>(a, stream); }
 
-// The requests' own tokens first: their sums are then at hand where a source's rows are finished.
-void launch_cache_shared(const CacheAttend &own, const CacheAttend &join, hipStream_t stream) {
-    launch_attend<kOwn>(own, stream);
-    launch_attend<kJoin>(join, stream);
+void launch_cache_shared(CacheAttend a, void *workspace, hipStream_t stream) {
+    a.token_notes = static_cast<TokenNote *>(workspace);
+    a.state = reinterpret_cast<float *>(static_cast<char *>(workspace) + note_bytes(a));
+    a.part = a.state + state_bytes(a) / sizeof(float);
+    launch_both(a, stream);
 }
 
 }  // namespace ice

@@ -4,7 +4,15 @@ import pytest
 import torch
 
 from tests.test_cache4_cpu import FAKE, status
+from tests import shared_ref as sh
 from tests.test_cache4_cut_cpu import CHUNK, FEW, check_units
+
+
+def tiles(queries, group):
+    """First rows of the tiles of the kernel for many queries: whole tokens, as evenly as they go, at most 192 rows."""
+    n = -(-queries // (CHUNK // group))
+    step = -(-queries // n)
+    return [(at * group, min(step, queries - at) * group) for at in range(0, queries, step)]
 
 
 def check(heads, group, lens, counts, max_shared=None, max_keys=None, block=16, width=None):
@@ -18,16 +26,66 @@ def check(heads, group, lens, counts, max_shared=None, max_keys=None, block=16, 
     keys = max(1, max(lens)) if max_keys is None else max_keys
     parts = b.ice_debug_cross_cut(c, group, len(lens), start, int(start[-1]), most, lens, keys, width)
     nbytes = p.ice_cache_attend_cross_bytes(c, group, len(lens), most, keys)
-    rows_most = most * group
-    room = next(r for r in (5, 8, 16, 32, FEW, 1 << 30) if rows_most <= r)
-    few = 16 if rows_most > FEW else room
+    many = most * group > FEW
     expected = {}
     for s, (length, n) in enumerate(zip(lens, counts)):
-        rows = min(n, most) * group
-        many = rows_most > FEW and rows > 16
-        for base in range(0, rows, CHUNK if many else 1 << 30):
-            expected[int(many), s, base] = (min(rows - base, CHUNK) if many else rows, 0, min(length, width * block))
-    check_units(dict(zip(b.CUT_FIELDS, parts.T)), nbytes, heads, expected, (few, min(CHUNK, rows_most)))
+        n = min(n, most)
+        for base, rows in tiles(n, group) if many and n else [(0, n * group)] if n else []:
+            expected[int(many), s, base] = (rows, 0, min(length, width * block))
+    check_units(dict(zip(b.CUT_FIELDS, parts.T)), nbytes, heads, expected, (next(r for r in (5, 8, 16, 32, FEW, 1 << 30) if most * group <= r), min(CHUNK, most * group)))
+
+
+def check_shared(heads, group, lens, qlens, source, window=0, max_query=None, max_shared=None, max_keys=None, max_source=None, block=16, width=None):
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(None, 1, heads, block)
+    n, start = len(lens), np.concatenate([[0], np.cumsum(qlens)])
+    tokens = int(start[-1]) + 2
+    plan = sh.sources(source, start, lens, n, tokens)
+    counts, lowest = np.diff(plan[: n + 1]), plan[n + 2: 2 * n + 2]
+    most = [max(max(x), 1) if m is None else m for x, m in ((qlens, max_query), (counts, max_shared))]
+    width = width or max(1, -(-max(lens) // block))
+    keys = [max(1, max(lens)) if k is None else k for k in (max_keys, max_source)]
+    parts = b.ice_debug_shared_cut(c, group, n, start, plan, tokens, *most, lens, *keys, width, window)
+    nbytes = p.ice_cache_attend_shared_bytes(c, group, n, tokens, *most, *keys) - tokens * heads * (32 + 1056 * group)
+    many, capacity = max(most) * group > FEW, width * block
+    expected = {}
+    for e in range(2 * n):
+        s = e % n
+        m = min(counts[s], most[1]) if e < n else min(qlens[s], most[0])
+        for base, rows in tiles(m, group) if many and m else [(0, m * group)] if m else []:
+            if e < n:  # every tile of a source takes what the lowest query's window leaves
+                low = max(lens[s] + int(lowest[s]) + 1, 0) - window if window else 0
+                seen = (min(max(low, 0), capacity, lens[s]), min(lens[s], capacity))
+            else:
+                ends = [lens[s] - qlens[s] + t + 1 for t in (base // group, (base + rows - 1) // group)]
+                low = max(max(ends[0], 0) - window, 0) if window else 0
+                seen = (min(low, capacity, lens[s]), min(max(ends[1], 0), capacity))
+            expected[int(many), e, base] = (rows, *seen)
+    room = next(r for r in (5, 8, 16, 32, FEW, 1 << 30) if max(most) * group <= r)
+    x = dict(zip(b.CUT_FIELDS, parts.T))
+    nbytes += 32 * (int(x["workgroup"].max(initial=-1)) + 1)  # (there are no notes by workgroup here)
+    check_units(x, nbytes, heads, expected, (room, min(CHUNK // group, max(most)) * group))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_requests_behind_sources_of_any_shape(seed):
+    rng = np.random.default_rng([seed, 6])
+    for _ in range(40):
+        n, group = int(rng.choice([1, 2, 5, 40, 130])), int(rng.choice([1, 2, 3, 4, 5, 7, 8, 11, 16]))
+        top = 1500 if rng.random() < 0.5 else max(1, FEW // group)
+        qlens = [int(np.exp(rng.uniform(0, np.log(top)))) if rng.random() < 0.6 else 0 for _ in range(n)]
+        lens = [int(np.exp(rng.uniform(0, np.log(40000 // n + 2)))) - 1 if rng.random() < 0.5 else max(0, int(m + rng.integers(-500, 900))) for m in qlens]
+        source = rng.choice([-1, int(rng.integers(0, n)), int(rng.integers(0, n))], n)
+        window = int(rng.choice([0, 0, 1, 127, 128, int(rng.integers(1, 1500))]))
+        some = lambda most: None if rng.random() < 0.7 else int(rng.integers(1, most))  # noqa: E731
+        check_shared(int(rng.choice([1, 2, 8])), group, lens, qlens, source, window, some(max(qlens) + 2), some(sum(qlens) + 2), some(9000), some(9000),
+                     width=None if rng.random() < 0.8 else max(1, max(lens) // 40))
+
+
+def test_more_rows_than_the_table_of_sums_has_places():
+    for n, queries in ((513, 1), (1500, 1), (3000, 60), (8192, 1)):
+        check_shared(1, 2, [9] * 7 + [500] + [20] * (n - 8), [queries if i % 3 else 0 for i in range(n)], np.where(np.arange(n) % 5 == 4, -1, 7))
 
 
 @pytest.mark.parametrize("seed", range(12))
@@ -59,7 +117,10 @@ def test_the_measured_cases():
         for s, g in zip(source, gain):
             if s >= 0:
                 counts[s] += g
-        check(case["heads"], case["group"], lengths, counts, block=case["block"])
+        if case["kind"] == "cross":
+            check(case["heads"], case["group"], lengths, counts, block=case["block"])
+        else:
+            check_shared(case["heads"], case["group"], lengths, gain, source, case["window"], block=case["block"])
 
 
 def test_the_hook_refuses():
@@ -69,6 +130,12 @@ def test_the_hook_refuses():
     for change in (dict(n_rows=0), dict(n_rows=8193), dict(n_tokens=-1), dict(max_shared=0), dict(max_keys=0), dict(max_blocks=0), dict(max_blocks=2 ** 27)):
         args = dict(cache=c, group_size=4, n_rows=1, start=e, n_tokens=1, max_shared=1, length=e, max_keys=16, max_blocks=1)
         assert status(b.ice_debug_cross_cut, **{**args, **change}) == b.ICE_ERR_SHAPE, change
+    e = np.zeros(8, np.int32)
+    for change in (dict(n_requests=0), dict(n_requests=8193), dict(n_tokens=-1), dict(max_query=0), dict(max_shared=0), dict(max_keys=0), dict(max_source_keys=0),
+                   dict(max_blocks=0), dict(window=-1)):
+        args = dict(cache=c, group_size=4, n_requests=1, query_start=e, plan=e, n_tokens=1, max_query=1, max_shared=1, length=e, max_keys=16, max_source_keys=16,
+                    max_blocks=1)
+        assert status(b.ice_debug_shared_cut, **{**args, **change}) == b.ICE_ERR_SHAPE, change
 
 
 # ------------------------------------------------------------------------------------------------------------- what is refused
@@ -115,7 +182,7 @@ def test_attention_to_sources_refuses():
                 window=0, out=FAKE, ot=0, lse=None, ws=FAKE, wb=1 << 30)
     need = {p.ice_cache_attend_cross: p.ice_cache_attend_cross_bytes(c, 4, 2, 1, 4096),
             p.ice_cache_attend_shared: p.ice_cache_attend_shared_bytes(c, 4, 2, 2, 1, 2, 64, 4096)}
-    assert need[p.ice_cache_attend_shared] > 2 * 8 * 528  # (every row's sums, and scratch)
+    assert need[p.ice_cache_attend_shared] > 2 * 8 * 1056  # (every row's sums over both sides' tokens, and scratch)
     for call, good, count in ((p.ice_cache_attend_cross, cross, "rows"), (p.ice_cache_attend_shared, both, "n")):
         go = lambda **change: status(call, c, *{**good, **change}.values())  # noqa: E731, B023
         for name in [x for x in ("q", "start", "source", "plan", "sl", "table", "out", "ws") if x in good]:
