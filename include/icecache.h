@@ -427,7 +427,7 @@ ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_toke
  *   seq_len [n_rows], block_table [n_rows][max_blocks]: those of the sources.  max_keys: about the longest of them, a hint.
  *   max_shared: no source has more queries (tokens; those beyond are left out), in [1, 2^24].
  *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with max_shared in the place of max_query and a source's queries in the place of a
- *     request's; where max_shared * group_size is above 48, a bf16 output's weights are rounded to bf16 once whatever its source's queries are.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
+ *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
  *   workspace: ice_cache_attend_cross_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
  * SHAPE for n_rows > 8192; UNSUPPORTED as for ice_cache_attend. */
 size_t ice_cache_attend_cross_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, int32_t max_shared, int32_t max_keys);
@@ -443,7 +443,8 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int
  *   source, plan: as given to and written by ice_plan_sources for this step, n_rows = n_requests, with seq_len.
  *   max_query, max_keys: of the requests' own queries and tokens, as for ice_cache_attend; max_shared: no source has more queries (tokens of all its requests;
  *     those beyond are left out, their outputs as they were), in [1, 2^24]; max_source_keys: about the longest source, a hint.
- *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as for ice_cache_attend_cross, with the larger of max_query and max_shared.
+ *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with the larger of max_query and max_shared in the place
+ *     of max_query; a source's queries and a request's own each for themselves.
  *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 1056 for every row of out, and scratch.
  * SHAPE for n_requests > 8192; UNSUPPORTED where (tokens of a table row / 128 + 3) * ((max_query + max_shared) / (192 / group_size) + 4) * 2 * n_requests *
  * n_kv_heads, or n_tokens * n_kv_heads, reaches 2^31. */

@@ -383,22 +383,401 @@ __device__ inline void clear_unsourced(const CacheAttend &a) {
 // Bound by the vector unit (busy 61 %) and HBM together where there is much to read: one token of 16 requests of up to 32 K tokens, 8 KV heads,
 // 68 us with the merge, 5.3 TB/s; about 220 vector instructions beside 16 products for 32 keys.  Else by its trips: one request of
 // 4 K tokens 10 us.  Five drafted tokens of 32 requests, 40 rows, a window of 4096: 55 us, 23 of them products.  Lists of 1024 for 128 units 13.5.
-template <int W, int PACK, int NT, int SETS, int FORM>
-__global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
+// LDS of a part: the waves' sums.  More than one tile of columns leaves no registers for a step on its way: three steps of a wave are copied to LDS by
+// direct loads (where the waves' sums meet later), [two tiles' key codes in operand order][their value codes][their scales].
+constexpr int kDepth = 3, kStage = 4352;
+constexpr int few_lds(int W, int NT) {
+    const int sums = (int)sizeof(float) * W * kRows * kRecord, stages = NT > 1 ? W * kDepth * kStage : 0;
+    return sums > stages ? sums : stages;
+}
+
+// The part [now, stop) of the unit [u0, u1): n_rows rows of KV head h, row s of the table; a quantum of the flat work is QUANTUM keys.  Every wave is done with
+// s_raw before and after.
+template <int W, int PACK, int NT, int SETS, int FORM, int QUANTUM>
+__device__ __attribute__((always_inline)) inline void few_part(const CacheAttend &a, const Unit<FORM> &unit, int s, int h, int n_rows, unsigned u0, unsigned u1, unsigned now,
+                                                               unsigned stop, bool alone, char *s_raw) {
     constexpr bool LIST = FORM == kListed;
     static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
     constexpr int R = kRows / PACK;  // rows in a tile of columns
     constexpr int Q = W * kStep;     // keys of a step of all waves
-    // More than one tile of columns leaves no registers for a step on its way: three steps of a wave are copied to LDS by direct loads
-    // (where the waves' sums meet later), [two tiles' key codes in operand order][their value codes][their scales].
-    constexpr int kDepth = 3, kStage = 4352;
-    constexpr size_t kSums = sizeof(float) * W * kRows * kRecord, kStages = NT > 1 ? (size_t)W * kDepth * kStage : 0;
-    __shared__ __attribute__((aligned(16))) char s_raw[kSums > kStages ? kSums : kStages];
+    static_assert(QUANTUM % Q == 0, "parts begin with a step");
     float(*s_acc)[kRows][kRecord] = reinterpret_cast<float(*)[kRows][kRecord]>(s_raw);
-    __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of Q keys before each request
-    __shared__ unsigned s_wave[W];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
     const int term = PACK == 1 ? 0 : c / R, col_row = PACK == 1 ? c : c % R;
+    const int tiles_mask = (1 << a.c.tile_shift) - 1;
+    const int k_row = 4 * (c & 3) + (c >> 2);  // token that is row c of the key operand: row 4 g + i is token 4 i + g
+    const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
+    const uint32_t v_at = kCacheV + 64 * g + 4 * c, vs_at = kCacheVS + 16 * g + 4 * (c >> 2);
+    const int t_last = (n_rows - 1) / a.G;
+    // keys of this part that any row sees, that every row sees, that this lane's rows see
+    const int q0 = unit.low(a, 0) / QUANTUM;
+    const PartKeys keys(a, unit, 0, t_last, QUANTUM, u0, u1, now, stop);
+    const int from = keys.from, to = keys.to;
+    int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
+    int low[NT], high[NT];
+    u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+        const int row = min(R * x + col_row, n_rows - 1);
+        sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+        const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
+    }
+    if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order)
+        all_low = low[0];
+        all_high = high[0];
+#pragma unroll
+        for (int x = 1; x < NT; ++x) {
+            all_low = max(all_low, low[x]);
+            all_high = min(all_high, high[x]);
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            all_low = max(all_low, __shfl_xor(all_low, d));
+            all_high = min(all_high, __shfl_xor(all_high, d));
+        }
+        all_low = __builtin_amdgcn_readfirstlane(all_low);
+        all_high = __builtin_amdgcn_readfirstlane(all_high);
+    }
+    const int step0 = (q0 + (int)(now - u0)) * (QUANTUM / kStep);  // the wave's steps: step0 + wave + W n
+    const int n_mine = to > from ? max((to - kStep * (step0 + wave) + Q - 1) / Q, 0) : 0;
+    const int *table = a.table + (size_t)s * a.max_blocks;
+    const int *list = LIST ? a.pos + ((size_t)s * a.c.H + h) * a.max_keys : nullptr;
+
+    // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n + l / 2, in units of tiles of the pool.  Listed:
+    // index of key l & 31 of step n + l / 32, in units of rows of the pool.  -1: no such place.  A list's positions are
+    // looked up two lots ahead, its blocks one lot, so that neither trip is waited for but at the start (16 requests x 8 heads x 1024 tokens:
+    // 14.4 us, 17.6 without; a dense lot lasts 32 steps, and a register more costs as much as its wait).
+    constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
+    auto position = [&](int n) __attribute__((always_inline)) -> int {  // listed
+        const long long e = (long long)(step0 + wave + W * (n + (lane >> 5))) * kStep + (lane & 31);
+        const int p = e < to ? list[e] : -1;
+        return p < unit.tokens ? p : -1;
+    };
+    auto block_of = [&](int p) __attribute__((always_inline)) -> int { return p >= 0 ? table[p >> (a.c.tile_shift + 4)] : -1; };
+    auto row_of = [&](int p, int id) __attribute__((always_inline)) -> int {
+        return (unsigned)id < (unsigned)a.c.n_blocks
+                   ? (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15)) : -1;
+    };
+    auto tile_of = [&](int n) __attribute__((always_inline)) -> int {  // dense
+        const int tile = (step0 + wave + W * (n + (lane >> 1))) * 2 + (lane & 1);
+        const int id = (long long)tile * 16 < to ? table[tile >> a.c.tile_shift] : -1;
+        return (unsigned)id < (unsigned)a.c.n_blocks ? (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask)) : -1;
+    };
+    struct Places {
+        int held, next, id, pos;  // on the lanes now; the next lot (listed: its positions and blocks), positions of the one behind it
+    } at = {-1, -1, -1, -1};
+    auto begin_places = [&]() __attribute__((always_inline)) {
+        if constexpr (LIST) {
+            const int p = position(0);
+            at.next = position(kAhead);
+            at.held = row_of(p, block_of(p));
+            at.id = block_of(at.next);
+            at.pos = position(2 * kAhead);
+        } else {
+            at.held = tile_of(0);
+        }
+    };
+    auto turn_places = [&](int n) __attribute__((always_inline)) {  // step n begins a lot
+        if constexpr (LIST) {
+            at.held = row_of(at.next, at.id);
+            at.next = at.pos;
+            at.id = block_of(at.next);
+            at.pos = position(n + 2 * kAhead);
+        } else {
+            at.held = tile_of(n);
+        }
+    };
+    // step n of this wave: key codes, value codes
+    auto request_keys = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
+        x.bad = 0;
+        if constexpr (LIST) x.bad = (uint32_t)(__ballot(held == -1) >> (32 * (n & 1)));
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if constexpr (LIST) {
+                const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + k_row), 0);
+                const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
+                x.k[b] = *(const u32x4 *)(t + 64 * (row & 15) + 16 * g);
+                x.ks[b] = t[kCacheKS + cache_scale_byte(row & 15, g)];
+            } else {
+                const int id = __builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b);
+                if (id < 0) x.bad |= 0xFFFFu << (16 * b);
+                const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
+                x.k[b] = __builtin_nontemporal_load((const u32x4 *)(t + k_at));
+                x.ks[b] = t[ks_at];
+            }
+        }
+    };
+    auto request_values = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if constexpr (LIST) {
+                uint32_t scales = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + 4 * i + g), 0);
+                    const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
+                    x.v[b][i] = *(const uint32_t *)(t + kCacheV + 64 * (row & 15) + 4 * c);
+                    scales |= (uint32_t)t[kCacheVS + cache_scale_byte(row & 15, c >> 2)] << (8 * i);
+                }
+                x.vs[b] = scales;
+            } else {
+                const uint8_t *t = a.c.data + (size_t)max(__builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b), 0) * kCacheTileBytes;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.v[b][i] = __builtin_nontemporal_load((const uint32_t *)(t + v_at + 256 * i));
+                x.vs[b] = *(const uint32_t *)(t + vs_at);
+            }
+        }
+    };
+
+    f32x4 acc[NT][8];  // acc[x][j][i]: dim 32 g + 8 i + j of column c of tile x
+    float m[NT], l[NT];
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+        m[x] = kNoMax;
+        l[x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const uint32_t cut1 = PACK > 1 && term >= 1 ? 0xFFFF0000u : 0u, cut2 = PACK > 2 && term >= 2 ? 0xFFFF0000u : 0u;
+    // Step n; take_values(): where the value codes are still to be fetched into y.
+    auto attend = [&](int n, Keys &y, auto take_values) __attribute__((always_inline)) {
+        const int key0 = (step0 + wave + W * n) * kStep;
+        f32x4 d[NT][2];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float sc = __uint_as_float(y.ks[b] << 23);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32x4 k = eight(y.k[b][j], sc);
+#pragma unroll
+                for (int x = 0; x < NT; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+            }
+        }
+        const uint32_t bad = y.bad;
+        take_values();
+        if (key0 < all_low || key0 + kStep > all_high || bad != 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int in = 16 * (e >> 2) + 4 * (e & 3) + g, key = key0 + in;
+                const bool gone = (bad >> in) & 1;
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+                    if (gone || key < low[x] || key >= high[x]) d[x][e >> 2][e & 3] = -INFINITY;
+                // what no row sees may hold anything: its value scale must not turn a weight of 0 into NaN
+                if (gone || key < from || key >= to) y.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+            }
+            if (!LIST && take_nan(y)) {
+                float nan[NT] = {};
+                find_nan<NT>(a, table, h, key0, from, to, g, low, high, nan);
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
+            }
+        }
+        u32x4 w[NT][SETS];  // the weights' terms
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
+            softmax(p, a.scale_log2, m[x], l[x], acc[x]);
+            if constexpr (PACK == 2 && SETS == 2) {  // first and second term in the first set; the third one on the first's lanes
+                float third[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float second = cut(p[e], 0xFFFF0000u);
+                    third[e] = term == 0 ? cut(second, 0xFFFF0000u) : 0.f;
+                    p[e] = term == 0 ? p[e] : second;
+                }
+                w[x][0] = tops(p);
+                w[x][1] = tops(third);
+            } else if constexpr (PACK == 1 && SETS == 1) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) w[x][0][e >> 1] = pack2(p[e], p[e + 1]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < SETS; ++t) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (t > 0) p[e] = cut(p[e], 0xFFFF0000u);
+                        if (PACK > 1) p[e] = cut(p[e], cut1);
+                        if (PACK > 2) p[e] = cut(p[e], cut2);
+                    }
+                    w[x][t] = tops(p);
+                }
+            }
+        }
+        float vsc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vsc[e] = scale_of(y.vs[e >> 2], e & 3);
+        auto dims = [&](auto sel) __attribute__((always_inline)) {
+            constexpr int j = decltype(sel)::value;
+            u32x4 v0, v1;
+            values<j>(y, vsc, v0, v1);
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int t = 0; t < SETS; ++t) {
+                    acc[x][2 * j] = mfma(v0, w[x][t], acc[x][2 * j]);
+                    acc[x][2 * j + 1] = mfma(v1, w[x][t], acc[x][2 * j + 1]);
+                }
+        };
+        dims(std::integral_constant<int, 0>());
+        dims(std::integral_constant<int, 1>());
+        dims(std::integral_constant<int, 2>());
+        dims(std::integral_constant<int, 3>());
+    };
+
+    if (n_mine > 0) {
+        begin_places();
+        if constexpr (NT == 1) {  // two steps in registers: one worked on, one on its way
+            Keys x, y;
+            auto request = [&](int n, Keys &z) __attribute__((always_inline)) {
+                if (n >= n_mine) return;
+                if (n % kAhead == 0 && n) turn_places(n);
+                request_keys(at.held, n, z);
+                request_values(at.held, n, z);
+            };
+            request(0, x);
+            for (int n = 0; n < n_mine; n += 2) {
+                request(n + 1, y);
+                attend(n, x, [] {});
+                if (n + 1 >= n_mine) break;
+                request(n + 2, x);
+                attend(n + 1, y, [] {});
+            }
+        } else {
+            char *const stage = s_raw + wave * (kDepth * kStage);
+            uint32_t missing = 0;  // tiles that do not exist, two bits a step, the latest request's lowest
+            auto request = [&](int n) __attribute__((always_inline)) {
+                if (n % kAhead == 0 && n) turn_places(n);
+                const int id0 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead)), id1 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead) + 1);
+                missing = missing << 2 | (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u);
+                const uint8_t *t0 = a.c.data + (size_t)max(id0, 0) * kCacheTileBytes, *t1 = a.c.data + (size_t)max(id1, 0) * kCacheTileBytes;
+                char *to_lds = stage + (n % kDepth) * kStage;
+                lds_dma_stream<16>((t0 + k_at), to_lds);
+                lds_dma_stream<16>((t1 + k_at), to_lds + 1024);
+                lds_dma_stream<16>((t0 + kCacheV + 16 * lane), to_lds + 2048);
+                lds_dma_stream<16>((t1 + kCacheV + 16 * lane), to_lds + 3 * 1024);
+                lds_dma_stream<4>(((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
+            };
+            for (int n = 0; n < min(kDepth, n_mine); ++n) request(n);
+            for (int n = 0; n < n_mine; ++n) {
+                const int later = min(kDepth - 1, n_mine - 1 - n);  // steps requested after this one, five loads each
+                if (later == 2) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+                else if (later == 1) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                const char *from_lds = stage + (n % kDepth) * kStage;
+                const uint32_t gone = missing >> (2 * later);
+                Keys x;
+                x.bad = (gone & 1 ? 0xFFFFu : 0u) | (gone & 2 ? 0xFFFF0000u : 0u);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    x.k[b] = *(const u32x4 *)(from_lds + 1024 * b + 16 * lane);
+                    x.ks[b] = *(const uint8_t *)(from_lds + 4096 + 128 * b + (ks_at - kCacheKS));
+                }
+                attend(n, x, [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x.v[b][i] = *(const uint32_t *)(from_lds + 2048 + 1024 * b + (v_at - kCacheV) + 256 * i);
+                        x.vs[b] = *(const uint32_t *)(from_lds + 4096 + 128 * b + (vs_at - kCacheKS));
+                    }
+                });
+                if (n + kDepth < n_mine) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stage has been read)
+                    request(n + kDepth);
+                }
+            }
+            __syncthreads();  // (the sums go where the stages were)
+        }
+    } else if constexpr (NT > 1) {
+        __syncthreads();
+    }
+
+    // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
+    const bool whole = now == u0 && stop == u1;
+    float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
+    const int d0 = 4 * (tid & 31);
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+        if (x > 0 && R * x >= n_rows) break;
+        l[x] += __shfl_xor(l[x], 16);
+        l[x] += __shfl_xor(l[x], 32);
+        if (R * x + col_row < n_rows && term < PACK) {
+            float *r = s_acc[wave][c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                *(f32x4 *)(r + 32 * g + 8 * i) = f32x4{acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+                *(f32x4 *)(r + 32 * g + 8 * i + 4) = f32x4{acc[x][4][i], acc[x][5][i], acc[x][6][i], acc[x][7][i]};
+            }
+            if (g == 0) {
+                r[kD] = m[x];
+                r[kD + 1] = l[x];
+            }
+        }
+        __syncthreads();
+        // (with one tile the reads of a thread's rows stand side by side, rows behind the last one read what lies there and write nothing: 24
+        // requests of mixed lengths 273 us, 281 row by row; with three tiles the registers for that are not there: drafts 64 us, 58)
+        constexpr int kPasses = NT == 1 ? (R + 2 * W - 1) / (2 * W) : 1;
+        for (int in0 = tid >> 5; in0 < (NT == 1 ? 2 * W : min(R, n_rows - R * x)); in0 += 2 * W * kPasses) {
+            f32x4 sum[kPasses];
+            float top[kPasses], all[kPasses];
+#pragma unroll
+            for (int pass = 0; pass < kPasses; ++pass) {
+                const int in = min(in0 + 2 * W * pass, R - 1);
+                float2 ml[W];
+#pragma unroll
+                for (int w = 0; w < W; ++w) ml[w] = *(const float2 *)&s_acc[w][in][kD];
+                top[pass] = kNoMax;
+#pragma unroll
+                for (int w = 0; w < W; ++w) top[pass] = fmaxf(top[pass], ml[w].x);
+                sum[pass] = f32x4{0.f, 0.f, 0.f, 0.f};
+                all[pass] = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(ml[w].x - top[pass]);
+                    f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
+#pragma unroll
+                    for (int t = 1; t < PACK; ++t) v += *(const f32x4 *)(s_acc[w][in + t * R] + d0);
+                    sum[pass] += v * f;
+                    all[pass] += ml[w].y * f;
+                }
+            }
+#pragma unroll
+            for (int pass = 0; pass < kPasses; ++pass) {
+                const int in = in0 + 2 * W * pass, row = R * x + in;
+                if (in >= R || row >= n_rows) continue;
+                if (whole) {
+                    put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum[pass], top[pass], all[pass], alone);
+                } else {
+                    float *r = record + (size_t)row * kRecord;
+                    *(f32x4 *)(r + d0) = sum[pass];
+                    if (d0 == 0) {
+                        r[kD] = top[pass];
+                        r[kD + 1] = all[pass];
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int W, int PACK, int NT, int SETS, int FORM>
+__global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_kernel(CacheAttend a) {
+    constexpr bool LIST = FORM == kListed;
+    constexpr int R = kRows / PACK;  // rows in a tile of columns
+    constexpr int Q = W * kStep;     // keys of a step of all waves
+    __shared__ __attribute__((aligned(16))) char s_raw[few_lds(W, NT)];
+    __shared__ unsigned s_before[LIST ? 1 : kEntries + 1];  // quanta of Q keys before each request
+    __shared__ unsigned s_wave[W];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
 
     unsigned total = 0;
     const Entries<FORM> entries(a);
@@ -447,10 +826,6 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         for (int width = 1 << (31 - __builtin_clz(entries.slots)); width; width >>= 1)
             if (entry + width < entries.slots && s_before[entry + width] <= begin) entry += width;
     }
-    const int tiles_mask = (1 << a.c.tile_shift) - 1;
-    const int k_row = 4 * (c & 3) + (c >> 2);  // token that is row c of the key operand: row 4 g + i is token 4 i + g
-    const uint32_t k_at = 64 * k_row + 16 * g, ks_at = kCacheKS + cache_scale_byte(k_row, g);
-    const uint32_t v_at = kCacheV + 64 * g + 4 * c, vs_at = kCacheVS + 16 * g + 4 * (c >> 2);
 
     for (unsigned now = begin; now < end;) {
         int s, h;
@@ -481,371 +856,14 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         const Unit<FORM> unit(a, s, h, std::true_type());
         if constexpr (FORM == kBoth) s = unit.side ? s : s - a.S;  // (from here on: the row of the table)
         const bool alone = is_alone<FORM>(a, unit.side, s);
-        const int n_rows = unit.queries(a) * a.G, t_last = (n_rows - 1) / a.G;
+        const int n_rows = unit.queries(a) * a.G;
         if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
             now = stop;
             continue;
         }
-        // keys of this part that any row sees, that every row sees, that this lane's rows see
-        const int q0 = unit.low(a, 0) / Q;
-        const PartKeys keys(a, unit, 0, t_last, Q, u0, u1, now, stop);
-        const int from = keys.from, to = keys.to;
-        int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
-        int low[NT], high[NT];
-        u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const int row = min(R * x + col_row, n_rows - 1);
-            sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
-            const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
-        }
-        if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order)
-            all_low = low[0];
-            all_high = high[0];
-#pragma unroll
-            for (int x = 1; x < NT; ++x) {
-                all_low = max(all_low, low[x]);
-                all_high = min(all_high, high[x]);
-            }
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) {
-                all_low = max(all_low, __shfl_xor(all_low, d));
-                all_high = min(all_high, __shfl_xor(all_high, d));
-            }
-            all_low = __builtin_amdgcn_readfirstlane(all_low);
-            all_high = __builtin_amdgcn_readfirstlane(all_high);
-        }
-        const int step0 = (q0 + (int)(now - u0)) * W;  // the wave's steps: step0 + wave + W n
-        const int n_mine = to > from ? max((to - kStep * (step0 + wave) + Q - 1) / Q, 0) : 0;
-        const int *table = a.table + (size_t)s * a.max_blocks;
-        const int *list = LIST ? a.pos + ((size_t)s * a.c.H + h) * a.max_keys : nullptr;
-
-        // Up to 64 places on the lanes.  Dense: index of tile l & 1 of the wave's step n + l / 2, in units of tiles of the pool.  Listed:
-        // index of key l & 31 of step n + l / 32, in units of rows of the pool.  -1: no such place.  A list's positions are
-        // looked up two lots ahead, its blocks one lot, so that neither trip is waited for but at the start (16 requests x 8 heads x 1024 tokens:
-        // 14.4 us, 17.6 without; a dense lot lasts 32 steps, and a register more costs as much as its wait).
-        constexpr int kAhead = LIST ? 2 : 32;  // steps whose places lie on the lanes
-        auto position = [&](int n) __attribute__((always_inline)) -> int {  // listed
-            const long long e = (long long)(step0 + wave + W * (n + (lane >> 5))) * kStep + (lane & 31);
-            const int p = e < to ? list[e] : -1;
-            return p < unit.tokens ? p : -1;
-        };
-        auto block_of = [&](int p) __attribute__((always_inline)) -> int { return p >= 0 ? table[p >> (a.c.tile_shift + 4)] : -1; };
-        auto row_of = [&](int p, int id) __attribute__((always_inline)) -> int {
-            return (unsigned)id < (unsigned)a.c.n_blocks
-                       ? (int)(((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((p >> 4) & tiles_mask)) * 16u + (p & 15)) : -1;
-        };
-        auto tile_of = [&](int n) __attribute__((always_inline)) -> int {  // dense
-            const int tile = (step0 + wave + W * (n + (lane >> 1))) * 2 + (lane & 1);
-            const int id = (long long)tile * 16 < to ? table[tile >> a.c.tile_shift] : -1;
-            return (unsigned)id < (unsigned)a.c.n_blocks ? (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + (tile & tiles_mask)) : -1;
-        };
-        struct Places {
-            int held, next, id, pos;  // on the lanes now; the next lot (listed: its positions and blocks), positions of the one behind it
-        } at = {-1, -1, -1, -1};
-        auto begin_places = [&]() __attribute__((always_inline)) {
-            if constexpr (LIST) {
-                const int p = position(0);
-                at.next = position(kAhead);
-                at.held = row_of(p, block_of(p));
-                at.id = block_of(at.next);
-                at.pos = position(2 * kAhead);
-            } else {
-                at.held = tile_of(0);
-            }
-        };
-        auto turn_places = [&](int n) __attribute__((always_inline)) {  // step n begins a lot
-            if constexpr (LIST) {
-                at.held = row_of(at.next, at.id);
-                at.next = at.pos;
-                at.id = block_of(at.next);
-                at.pos = position(n + 2 * kAhead);
-            } else {
-                at.held = tile_of(n);
-            }
-        };
-        // step n of this wave: key codes, value codes
-        auto request_keys = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
-            x.bad = 0;
-            if constexpr (LIST) x.bad = (uint32_t)(__ballot(held == -1) >> (32 * (n & 1)));
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                if constexpr (LIST) {
-                    const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + k_row), 0);
-                    const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
-                    x.k[b] = *(const u32x4 *)(t + 64 * (row & 15) + 16 * g);
-                    x.ks[b] = t[kCacheKS + cache_scale_byte(row & 15, g)];
-                } else {
-                    const int id = __builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b);
-                    if (id < 0) x.bad |= 0xFFFFu << (16 * b);
-                    const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
-                    x.k[b] = __builtin_nontemporal_load((const u32x4 *)(t + k_at));
-                    x.ks[b] = t[ks_at];
-                }
-            }
-        };
-        auto request_values = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                if constexpr (LIST) {
-                    uint32_t scales = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t row = (uint32_t)max(__shfl(held, 32 * (n & 1) + 16 * b + 4 * i + g), 0);
-                        const uint8_t *t = a.c.data + (size_t)(row >> 4) * kCacheTileBytes;
-                        x.v[b][i] = *(const uint32_t *)(t + kCacheV + 64 * (row & 15) + 4 * c);
-                        scales |= (uint32_t)t[kCacheVS + cache_scale_byte(row & 15, c >> 2)] << (8 * i);
-                    }
-                    x.vs[b] = scales;
-                } else {
-                    const uint8_t *t = a.c.data + (size_t)max(__builtin_amdgcn_readlane(held, 2 * (n % kAhead) + b), 0) * kCacheTileBytes;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x.v[b][i] = __builtin_nontemporal_load((const uint32_t *)(t + v_at + 256 * i));
-                    x.vs[b] = *(const uint32_t *)(t + vs_at);
-                }
-            }
-        };
-
-        f32x4 acc[NT][8];  // acc[x][j][i]: dim 32 g + 8 i + j of column c of tile x
-        float m[NT], l[NT];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            m[x] = kNoMax;
-            l[x] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        const uint32_t cut1 = PACK > 1 && term >= 1 ? 0xFFFF0000u : 0u, cut2 = PACK > 2 && term >= 2 ? 0xFFFF0000u : 0u;
-        // Step n; take_values(): where the value codes are still to be fetched into y.
-        auto attend = [&](int n, Keys &y, auto take_values) __attribute__((always_inline)) {
-            const int key0 = (step0 + wave + W * n) * kStep;
-            f32x4 d[NT][2];
-#pragma unroll
-            for (int x = 0; x < NT; ++x) d[x][0] = d[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const float sc = __uint_as_float(y.ks[b] << 23);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const u32x4 k = eight(y.k[b][j], sc);
-#pragma unroll
-                    for (int x = 0; x < NT; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
-                }
-            }
-            const uint32_t bad = y.bad;
-            take_values();
-            if (key0 < all_low || key0 + kStep > all_high || bad != 0) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int in = 16 * (e >> 2) + 4 * (e & 3) + g, key = key0 + in;
-                    const bool gone = (bad >> in) & 1;
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-                        if (gone || key < low[x] || key >= high[x]) d[x][e >> 2][e & 3] = -INFINITY;
-                    // what no row sees may hold anything: its value scale must not turn a weight of 0 into NaN
-                    if (gone || key < from || key >= to) y.vs[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-                }
-                if (!LIST && take_nan(y)) {
-                    float nan[NT] = {};
-                    find_nan<NT>(a, table, h, key0, from, to, g, low, high, nan);
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) acc[x][j] += nan[x];
-                }
-            }
-            u32x4 w[NT][SETS];  // the weights' terms
-#pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                float p[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = d[x][e >> 2][e & 3];
-                softmax(p, a.scale_log2, m[x], l[x], acc[x]);
-                if constexpr (PACK == 2 && SETS == 2) {  // first and second term in the first set; the third one on the first's lanes
-                    float third[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float second = cut(p[e], 0xFFFF0000u);
-                        third[e] = term == 0 ? cut(second, 0xFFFF0000u) : 0.f;
-                        p[e] = term == 0 ? p[e] : second;
-                    }
-                    w[x][0] = tops(p);
-                    w[x][1] = tops(third);
-                } else if constexpr (PACK == 1 && SETS == 1) {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) w[x][0][e >> 1] = pack2(p[e], p[e + 1]);
-                } else {
-#pragma unroll
-                    for (int t = 0; t < SETS; ++t) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            if (t > 0) p[e] = cut(p[e], 0xFFFF0000u);
-                            if (PACK > 1) p[e] = cut(p[e], cut1);
-                            if (PACK > 2) p[e] = cut(p[e], cut2);
-                        }
-                        w[x][t] = tops(p);
-                    }
-                }
-            }
-            float vsc[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vsc[e] = scale_of(y.vs[e >> 2], e & 3);
-            auto dims = [&](auto sel) __attribute__((always_inline)) {
-                constexpr int j = decltype(sel)::value;
-                u32x4 v0, v1;
-                values<j>(y, vsc, v0, v1);
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int t = 0; t < SETS; ++t) {
-                        acc[x][2 * j] = mfma(v0, w[x][t], acc[x][2 * j]);
-                        acc[x][2 * j + 1] = mfma(v1, w[x][t], acc[x][2 * j + 1]);
-                    }
-            };
-            dims(std::integral_constant<int, 0>());
-            dims(std::integral_constant<int, 1>());
-            dims(std::integral_constant<int, 2>());
-            dims(std::integral_constant<int, 3>());
-        };
-
-        if (n_mine > 0) {
-            begin_places();
-            if constexpr (NT == 1) {  // two steps in registers: one worked on, one on its way
-                Keys x, y;
-                auto request = [&](int n, Keys &z) __attribute__((always_inline)) {
-                    if (n >= n_mine) return;
-                    if (n % kAhead == 0 && n) turn_places(n);
-                    request_keys(at.held, n, z);
-                    request_values(at.held, n, z);
-                };
-                request(0, x);
-                for (int n = 0; n < n_mine; n += 2) {
-                    request(n + 1, y);
-                    attend(n, x, [] {});
-                    if (n + 1 >= n_mine) break;
-                    request(n + 2, x);
-                    attend(n + 1, y, [] {});
-                }
-            } else {
-                char *const stage = s_raw + wave * (kDepth * kStage);
-                uint32_t missing = 0;  // tiles that do not exist, two bits a step, the latest request's lowest
-                auto request = [&](int n) __attribute__((always_inline)) {
-                    if (n % kAhead == 0 && n) turn_places(n);
-                    const int id0 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead)), id1 = __builtin_amdgcn_readlane(at.held, 2 * (n % kAhead) + 1);
-                    missing = missing << 2 | (id0 < 0 ? 1u : 0u) | (id1 < 0 ? 2u : 0u);
-                    const uint8_t *t0 = a.c.data + (size_t)max(id0, 0) * kCacheTileBytes, *t1 = a.c.data + (size_t)max(id1, 0) * kCacheTileBytes;
-                    char *to_lds = stage + (n % kDepth) * kStage;
-                    lds_dma_stream<16>((t0 + k_at), to_lds);
-                    lds_dma_stream<16>((t1 + k_at), to_lds + 1024);
-                    lds_dma_stream<16>((t0 + kCacheV + 16 * lane), to_lds + 2048);
-                    lds_dma_stream<16>((t1 + kCacheV + 16 * lane), to_lds + 3 * 1024);
-                    lds_dma_stream<4>(((lane < 32 ? t0 : t1) + kCacheKS + 4 * (lane & 31)), to_lds + 4096);
-                };
-                for (int n = 0; n < min(kDepth, n_mine); ++n) request(n);
-                for (int n = 0; n < n_mine; ++n) {
-                    const int later = min(kDepth - 1, n_mine - 1 - n);  // steps requested after this one, five loads each
-                    if (later == 2) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
-                    else if (later == 1) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-                    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                    const char *from_lds = stage + (n % kDepth) * kStage;
-                    const uint32_t gone = missing >> (2 * later);
-                    Keys x;
-                    x.bad = (gone & 1 ? 0xFFFFu : 0u) | (gone & 2 ? 0xFFFF0000u : 0u);
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        x.k[b] = *(const u32x4 *)(from_lds + 1024 * b + 16 * lane);
-                        x.ks[b] = *(const uint8_t *)(from_lds + 4096 + 128 * b + (ks_at - kCacheKS));
-                    }
-                    attend(n, x, [&]() __attribute__((always_inline)) {
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) x.v[b][i] = *(const uint32_t *)(from_lds + 2048 + 1024 * b + (v_at - kCacheV) + 256 * i);
-                            x.vs[b] = *(const uint32_t *)(from_lds + 4096 + 128 * b + (vs_at - kCacheKS));
-                        }
-                    });
-                    if (n + kDepth < n_mine) {
-                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stage has been read)
-                        request(n + kDepth);
-                    }
-                }
-                __syncthreads();  // (the sums go where the stages were)
-            }
-        } else if constexpr (NT > 1) {
-            __syncthreads();
-        }
-
-        // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
-        const bool whole = now == u0 && stop == u1;
-        float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
-        const int d0 = 4 * (tid & 31);
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            if (x > 0 && R * x >= n_rows) break;
-            l[x] += __shfl_xor(l[x], 16);
-            l[x] += __shfl_xor(l[x], 32);
-            if (R * x + col_row < n_rows && term < PACK) {
-                float *r = s_acc[wave][c];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    *(f32x4 *)(r + 32 * g + 8 * i) = f32x4{acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
-                    *(f32x4 *)(r + 32 * g + 8 * i + 4) = f32x4{acc[x][4][i], acc[x][5][i], acc[x][6][i], acc[x][7][i]};
-                }
-                if (g == 0) {
-                    r[kD] = m[x];
-                    r[kD + 1] = l[x];
-                }
-            }
-            __syncthreads();
-            // (with one tile the reads of a thread's rows stand side by side, rows behind the last one read what lies there and write nothing: 24
-            // requests of mixed lengths 273 us, 281 row by row; with three tiles the registers for that are not there: drafts 64 us, 58)
-            constexpr int kPasses = NT == 1 ? (R + 2 * W - 1) / (2 * W) : 1;
-            for (int in0 = tid >> 5; in0 < (NT == 1 ? 2 * W : min(R, n_rows - R * x)); in0 += 2 * W * kPasses) {
-                f32x4 sum[kPasses];
-                float top[kPasses], all[kPasses];
-#pragma unroll
-                for (int pass = 0; pass < kPasses; ++pass) {
-                    const int in = min(in0 + 2 * W * pass, R - 1);
-                    float2 ml[W];
-#pragma unroll
-                    for (int w = 0; w < W; ++w) ml[w] = *(const float2 *)&s_acc[w][in][kD];
-                    top[pass] = kNoMax;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) top[pass] = fmaxf(top[pass], ml[w].x);
-                    sum[pass] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    all[pass] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        const float f = __builtin_amdgcn_exp2f(ml[w].x - top[pass]);
-                        f32x4 v = *(const f32x4 *)(s_acc[w][in] + d0);
-#pragma unroll
-                        for (int t = 1; t < PACK; ++t) v += *(const f32x4 *)(s_acc[w][in + t * R] + d0);
-                        sum[pass] += v * f;
-                        all[pass] += ml[w].y * f;
-                    }
-                }
-#pragma unroll
-                for (int pass = 0; pass < kPasses; ++pass) {
-                    const int in = in0 + 2 * W * pass, row = R * x + in;
-                    if (in >= R || row >= n_rows) continue;
-                    if (whole) {
-                        put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum[pass], top[pass], all[pass], alone);
-                    } else {
-                        float *r = record + (size_t)row * kRecord;
-                        *(f32x4 *)(r + d0) = sum[pass];
-                        if (d0 == 0) {
-                            r[kD] = top[pass];
-                            r[kD + 1] = all[pass];
-                        }
-                    }
-                }
-            }
-            __syncthreads();
-        }
+        few_part<W, PACK, NT, SETS, FORM, Q>(a, unit, s, h, n_rows, u0, u1, now, stop, alone, s_raw);
         if constexpr (FORM == kBoth) {
-            if (stop == u1) put_notes(a, unit, h, 0, n_rows, whole ? -1 : (int)pieces.owner(u0), alone);
+            if (stop == u1) put_notes(a, unit, h, 0, n_rows, now == u0 ? -1 : (int)pieces.owner(u0), alone);
         } else if (now > u0 && stop == u1) {
             note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows};
         }
@@ -875,6 +893,9 @@ constexpr int kRound = kWaves * 16;                  // keys of a round
 // requests: its own order 1852 us; operands two ahead 1826; weights beside products, 4 a product 1781, 3 1749, 2 1728, 1 1746.
 constexpr int kVector = 0x002, kMatrix = 0x008, kLdsRead = 0x100;
 constexpr int kAhead = 2, kWeightOps = 28, kBeside = 2;
+// Units of at most kRows rows among others, of all forms but Causal (where another launch takes them), are done as the few-query kernel does them; a
+// quantum of theirs is so many keys.
+constexpr int kFewQuantum = 4 * kQuantum;
 
 struct Chunks {  // how a request's row tiles lie in the flat work of one KV head
     int n_rows, tiles, step, quantum;  // step: rows of a tile
@@ -892,7 +913,8 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
             const int most = kChunkRows / a.G, n = n_rows / a.G;
             tiles = (n + most - 1) / most;
             step = (n + tiles - 1) / tiles * a.G;
-            if (step <= kRows * kWaves) quantum = 2 * kQuantum;
+            if (n_rows <= kRows) quantum = kFewQuantum;
+            else if (step <= kRows * kWaves) quantum = 2 * kQuantum;
         }
         tiles = (n_rows + step - 1) / step;
         const int middle = quanta(a, u, (tiles - 1) / 2);
@@ -926,7 +948,13 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
 
 template <int SETS, int FORM>
 __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend a) {
-    __shared__ u32x4 s_k[2][kWaves][4][64], s_v[2][kRound / kStep][8][64];
+    struct Operands {
+        u32x4 k[2][kWaves][4][64], v[2][kRound / kStep][8][64];
+    };
+    __shared__ __attribute__((aligned(16))) char s_raw[sizeof(Operands)];
+    static_assert(sizeof(Operands) >= few_lds(kWaves, 1), "a part of few rows has room");
+    auto &s_k = reinterpret_cast<Operands *>(s_raw)->k;
+    auto &s_v = reinterpret_cast<Operands *>(s_raw)->v;
     __shared__ unsigned s_before[kEntries + 1], s_wave[kWaves];
     __shared__ uint32_t s_flags[2][kWaves];  // of a tile of keys: bit 0: in no block, bit 1: values held as NaN were taken out
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -990,6 +1018,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const Chunks::Tile place = ch.at(a, unit, first + (unsigned)h * ch.per_head, now);
         const int all_rows = ch.n_rows, tile = __builtin_amdgcn_readfirstlane(place.tile);
         const unsigned u0 = place.u0, u1 = place.u1, stop = min(u1, end);
+        if constexpr (FORM != kCausal)
+            if (all_rows <= kRows) {
+                few_part<kWaves, 1, 1, SETS == 1 ? 2 : 3, FORM, kFewQuantum>(a, unit, s, h, all_rows, u0, u1, now, stop, alone, s_raw);
+                if constexpr (FORM == kBoth) {
+                    if (stop == u1) put_notes(a, unit, h, 0, all_rows, now == u0 ? -1 : (int)pieces.owner(u0), alone);
+                } else if (now > u0 && stop == u1) {
+                    note = {(int)pieces.owner(u0), h, unit.row0, 0, all_rows};
+                }
+                now = stop;
+                continue;
+            }
         const int base = ch.step * tile, n_rows = min(all_rows - base, ch.step);
         const int t_first = base / a.G, t_last = (base + n_rows - 1) / a.G;
         const int q0 = unit.low(a, t_first) / ch.quantum + (int)(now - u0);
@@ -1107,8 +1146,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                     request(held, n + 1);
                 }
                 lds_barrier();
+                if constexpr (decltype(count)::value == 0) continue;  // (no rows: this wave only converts)
                 // scores of the round's 64 keys (those behind the last one are masked)
-                constexpr int NX = decltype(count)::value, NB = kRound / 16;
+                constexpr int NX = decltype(count)::value ? decltype(count)::value : 1, NB = kRound / 16;
                 const int key0 = key_at + n * kRound;
                 f32x4 d[NX][NB];
 #pragma unroll
@@ -1237,7 +1277,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         } else {
             if (n_tiles > 2) run(std::integral_constant<int, kTiles>());
             else if (n_tiles > 1) run(std::integral_constant<int, 2>());
-            else run(std::integral_constant<int, 1>());
+            else if (n_tiles > 0) run(std::integral_constant<int, 1>());
+            else run(std::integral_constant<int, 0>());
         }
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1;
@@ -1517,16 +1558,6 @@ inline void launch_attend(CacheAttend a, hipStream_t stream) {
             cache_merge_kernel<1, FORM><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
         }
     }
-}
-
-constexpr long long kJoinRows = 4096;  // rows whose sums are joined by many threads each: few rows have many records
-inline void launch_both(const CacheAttend &a, hipStream_t stream) {
-    if (!a.many) launch_few<kWaves, kBoth>(a, stream);
-    else if (a.out_bf16) cache_chunk_kernel<1, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
-    else cache_chunk_kernel<3, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
-    const unsigned units = (unsigned)a.T * (unsigned)a.c.H;
-    if ((long long)units * a.G <= kJoinRows) cache_join_kernel<8><<<dim3(units, a.G), kMergeThreads, 0, stream>>>(a);
-    else cache_join_kernel<2><<<dim3(units, (a.G + 3) / 4), kMergeThreads, 0, stream>>>(a);
 }
 
 }  // namespace
