@@ -118,7 +118,7 @@ template <typename U> __host__ __device__ inline int quanta_of(const CacheAttend
 // What a unit costs beside its keys, in quanta of the kernel for many queries: it is that much longer in the flat work, behind its keys.  (Of Causal
 // nothing: its units are long there.  Six chunks of 250 to 500 queries on 500 to 1500 keys of their own and 32 K of a source, us: 0 1990, 2 1340, 3 1260, 4 1270; 48 times
 // four drafted tokens on up to 2 K and 8 K: 98, 89, 100, 105.)
-constexpr int chunk_setup(int form) { return form == kCross || form == kBoth ? 2 : 0; }
+__host__ __device__ inline int chunk_setup(int form, int rows) { return form == kCross || form == kBoth ? (rows <= kRows ? 1 : 2) : 0; }
 // The quanta of a request in the kernel for few queries, if it takes that many rows.
 template <int FORM> __host__ __device__ inline int few_quanta(const CacheAttend &a, const Unit<FORM> &u, int most_rows, int quantum) {
     const int q = u.queries(a);
@@ -891,7 +891,7 @@ constexpr int kChunkRows = kWaves * kTiles * kRows;  // rows of a workgroup
 constexpr int kRound = kWaves * 16;                  // keys of a round
 // What the compiler is asked for between the products (kinds of instructions, and how many).  A chunk of 2048 queries on 32 K keys, two
 // requests: its own order 1852 us; operands two ahead 1826; weights beside products, 4 a product 1781, 3 1749, 2 1728, 1 1746.
-constexpr int kVector = 0x002, kMatrix = 0x008, kLdsRead = 0x100;
+constexpr int kVector = 0x002, kScalar = 0x004, kMatrix = 0x008, kLdsRead = 0x100;
 constexpr int kAhead = 2, kWeightOps = 28, kBeside = 2;
 // Units of at most kRows rows among others, of all forms but Causal (where another launch takes them), are done as the few-query kernel does them; a
 // quantum of theirs is so many keys.
@@ -901,7 +901,7 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
     int n_rows, tiles, step, quantum;  // step: rows of a tile
     unsigned pair, single, per_head;   // quanta of a pair, of the middle tile of an odd number, of all
     template <int FORM> __host__ __device__ int quanta(const CacheAttend &a, const Unit<FORM> &u, int tile) const {
-        return quanta_of(a, u, step * tile / a.G, (min(step * (tile + 1), n_rows) - 1) / a.G, quantum) + chunk_setup(FORM);
+        return quanta_of(a, u, step * tile / a.G, (min(step * (tile + 1), n_rows) - 1) / a.G, quantum) + chunk_setup(FORM, n_rows);
     }
     template <int FORM> __host__ __device__ Chunks(const CacheAttend &a, const Unit<FORM> &u) : step(kChunkRows), quantum(kQuantum) {
         n_rows = u.queries(a) * a.G;
@@ -946,7 +946,9 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
     }
 };
 
-template <int SETS, int FORM>
+// TILES: of rows that a wave has room for; kTiles, or 2 where no unit has more than kSmallRows rows (decode steps behind a source).
+constexpr int kSmallRows = 2 * kWaves * kRows;
+template <int SETS, int FORM, int TILES>
 __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend a) {
     struct Operands {
         u32x4 k[2][kWaves][4][64], v[2][kRound / kStep][8][64];
@@ -1042,10 +1044,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const int key_at = q0 * ch.quantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
         // this lane's rows: columns of tiles wave + 4 x
-        int low[kTiles], high[kTiles], wave_low = 0, wave_high = to;
-        u32x4 qv[kTiles][4];
+        int low[TILES], high[TILES], wave_low = 0, wave_high = to;
+        u32x4 qv[TILES][4];
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
+        for (int x = 0; x < TILES; ++x) {
             const int row = base + min(kRows * (kWaves * x + wave) + c, n_rows - 1);
             sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
             const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
@@ -1053,13 +1055,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
         {  // keys that all rows of this wave see
-            const int r0 = min(kRows * wave, n_rows - 1), r1 = min(kRows * (kWaves * (kTiles - 1) + wave) + kRows - 1, n_rows - 1);
+            const int r0 = min(kRows * wave, n_rows - 1), r1 = min(kRows * (kWaves * (TILES - 1) + wave) + kRows - 1, n_rows - 1);
             wave_low = max(unit.sees_from(a, (base + r1) / a.G), from);
             wave_high = min(unit.sees_to((base + r0) / a.G), to);
         }
         if (FORM == kBoth && unit.side) {
-            wave_low = max(max(low[0], low[1]), low[2]);
-            wave_high = min(min(high[0], high[1]), high[2]);
+            wave_low = low[0];
+            wave_high = high[0];
+#pragma unroll
+            for (int x = 1; x < TILES; ++x) {
+                wave_low = max(wave_low, low[x]);
+                wave_high = min(wave_high, high[x]);
+            }
 #pragma unroll
             for (int d = 1; d < 16; d <<= 1) {
                 wave_low = max(wave_low, __shfl_xor(wave_low, d));
@@ -1076,35 +1083,43 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             if (id < 0 || id >= a.c.n_blocks) return -1;
             return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((int)t & tiles_mask));
         };
-        u32x4 kc, vc;  // this wave's codes of the next round
-        uint32_t ksc, vsc;
-        bool gone;
-        auto request = [&](int held, int n) __attribute__((always_inline)) {
-            const int id = __builtin_amdgcn_readlane(held, n & 63);
-            gone = id < 0;
-            const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
-            kc = *(const u32x4 *)(t + k_at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vc[i] = *(const uint32_t *)(t + v_at + 256 * i);
-            ksc = t[ks_at];
-            vsc = *(const uint32_t *)(t + vs_at);
+        struct Codes {  // this wave's of a round
+            u32x4 k, v;
+            uint32_t ks, vs;
+            bool gone;
         };
-        f32x4 acc[kTiles][8];
-        float m[kTiles], l[kTiles];
+        int held = rounds > 0 ? places(0) : -1;
+        auto request = [&](Codes &x, int n) __attribute__((always_inline)) {
+            if (n > 0 && (n & 63) == 0) held = places(n);
+            const int id = __builtin_amdgcn_readlane(held, n & 63);
+            x.gone = id < 0;
+            const uint8_t *t = a.c.data + (size_t)max(id, 0) * kCacheTileBytes;
+            x.k = *(const u32x4 *)(t + k_at);
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
+            for (int i = 0; i < 4; ++i) x.v[i] = *(const uint32_t *)(t + v_at + 256 * i);
+            x.ks = t[ks_at];
+            x.vs = *(const uint32_t *)(t + vs_at);
+        };
+        f32x4 acc[TILES][8];
+        float m[TILES], l[TILES];
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
             m[x] = kNoMax;
             l[x] = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[x][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const int n_tiles = (n_rows - kRows * wave + kRows * kWaves - 1) / (kRows * kWaves);  // of this wave (may be 0 or less)
-        int held = rounds > 0 ? places(0) : -1;
-        if (rounds > 0) request(held, 0);
-        // the rounds of a wave with NX tiles of rows, without a branch on the tile between the products
+        // the rounds of a wave with NX tiles of rows, without a branch on the tile between the products; codes are asked for a round ahead
         auto run = [&](auto count) __attribute__((always_inline)) {
+            Codes codes;
+            if (rounds > 0) request(codes, 0);
             for (int n = 0; n < rounds; ++n) {
                 const int buf = n & 1;
+                const u32x4 kc = codes.k, vc = codes.v;
+                const uint32_t ksc = codes.ks;
+                uint32_t vsc = codes.vs;
+                const bool gone = codes.gone;
                 {  // this wave's keys of the round become operands
                     const int key0 = key_at + n * kRound + 16 * wave;
                     bool nan = false;
@@ -1141,37 +1156,66 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                     dims(std::integral_constant<int, 2>());
                     dims(std::integral_constant<int, 3>());
                 }
-                if (n + 1 < rounds) {
-                    if (((n + 1) & 63) == 0) held = places(n + 1);
-                    request(held, n + 1);
-                }
+                if (n + 1 < rounds) request(codes, n + 1);
                 lds_barrier();
                 if constexpr (decltype(count)::value == 0) continue;  // (no rows: this wave only converts)
                 // scores of the round's 64 keys (those behind the last one are masked)
                 constexpr int NX = decltype(count)::value ? decltype(count)::value : 1, NB = kRound / 16;
+                // of one or two tiles of rows, where a product is soon done: operands read side by side, while those before them are used
+                constexpr int GROUP = FORM == kCausal || NX > 2 ? 0 : NX == 1 ? 4 : 2;
                 const int key0 = key_at + n * kRound;
                 f32x4 d[NX][NB];
+                uint32_t flags = 0;
+                auto read_flags = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
+                    for (int b = 0; b < NB; ++b) flags |= s_flags[buf][b] << (2 * b);
+                };
+                if constexpr (GROUP > 0) read_flags();
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int x = 0; x < NX; ++x) d[x][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                // N operands, read(i), each used by use(i, operand)
+                auto grouped = [&](auto total, auto read, auto use) __attribute__((always_inline)) {
+                    constexpr int N = decltype(total)::value, G = GROUP ? GROUP : 1;
+                    u32x4 o[2][G];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const u32x4 k = s_k[buf][b][j][lane];
+                    for (int i = 0; i < G; ++i) o[0][i] = read(i);
 #pragma unroll
-                        for (int x = 0; x < NX; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                    for (int at = 0; at < N; at += G) {
+                        const int in = at / G & 1;
+#pragma unroll
+                        for (int i = 0; i < G; ++i)
+                            if (at + G < N) o[in ^ 1][i] = read(at + G + i);
+                        __builtin_amdgcn_sched_barrier(kScalar | kVector);  // (these may pass, reads of LDS may not)
+#pragma unroll
+                        for (int i = 0; i < G; ++i) use(at + i, o[in][i]);
+                    }
+                };
+                if constexpr (GROUP > 0) {
+                    grouped(std::integral_constant<int, 4 * NB>(), [&](int i) { return s_k[buf][i >> 2][i & 3][lane]; },
+                            [&](int i, const u32x4 &k) {
+#pragma unroll
+                                for (int x = 0; x < NX; ++x) d[x][i >> 2] = mfma(k, qv[x][i & 3], d[x][i >> 2]);
+                            });
+                } else {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const u32x4 k = s_k[buf][b][j][lane];
+#pragma unroll
+                            for (int x = 0; x < NX; ++x) d[x][b] = mfma(k, qv[x][j], d[x][b]);
+                        }
+                    // (operands are read kAhead ahead of their products)
+                    __builtin_amdgcn_sched_group_barrier(kLdsRead, kAhead, 0);
+#pragma unroll
+                    for (int i = 0; i < 4 * NB; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(kMatrix, NX, 0);
+                        if (i + kAhead < 4 * NB) __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
                     }
                 }
-                // (operands are read kAhead ahead of their products)
-                __builtin_amdgcn_sched_group_barrier(kLdsRead, kAhead, 0);
-#pragma unroll
-                for (int i = 0; i < 4 * NB; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(kMatrix, NX, 0);
-                    if (i + kAhead < 4 * NB) __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
-                }
-                uint32_t flags = 0;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) flags |= s_flags[buf][b] << (2 * b);
+                if constexpr (GROUP == 0) read_flags();
                 flags = (uint32_t)__builtin_amdgcn_readfirstlane((int)flags);
                 if (key0 < wave_low || key0 + kRound > wave_high || flags != 0) {
 #pragma unroll
@@ -1185,9 +1229,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                                 if (none || key < low[x] || key >= high[x]) d[x][b][i] = -INFINITY;
                         }
                     if (flags & 0xAAu) {
-                        float nan[kTiles] = {};
+                        float nan[TILES] = {};
                         for (int step = 0; step < kRound / kStep; ++step)
-                            find_nan<kTiles>(a, table, h, key0 + step * kStep, from, to, g, low, high, nan);
+                            find_nan<TILES>(a, table, h, key0 + step * kStep, from, to, g, low, high, nan);
 #pragma unroll
                         for (int x = 0; x < NX; ++x)
 #pragma unroll
@@ -1217,9 +1261,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                     }
                 }
                 // weights and the value product, without a branch, so that the one's instructions fill the other's time
-#pragma unroll
-                for (int step = 0; step < kRound / kStep; ++step) {
-                    u32x4 w[NX][SETS];
+                u32x4 w[NX][SETS];
+                auto weights = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
                     for (int x = 0; x < NX; ++x) {
                         float p[8];
@@ -1241,14 +1284,26 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                             }
                         }
                     }
+                };
+                auto product = [&](int j, const u32x4 &v) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const u32x4 v = s_v[buf][step][j][lane];
+                    for (int x = 0; x < NX; ++x)
 #pragma unroll
-                        for (int x = 0; x < NX; ++x)
+                        for (int t = 0; t < SETS; ++t) acc[x][j] = mfma(v, w[x][t], acc[x][j]);
+                };
+                if constexpr (GROUP > 0) {
+                    grouped(std::integral_constant<int, 8 * kRound / kStep>(), [&](int i) { return s_v[buf][i >> 3][i & 7][lane]; },
+                            [&](int i, const u32x4 &v) {
+                                if ((i & 7) == 0) weights(i >> 3);
+                                product(i & 7, v);
+                            });
+                    continue;
+                }
 #pragma unroll
-                            for (int t = 0; t < SETS; ++t) acc[x][j] = mfma(v, w[x][t], acc[x][j]);
-                    }
+                for (int step = 0; step < kRound / kStep; ++step) {
+                    weights(step);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) product(j, s_v[buf][step][j][lane]);
                 }
                 // the order of the products: the first step's weights (kWeightOps a tile); its products, beside each of which kBeside
                 // instructions of the second step's weights go; the second step's products
@@ -1272,19 +1327,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         };
         // (a wave without rows converts all the same; its one tile is not written)
         if constexpr (FORM == kCausal) {
-            if (n_tiles > 1) run(std::integral_constant<int, kTiles>());
+            if (n_tiles > 1) run(std::integral_constant<int, TILES>());
             else run(std::integral_constant<int, 1>());
         } else {
-            if (n_tiles > 2) run(std::integral_constant<int, kTiles>());
-            else if (n_tiles > 1) run(std::integral_constant<int, 2>());
-            else if (n_tiles > 0) run(std::integral_constant<int, 1>());
-            else run(std::integral_constant<int, 0>());
+            if constexpr (TILES > 2) {
+                if (n_tiles > 2) run(std::integral_constant<int, TILES>());
+                else if (n_tiles > 1) run(std::integral_constant<int, 2>());
+                else if (n_tiles > 0) run(std::integral_constant<int, 1>());
+                else run(std::integral_constant<int, 0>());
+            } else {
+                if (n_tiles > 1) run(std::integral_constant<int, 2>());
+                else if (n_tiles > 0) run(std::integral_constant<int, 1>());
+                else run(std::integral_constant<int, 0>());
+            }
         }
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1;
         float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
+        for (int x = 0; x < TILES; ++x) {
             const int in = kRows * (kWaves * x + wave) + c, row = base + in;
             l[x] += __shfl_xor(l[x], 16);
             l[x] += __shfl_xor(l[x], 32);
@@ -1537,6 +1598,17 @@ inline void launch_few_merge(const CacheAttend &a, hipStream_t stream) {
 }
 
 template <int FORM>
+inline void launch_chunks(const CacheAttend &a, int groups, hipStream_t stream) {
+    if constexpr (FORM != kCausal)
+        if (a.rows <= kSmallRows) {
+            if (a.out_bf16) cache_chunk_kernel<1, FORM, 2><<<groups, kWaves * 64, 0, stream>>>(a);
+            else cache_chunk_kernel<3, FORM, 2><<<groups, kWaves * 64, 0, stream>>>(a);
+            return;
+        }
+    if (a.out_bf16) cache_chunk_kernel<1, FORM, kTiles><<<groups, kWaves * 64, 0, stream>>>(a);
+    else cache_chunk_kernel<3, FORM, kTiles><<<groups, kWaves * 64, 0, stream>>>(a);
+}
+template <int FORM>
 inline void launch_attend(CacheAttend a, hipStream_t stream) {
     float *const part = a.part;
     for (a.first = 0; a.first < a.S; a.first += kEntries) {
@@ -1553,8 +1625,7 @@ inline void launch_attend(CacheAttend a, hipStream_t stream) {
             a.rows = chunk_rows(a);
             a.notes = (MergeNote *)part;
             a.part = (float *)(a.notes + a.many_groups);
-            if (a.out_bf16) cache_chunk_kernel<1, FORM><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
-            else cache_chunk_kernel<3, FORM><<<a.many_groups, kWaves * 64, 0, stream>>>(a);
+            launch_chunks<FORM>(a, a.many_groups, stream);
             cache_merge_kernel<1, FORM><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
         }
     }

@@ -103,8 +103,7 @@ void launch_cache_cross(const CacheAttend &a, hipStream_t stream) { launch_atten
 constexpr long long kJoinRows = 4096;  // rows whose sums are joined by many threads each: few rows have many records
 static void launch_both(const CacheAttend &a, hipStream_t stream) {
     if (!a.many) launch_few<kWaves, kBoth>(a, stream);
-    else if (a.out_bf16) cache_chunk_kernel<1, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
-    else cache_chunk_kernel<3, kBoth><<<a.groups, kWaves * 64, 0, stream>>>(a);
+    else launch_chunks<kBoth>(a, a.groups, stream);
     const unsigned units = (unsigned)a.T * (unsigned)a.c.H;
     if ((long long)units * a.G <= kJoinRows) cache_join_kernel<8><<<dim3(units, a.G), kMergeThreads, 0, stream>>>(a);
     else cache_join_kernel<2><<<dim3(units, (a.G + 3) / 4), kMergeThreads, 0, stream>>>(a);
