@@ -181,12 +181,10 @@ __device__ inline void put_query(const CacheAttend &a, bool side, int row0, int 
         put_row(a, at, d0, sum, top, total);
     }
 }
-// Of Both: a request without a source, that is a row of the table, not its own.
-template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, bool side, int s) {
-    if constexpr (FORM != kBoth) return false;
-    if (side) return false;
-    const int to = __builtin_amdgcn_readfirstlane(a.source[s]);
-    return (unsigned)to >= (unsigned)a.S || to == s;
+// Of Both: a request without a source, that is a row of the table, not its own.  source: source_at's, asked for early and looked at late.
+template <int FORM> __device__ inline int source_at(const CacheAttend &a, int s) { return FORM == kBoth ? a.source[s] : 0; }
+template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, bool side, int s, int source) {
+    return FORM == kBoth && !side && ((unsigned)source >= (unsigned)a.S || source == s);
 }
 // Of Both, by the workgroup that a unit ends in: where each query's sums are.  rows: of the unit, from the request's row `base` on.
 __device__ inline void put_notes(const CacheAttend &a, const Unit<kBoth> &u, int h, int base, int rows, int first, bool alone) {
@@ -395,7 +393,7 @@ constexpr int few_lds(int W, int NT) {
 // s_raw before and after.
 template <int W, int PACK, int NT, int SETS, int FORM, int QUANTUM>
 __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend &a, const Unit<FORM> &unit, int s, int h, int n_rows, unsigned u0, unsigned u1, unsigned now,
-                                                               unsigned stop, bool alone, char *s_raw) {
+                                                               unsigned stop, int source, char *s_raw) {
     constexpr bool LIST = FORM == kListed;
     static_assert(PACK == 1 || NT == 1, "terms share the columns of one tile");
     constexpr int R = kRows / PACK;  // rows in a tile of columns
@@ -416,30 +414,34 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
     int all_low = max(unit.sees_from(a, t_last), from), all_high = min(unit.sees_to(0), to);
     int low[NT], high[NT];
     u32x4 qv[NT][4];  // right operand of step j: dims 32 g + 8 j .. + 8 of the column's row
+    auto begin_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < NT; ++x) {
-        const int row = min(R * x + col_row, n_rows - 1);
-        sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
-        const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
+        for (int x = 0; x < NT; ++x) {
+            const int row = min(R * x + col_row, n_rows - 1);
+            sees<FORM>(a, unit, FORM == kBoth ? a.seq_len[s] : 0, row, from, to, low[x], high[x]);
+            const bf16_t *p = query_at<FORM>(a, unit.side, unit.row0, h, row) + 32 * g;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
-    }
-    if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order)
-        all_low = low[0];
-        all_high = high[0];
-#pragma unroll
-        for (int x = 1; x < NT; ++x) {
-            all_low = max(all_low, low[x]);
-            all_high = min(all_high, high[x]);
+            for (int j = 0; j < 4; ++j) qv[x][j] = *(const u32x4 *)(p + 8 * j);
         }
+        if (FORM == kBoth && unit.side) {  // (a source's queries stand in no order)
+            all_low = low[0];
+            all_high = high[0];
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
-            all_low = max(all_low, __shfl_xor(all_low, d));
-            all_high = min(all_high, __shfl_xor(all_high, d));
+            for (int x = 1; x < NT; ++x) {
+                all_low = max(all_low, low[x]);
+                all_high = min(all_high, high[x]);
+            }
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) {
+                all_low = max(all_low, __shfl_xor(all_low, d));
+                all_high = min(all_high, __shfl_xor(all_high, d));
+            }
+            all_low = __builtin_amdgcn_readfirstlane(all_low);
+            all_high = __builtin_amdgcn_readfirstlane(all_high);
         }
-        all_low = __builtin_amdgcn_readfirstlane(all_low);
-        all_high = __builtin_amdgcn_readfirstlane(all_high);
-    }
+    };
+    constexpr bool kPlacesFirst = FORM == kCross || FORM == kBoth;  // (beside the trips for the list and the queries)
+    if constexpr (!kPlacesFirst) begin_rows();
     const int step0 = (q0 + (int)(now - u0)) * (QUANTUM / kStep);  // the wave's steps: step0 + wave + W n
     const int n_mine = to > from ? max((to - kStep * (step0 + wave) + Q - 1) / Q, 0) : 0;
     const int *table = a.table + (size_t)s * a.max_blocks;
@@ -489,6 +491,10 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
             at.held = tile_of(n);
         }
     };
+    if constexpr (kPlacesFirst) {
+        if (n_mine > 0) begin_places();
+        begin_rows();
+    }
     // step n of this wave: key codes, value codes
     auto request_keys = [&](int held, int n, Keys &x) __attribute__((always_inline)) {
         x.bad = 0;
@@ -634,7 +640,7 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
     };
 
     if (n_mine > 0) {
-        begin_places();
+        if constexpr (!kPlacesFirst) begin_places();
         if constexpr (NT == 1) {  // two steps in registers: one worked on, one on its way
             Keys x, y;
             auto request = [&](int n, Keys &z) __attribute__((always_inline)) {
@@ -701,7 +707,7 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
     }
 
     // the waves' sums, and the terms', meet in LDS; 32 threads to a row, four dims each
-    const bool whole = now == u0 && stop == u1;
+    const bool whole = now == u0 && stop == u1, alone = is_alone<FORM>(a, unit.side, s, source);
     float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
     const int d0 = 4 * (tid & 31);
 #pragma unroll
@@ -855,15 +861,15 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         const unsigned stop = min(u1, end);
         const Unit<FORM> unit(a, s, h, std::true_type());
         if constexpr (FORM == kBoth) s = unit.side ? s : s - a.S;  // (from here on: the row of the table)
-        const bool alone = is_alone<FORM>(a, unit.side, s);
+        const int source = source_at<FORM>(a, s);
         const int n_rows = unit.queries(a) * a.G;
         if (!LIST && (n_rows <= 0 || n_rows > NT * R)) {  // (equal units: nothing to do here, or the other kernel's)
             now = stop;
             continue;
         }
-        few_part<W, PACK, NT, SETS, FORM, Q>(a, unit, s, h, n_rows, u0, u1, now, stop, alone, s_raw);
+        few_part<W, PACK, NT, SETS, FORM, Q>(a, unit, s, h, n_rows, u0, u1, now, stop, source, s_raw);
         if constexpr (FORM == kBoth) {
-            if (stop == u1) put_notes(a, unit, h, 0, n_rows, now == u0 ? -1 : (int)pieces.owner(u0), alone);
+            if (stop == u1) put_notes(a, unit, h, 0, n_rows, now == u0 ? -1 : (int)pieces.owner(u0), is_alone<FORM>(a, unit.side, s, source));
         } else if (now > u0 && stop == u1) {
             note = {(int)pieces.owner(u0), h, unit.row0, 0, n_rows};
         }
@@ -1014,7 +1020,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             }
         const Unit<FORM> unit(a, s, 0, std::true_type());
         if constexpr (FORM == kBoth) s = unit.side ? s : s - a.S;  // (from here on: the row of the table)
-        const bool alone = is_alone<FORM>(a, unit.side, s);
+        const int source = source_at<FORM>(a, s);
         const Chunks ch(a, unit);
         const int h = __builtin_amdgcn_readfirstlane((int)((now - first) / ch.per_head));
         const Chunks::Tile place = ch.at(a, unit, first + (unsigned)h * ch.per_head, now);
@@ -1022,9 +1028,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         const unsigned u0 = place.u0, u1 = place.u1, stop = min(u1, end);
         if constexpr (FORM != kCausal)
             if (all_rows <= kRows) {
-                few_part<kWaves, 1, 1, SETS == 1 ? 2 : 3, FORM, kFewQuantum>(a, unit, s, h, all_rows, u0, u1, now, stop, alone, s_raw);
+                few_part<kWaves, 1, 1, SETS == 1 ? 2 : 3, FORM, kFewQuantum>(a, unit, s, h, all_rows, u0, u1, now, stop, source, s_raw);
                 if constexpr (FORM == kBoth) {
-                    if (stop == u1) put_notes(a, unit, h, 0, all_rows, now == u0 ? -1 : (int)pieces.owner(u0), alone);
+                    if (stop == u1) put_notes(a, unit, h, 0, all_rows, now == u0 ? -1 : (int)pieces.owner(u0), is_alone<FORM>(a, unit.side, s, source));
                 } else if (now > u0 && stop == u1) {
                     note = {(int)pieces.owner(u0), h, unit.row0, 0, all_rows};
                 }
@@ -1043,6 +1049,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         }
         const int key_at = q0 * ch.quantum;  // of the first round
         const int rounds = to > from ? (to - key_at + kRound - 1) / kRound : 0;
+        const int *table = a.table + (size_t)s * a.max_blocks;
+        auto places = [&](int n0) __attribute__((always_inline)) -> int {  // this wave's tile of round n0 + l
+            const long long t = (long long)(key_at >> 4) + (long long)(n0 + lane) * kWaves + wave;
+            if (t * 16 >= to) return -1;
+            const int id = table[t >> a.c.tile_shift];
+            if (id < 0 || id >= a.c.n_blocks) return -1;
+            return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((int)t & tiles_mask));
+        };
+        int held = -1;
+        if constexpr (FORM != kCausal) held = rounds > 0 ? places(0) : -1;  // (beside the trips for the list and the queries)
         // this lane's rows: columns of tiles wave + 4 x
         int low[TILES], high[TILES], wave_low = 0, wave_high = to;
         u32x4 qv[TILES][4];
@@ -1075,20 +1091,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             wave_low = __builtin_amdgcn_readfirstlane(wave_low);
             wave_high = __builtin_amdgcn_readfirstlane(wave_high);
         }
-        const int *table = a.table + (size_t)s * a.max_blocks;
-        auto places = [&](int n0) __attribute__((always_inline)) -> int {  // this wave's tile of round n0 + l
-            const long long t = (long long)(key_at >> 4) + (long long)(n0 + lane) * kWaves + wave;
-            if (t * 16 >= to) return -1;
-            const int id = table[t >> a.c.tile_shift];
-            if (id < 0 || id >= a.c.n_blocks) return -1;
-            return (int)((((unsigned)id * a.c.H + h) << a.c.tile_shift) + ((int)t & tiles_mask));
-        };
         struct Codes {  // this wave's of a round
             u32x4 k, v;
             uint32_t ks, vs;
             bool gone;
         };
-        int held = rounds > 0 ? places(0) : -1;
+        if constexpr (FORM == kCausal) held = rounds > 0 ? places(0) : -1;
         auto request = [&](Codes &x, int n) __attribute__((always_inline)) {
             if (n > 0 && (n & 63) == 0) held = places(n);
             const int id = __builtin_amdgcn_readlane(held, n & 63);
@@ -1342,7 +1350,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             }
         }
         lds_barrier();  // (the last operands have been used: the next part writes others)
-        const bool whole = now == u0 && stop == u1;
+        const bool whole = now == u0 && stop == u1, alone = is_alone<FORM>(a, unit.side, s, source);
         float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
@@ -1365,7 +1373,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             }
         }
         if constexpr (FORM == kBoth) {
-            if (stop == u1) put_notes(a, unit, h, base, n_rows, whole ? -1 : (int)pieces.owner(u0), alone);
+            if (stop == u1) put_notes(a, unit, h, base, n_rows, whole ? -1 : (int)pieces.owner(u0), is_alone<FORM>(a, unit.side, s, source));
         } else if (now > u0 && stop == u1) {
             note = {(int)pieces.owner(u0), h, unit.row0, base, FORM == kCausal ? all_rows : min(all_rows, base + n_rows)};
         }
