@@ -253,56 +253,76 @@ __device__ inline uint32_t round2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// A wave takes four consecutive tokens, 16 lanes of 8 dims to a row, and PER heads of them: of the queries, then the keys, then the values.
-// Pair i of a row's rotated dims (half apart, or neighbours) becomes (x cos - y sin, x sin + y cos), products and sums each rounded to
+// A wave takes four consecutive tokens, 16 lanes of 8 dims to a row, and `span` heads of them, PER at a time: of the queries, then the keys, then the
+// values.  Pair i of a row's rotated dims (half apart, or neighbours) becomes (x cos - y sin, x sin + y cos), products and sums each rounded to
 // 32 bits; a query is then rounded to bf16 and a key held, so either is rounded to fewer bits once.
 template <int PER>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int chunks) {
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int chunks, int span) {
     const int lane = threadIdx.x & 63, i = lane & 15, r = lane >> 4;
     const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int chunk = (int)(unit % chunks);
-    const long long t0 = unit / chunks * 4;
+    const int chunk = __builtin_amdgcn_readfirstlane((int)(unit % chunks)), t0 = __builtin_amdgcn_readfirstlane((int)min(unit / chunks * 4, (long long)a.n_tokens));
     if (t0 >= a.n_tokens) return;
-    const int t = (int)min(t0 + r, (long long)a.n_tokens - 1), n = a.n_requests;
-    const int pair_lanes = a.half >> 3, head0 = chunk * PER;
+    const int t = (int)min((long long)t0 + r, (long long)a.n_tokens - 1), n = a.n_requests;
+    const int pair_lanes = a.half >> 3, head0 = chunk * span, heads = a.q_heads + 2 * a.c.H, head1 = min(head0 + span, heads);
     const bool turned = i < 2 * pair_lanes, first = i < pair_lanes;
     const int other = a.neighbours || !turned ? i : first ? i + pair_lanes : i - pair_lanes;
-    uint4 w[PER], u[PER];
+    struct Rows {
+        uint4 w[PER], u[PER];  // a row's eight dims, and those that they are paired with
+    };
+    auto request = [&](int c0, Rows &x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int c = head0 + j;
-        const bf16_t *x = nullptr;
-        if (c < a.q_heads) x = a.q + t * a.q_stride + (long long)c * kD;
-        else if (c < a.q_heads + a.c.H) x = a.k + t * a.k_stride + (long long)(c - a.q_heads) * kD;
-        else if (c < a.q_heads + 2 * a.c.H) x = a.v + t * a.v_stride + (long long)(c - a.q_heads - a.c.H) * kD;
-        w[j] = u[j] = make_uint4(0, 0, 0, 0);
-        if (x) {
-            w[j] = *(const uint4 *)(x + 8 * i);
-            if (a.half && !a.neighbours && c < a.q_heads + a.c.H) u[j] = *(const uint4 *)(x + 8 * other);
+        for (int j = 0; j < PER; ++j) {
+            const int c = c0 + j;
+            if (c >= head1) break;
+            const bf16_t *p;
+            if (c < a.q_heads) p = a.q + t * a.q_stride + (long long)c * kD;
+            else if (c < a.q_heads + a.c.H) p = a.k + t * a.k_stride + (long long)(c - a.q_heads) * kD;
+            else p = a.v + t * a.v_stride + (long long)(c - a.q_heads - a.c.H) * kD;
+            x.w[j] = *(const uint4 *)(p + 8 * i);
+            if (a.half && !a.neighbours && c < a.q_heads + a.c.H) x.u[j] = *(const uint4 *)(p + 8 * other);
         }
-    }
-    // The request of each of the four tokens: the number of requests that end at or before it, 64 starts looked at in a trip.
-    int owner[4] = {0, 0, 0, 0}, step = 1;
-    while ((long long)step * 64 < n) step *= 64;
-    for (; step; step /= 64) {
+    };
+    Rows x;
+    request(head0, x);
+    // The request of each of the four tokens: the number of requests that end at or before it.  Up to 64 requests lie on the lanes, their lengths and
+    // sources beside them; else 64 starts are looked at in a trip.
+    int s, end, len, source, source_len;
+    if (n <= 64) {
+        const int at = min(lane, n - 1), start = a.query_start[at + 1], length = a.seq_len[at], named = a.source ? a.source[at] : -1;
+        int owner[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const long long e = owner[k] + (long long)(lane + 1) * step;
-            const bool before = e <= n && a.query_start[e] <= t0 + k;
-            owner[k] += (int)__popcll(__ballot(before)) * step;
+        for (int k = 0; k < 4; ++k) owner[k] = (int)__popcll(__ballot(lane < n && start <= t0 + k));
+        s = r == 0 ? owner[0] : r == 1 ? owner[1] : r == 2 ? owner[2] : owner[3];
+        const int safe = min(s, n - 1);
+        end = __shfl(start, safe);
+        len = __shfl(length, safe);
+        source = __shfl(named, safe);
+        source_len = __shfl(length, (unsigned)source < (unsigned)n ? source : 0);
+    } else {
+        int owner[4] = {0, 0, 0, 0}, step = 1;
+        while ((long long)step * 64 < n) step *= 64;
+        for (; step; step /= 64) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const long long e = owner[k] + (long long)(lane + 1) * step;
+                const bool before = e <= n && a.query_start[e] <= t0 + k;
+                owner[k] += (int)__popcll(__ballot(before)) * step;
+            }
         }
+        s = r == 0 ? owner[0] : r == 1 ? owner[1] : r == 2 ? owner[2] : owner[3];
+        const int safe = min(s, n - 1);
+        end = a.query_start[safe + 1];
+        len = a.seq_len[safe];
+        source = a.source ? a.source[safe] : -1;
+        source_len = a.seq_len[(unsigned)source < (unsigned)n ? source : 0];
     }
-    const int s = r == 0 ? owner[0] : r == 1 ? owner[1] : r == 2 ? owner[2] : owner[3];
     const bool real = t0 + r < a.n_tokens && s < n;
-    const int s_safe = min(s, n - 1);
-    const int end = min(max(a.query_start[s_safe + 1], 0), a.n_tokens), len = max(a.seq_len[s_safe], 0);
-    const int source = a.source ? a.source[s_safe] : -1;
-    const long long place = (long long)len - end + t;
-    const long long position = place + ((unsigned)source < (unsigned)n && source != s ? max(a.seq_len[(unsigned)source < (unsigned)n ? source : 0], 0) : 0);
+    const long long place = (long long)max(len, 0) - min(max(end, 0), a.n_tokens) + t;
+    const long long position = place + ((unsigned)source < (unsigned)n && source != s ? max(source_len, 0) : 0);
     const bool known = real && (!a.half || (position >= 0 && position < a.n_positions));
     const int tokens_shift = a.c.tile_shift + 4;
     const bool in_row = known && place >= 0 && place < (long long)a.max_blocks << tokens_shift;
-    const int block = in_row ? a.table[(size_t)s_safe * a.max_blocks + (size_t)(place >> tokens_shift)] : -1;
+    const int block = in_row ? a.table[(size_t)min(s, n - 1) * a.max_blocks + (size_t)(place >> tokens_shift)] : -1;
     float cs[8], sn[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -322,45 +342,49 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int ch
     }
     const bool held = in_row && block >= 0 && block < a.c.n_blocks;
     const int at = (int)place & ((16 << a.c.tile_shift) - 1), row = at & 15;
+    for (int c0 = head0; c0 < head1; c0 += PER) {
+        const Rows y = x;
+        if (c0 + PER < head1) request(c0 + PER, x);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
+        for (int j = 0; j < PER; ++j) {
 #pragma clang fp contract(off)
-        const int c = head0 + j;
-        if (c >= a.q_heads + 2 * a.c.H) break;
-        float f[8];
-        widen8(w[j], f);
-        if (a.half && turned && c < a.q_heads + a.c.H) {
-            if (a.neighbours) {
+            const int c = c0 + j;
+            if (c >= head1) break;
+            float f[8];
+            widen8(y.w[j], f);
+            if (a.half && turned && c < a.q_heads + a.c.H) {
+                if (a.neighbours) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = f[2 * e], y = f[2 * e + 1];
-                    const float xc = x * cs[e], ys = y * sn[e], xs = x * sn[e], yc = y * cs[e];
-                    f[2 * e] = xc - ys;
-                    f[2 * e + 1] = xs + yc;
-                }
-            } else {
-                float o[8];
-                widen8(u[j], o);
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = f[2 * e], q = f[2 * e + 1];
+                        const float pc = p * cs[e], qs = q * sn[e], ps = p * sn[e], qc = q * cs[e];
+                        f[2 * e] = pc - qs;
+                        f[2 * e + 1] = ps + qc;
+                    }
+                } else {
+                    float o[8];
+                    widen8(y.u[j], o);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float mine = f[e] * cs[e], theirs = o[e] * sn[e];
-                    f[e] = first ? mine - theirs : theirs + mine;
+                    for (int e = 0; e < 8; ++e) {
+                        const float mine = f[e] * cs[e], theirs = o[e] * sn[e];
+                        f[e] = first ? mine - theirs : theirs + mine;
+                    }
                 }
             }
+            if (c < a.q_heads) {
+                if (known)
+                    *(uint4 *)(a.q_out + t * a.q_out_stride + (long long)c * kD + 8 * i) =
+                        make_uint4(round2(f[0], f[1]), round2(f[2], f[3]), round2(f[4], f[5]), round2(f[6], f[7]));
+                continue;
+            }
+            const int side = c >= a.q_heads + a.c.H ? 1 : 0, h = c - a.q_heads - side * a.c.H;
+            int scale;
+            const uint32_t code = hold(f, scale);
+            if (!held) continue;
+            uint8_t *tile = a.c.data + ((((size_t)block * a.c.H + h) << a.c.tile_shift) + (at >> 4)) * kCacheTileBytes;
+            *(uint32_t *)(tile + kCacheV * side + 64 * row + 4 * i) = code;
+            if ((i & 3) == 0) tile[kCacheKS + 64 * side + cache_scale_byte(row, i >> 2)] = (uint8_t)scale;
         }
-        if (c < a.q_heads) {
-            if (known)
-                *(uint4 *)(a.q_out + t * a.q_out_stride + (long long)c * kD + 8 * i) =
-                    make_uint4(round2(f[0], f[1]), round2(f[2], f[3]), round2(f[4], f[5]), round2(f[6], f[7]));
-            continue;
-        }
-        const int side = c >= a.q_heads + a.c.H ? 1 : 0, h = c - a.q_heads - side * a.c.H;
-        int scale;
-        const uint32_t code = hold(f, scale);
-        if (!held) continue;
-        uint8_t *tile = a.c.data + ((((size_t)block * a.c.H + h) << a.c.tile_shift) + (at >> 4)) * kCacheTileBytes;
-        *(uint32_t *)(tile + kCacheV * side + 64 * row + 4 * i) = code;
-        if ((i & 3) == 0) tile[kCacheKS + 64 * side + cache_scale_byte(row, i >> 2)] = (uint8_t)scale;
     }
 }
 
@@ -436,16 +460,18 @@ void launch_cache_write(const CacheDims &c, const bf16_t *k, const bf16_t *v, lo
     cache_write_kernel<<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(c, k, v, k_stride, v_stride, slots, n_tokens);
 }
 
+// Heads of a wave, and how many it asks for at a time.  Two prompts of 16 K tokens, 32 query and 8 KV heads, with the read of the cache behind it, us: 4 and 4
+// heads 238, 8 and 4 180, 16 and 4 195, 48 and 4 206, 16 and 8 206, 16 and 2 202.  Few rows: a head a wave.
 void launch_cache_append(const CacheAppend &a, hipStream_t stream) {
     const int heads = a.q_heads + 2 * a.c.H;
     const long long quads = ((long long)a.n_tokens + 3) / 4;
     if (quads * heads <= 8192) {
-        cache_append_kernel<1><<<(unsigned)((quads * heads + 3) / 4), 256, 0, stream>>>(a, heads);
+        cache_append_kernel<1><<<(unsigned)((quads * heads + 3) / 4), 256, 0, stream>>>(a, heads, 1);
         return;
     }
     constexpr int kPer = 4;
-    const int chunks = (heads + kPer - 1) / kPer;
-    cache_append_kernel<kPer><<<(unsigned)((quads * chunks + 3) / 4), 256, 0, stream>>>(a, chunks);
+    const int span = quads * heads <= 65536 ? kPer : 2 * kPer, chunks = (heads + span - 1) / span;
+    cache_append_kernel<kPer><<<(unsigned)((quads * chunks + 3) / 4), 256, 0, stream>>>(a, chunks, span);
 }
 
 void launch_cache_read(const CacheDims &c, int n_requests, const int *seq_len, const int *table, int max_blocks, const int *first,

@@ -9,74 +9,106 @@ namespace ice {
 namespace {
 
 // ------------------------------------------------------------------------------------------------------------ sorted queries
-// Where a request's queries stand in the list is the number of those with a lower source, or the same one and a lower request.  A wave counts
-// them for a request, and for a row of the table those with a lower source, over all requests in LDS; so no workgroup waits for another and the order is
-// always the same.
-constexpr int kSourceThreads = 1024, kSourceShare = 64;  // requests of a workgroup at most
+// Every workgroup counts all requests' queries by row of the table in LDS (whole numbers: the order of the additions does not matter), those of the requests
+// before its own share apart, and sums them up; so it knows where the queries of its requests stand, no workgroup waits for another, and the order is always the
+// same.  Bound by latency: a trip for the requests' words, the counts (a lane at a time where requests share a row), the sums, the stores.
+constexpr int kSourceThreads = 1024, kSourceShare = 64;  // of a workgroup, and requests of one, at most
 __global__ __launch_bounds__(kSourceThreads) void plan_sources_kernel(CacheSources p, int share, int row_share) {
-    extern __shared__ int sources_lds[];
-    const int n = p.n_requests, rows = p.n_rows, T = p.n_tokens, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int *s_to = sources_lds, *s_many = sources_lds + n, *s_place = sources_lds + 2 * n;
-    __shared__ unsigned s_at[kSourceShare], s_total;
-    int *start = p.plan, *lowest = p.plan + rows + 2, *token = p.plan + 2 * rows + 2, *place = token + T;
-    if (tid == 0) s_total = 0;
-    __syncthreads();
-    unsigned total = 0;
-    for (int s = tid; s < n; s += kSourceThreads) {
-        const int from = min(max(p.query_start[s], 0), T), many = min(max(p.query_start[s + 1], from), T) - from, to = p.source[s];
-        s_to[s] = (unsigned)to >= (unsigned)rows || (p.seq_len && to == s) ? rows : to;
-        s_many[s] = many;
-        s_place[s] = p.seq_len ? (int)((unsigned)max(p.seq_len[s], 0) - (unsigned)many) : 0;
-        total += (unsigned)many;
-    }
-    if (total) atomicAdd(&s_total, total);
-    __syncthreads();
+    extern __shared__ unsigned sources_lds[];
+    const int n = p.n_requests, rows = p.n_rows, T = p.n_tokens, threads = blockDim.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = threads >> 6;
+    unsigned *before = sources_lds, *begin = before + rows + 1;  // queries of the requests before this share; all others, later where a row's queries begin
+    int *least = (int *)(begin + rows + 1);
+    __shared__ unsigned s_wave[kSourceThreads / 64], s_total, s_at[kSourceShare];
+    __shared__ int s_from[kSourceShare], s_to[kSourceShare], s_many[kSourceShare], s_place[kSourceShare];
     const int r0 = min((int)blockIdx.x * share, n), r1 = min(r0 + share, n);
-    const int g0 = min((int)blockIdx.x * row_share, rows + 2), g1 = min(g0 + row_share, rows + 2);
-    for (int item = wave; item < r1 - r0 + g1 - g0; item += kSourceThreads / 64) {
-        const bool request = item < r1 - r0;
-        const int s = r0 + item, g = request ? s_to[s] : g0 + item - (r1 - r0), before = request ? s : 0;
-        unsigned sum = 0;
-        int least = 0x7FFFFFFF;
-        for (int e = lane; e < n; e += 64) {
-            const int to = s_to[e], many = s_many[e];
-            if (to < g || (to == g && e < before)) sum += (unsigned)many;
-            if (to == g && many > 0) least = min(least, s_place[e]);
-        }
-        sum = (unsigned)wave_scan_add((int)sum);
-        if (request) {
-            if (lane == 63) s_at[item] = sum;
-            continue;
-        }
+    int *start = p.plan, *lowest = p.plan + rows + 2, *token = p.plan + 2 * rows + 2, *place = token + T;
+    for (int g = tid; g <= rows; g += threads) {
+        before[g] = begin[g] = 0;
+        if (g < rows) least[g] = 0x7FFFFFFF;
+    }
+    constexpr int kTogether = 4;  // requests whose words a thread asks for side by side
+    for (int s0 = tid; s0 - tid < n; s0 += kTogether * threads) {
+        int x[kTogether], y[kTogether], named[kTogether], len[kTogether];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
-        if (lane == 63) {
-            start[g] = (int)min(sum, (unsigned)T);
-            if (g < rows) lowest[g] = least;
+        for (int k = 0; k < kTogether; ++k) {
+            const int s = min(s0 + k * threads, n - 1);
+            x[k] = p.query_start[s];
+            y[k] = p.query_start[s + 1];
+            named[k] = p.source[s];
+            len[k] = p.seq_len ? p.seq_len[s] : 0;
+        }
+        if (s0 == tid) __syncthreads();  // (the counts are 0)
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int s = s0 + k * threads;
+            if (s >= n) break;
+            const int from = min(max(x[k], 0), T), many = min(max(y[k], from), T) - from;
+            const int to = (unsigned)named[k] >= (unsigned)rows || (p.seq_len && named[k] == s) ? rows : named[k];
+            const int at = p.seq_len ? (int)((unsigned)max(len[k], 0) - (unsigned)many) : 0;
+            if (many > 0) {
+                atomicAdd((s < r0 ? before : begin) + to, (unsigned)many);
+                if (to < rows) atomicMin(least + to, at);
+            }
+            if (s >= r0 && s < r1) {
+                s_from[s - r0] = from;
+                s_to[s - r0] = to;
+                s_many[s - r0] = many;
+                s_place[s - r0] = at;
+            }
         }
     }
     __syncthreads();
-    for (int s = r0; s < r1; ++s) {
-        const int from = min(max(p.query_start[s], 0), T), many = s_many[s];
-        for (int j = tid; j < many; j += kSourceThreads) {
-            const unsigned at = s_at[s - r0] + (unsigned)j;
-            if (at >= (unsigned)T) break;
-            token[at] = from + j;
-            place[at] = p.seq_len ? (int)((unsigned)s_place[s] + (unsigned)j) : 0;
-        }
+    const int each = (rows + threads) / threads, g0 = min(tid * each, rows + 1), g1 = min(g0 + each, rows + 1);
+    unsigned own = 0;
+    for (int g = g0; g < g1; ++g) own += before[g] + begin[g];
+    const unsigned incl = (unsigned)wave_scan_add((int)own);
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    unsigned at = incl - own;
+    for (int w = 0; w < wave; ++w) at += s_wave[w];
+    for (int g = g0; g < g1; ++g) {
+        const unsigned here = before[g] + begin[g];
+        begin[g] = at;
+        at += here;
     }
-    for (long long e = (long long)min(s_total, (unsigned)T) + (long long)blockIdx.x * kSourceThreads + tid; e < T; e += (long long)gridDim.x * kSourceThreads)
+    if (tid == threads - 1) s_total = at;
+    __syncthreads();
+    for (int s = r0 + wave; s < r1; s += waves) {  // (a share is no longer than a wave)
+        const int to = s_to[s - r0];
+        const bool same = lane < s - r0 && s_to[lane] == to;
+        const unsigned sum = (unsigned)wave_scan_add(same ? s_many[lane] : 0);
+        if (lane == 63) s_at[s - r0] = begin[to] + before[to] + sum;
+    }
+    for (int g = min((int)blockIdx.x * row_share, rows + 2) + tid; g < min(((int)blockIdx.x + 1) * row_share, rows + 2); g += threads) {
+        start[g] = (int)min(g <= rows ? begin[g] : s_total, (unsigned)T);
+        if (g < rows) lowest[g] = least[g];
+    }
+    __syncthreads();
+    // a wave to a request, but all of them to one of many queries
+    auto put = [&](int s, int from, int step) {
+        for (int j = from; j < s_many[s]; j += step) {
+            const unsigned e = s_at[s] + (unsigned)j;
+            if (e >= (unsigned)T) break;
+            token[e] = s_from[s] + j;
+            place[e] = p.seq_len ? (int)((unsigned)s_place[s] + (unsigned)j) : 0;
+        }
+    };
+    for (int s = wave; s < r1 - r0; s += waves)
+        if (s_many[s] <= kSourceThreads) put(s, lane, 64);
+    for (int s = 0; s < r1 - r0; ++s)
+        if (s_many[s] > kSourceThreads) put(s, tid, threads);
+    for (long long e = (long long)min(s_total, (unsigned)T) + (long long)blockIdx.x * threads + tid; e < T; e += (long long)gridDim.x * threads)
         token[e] = place[e] = -1;
 }
 
 }  // namespace
 
 void launch_plan_sources(const CacheSources &p, hipStream_t stream) {
-    const int items = p.n_requests + p.n_rows + 2;
-    const int groups = std::min(256, (items + 15) / 16);
-    const size_t lds = 3 * (size_t)p.n_requests * sizeof(int);
-    if (lds > 65536 - 1024) allow_dynamic_lds((const void *)plan_sources_kernel, lds);
-    plan_sources_kernel<<<groups, kSourceThreads, lds, stream>>>(p, (p.n_requests + groups - 1) / groups, (p.n_rows + 2 + groups - 1) / groups);
+    const int threads = p.n_requests <= 256 ? 256 : kSourceThreads;
+    const int groups = std::min(256, (std::max(p.n_requests, p.n_rows + 2) + threads / 64 - 1) / (threads / 64));
+    const size_t lds = (3 * (size_t)p.n_rows + 2) * sizeof(int);
+    if (lds > 65536 - 4096) allow_dynamic_lds((const void *)plan_sources_kernel, lds);
+    plan_sources_kernel<<<groups, threads, lds, stream>>>(p, (p.n_requests + groups - 1) / groups, (p.n_rows + 2 + groups - 1) / groups);
 }
 
 // ------------------------------------------------------------------------------------------------------------------ attention
