@@ -639,6 +639,18 @@ static ice_status_t check_rows(int32_t n_rows) {
     return n_rows < 1 || n_rows > kSourceRows ? fail(ICE_ERR_SHAPE, "%d rows of the table: outside [1, %d]", n_rows, kSourceRows) : ICE_OK;
 }
 
+// (the quanta of a launch's entries are counted in 31 bits; row tiles of sources are whole tokens, those of both sides lie in one launch)
+static ice_status_t check_sources_count(const ice_cache_t *c, const CacheAttend &a, double queries, double entries) {
+    const double keys = (double)a.max_blocks * c->block_size / 128 + 4, tile = 192 / a.G;
+    if (keys * (queries / tile + 2) * entries * c->n_kv_heads >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d rows x %d KV heads x %d blocks x %.0f queries: too many for one call", a.S, c->n_kv_heads, a.max_blocks, queries);
+    return ICE_OK;
+}
+static ice_status_t check_shared_count(const ice_cache_t *c, const CacheAttend &a) {
+    return check_sources_count(c, a, (double)a.max_query + a.max_shared, 2.0 * a.S);
+}
+static ice_status_t check_cross_count(const ice_cache_t *c, const CacheAttend &a) { return check_sources_count(c, a, a.max_query, std::min(a.S, 1024)); }
+
 // where a list's parts lie (ice_plan_sources)
 static void set_list(CacheAttend &a, const int32_t *plan) {
     a.list_start = plan;
@@ -672,6 +684,7 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *c, const void *q, int64_t
     a.seq_len = seq_len;
     a.table = table;
     a.max_blocks = max_blocks;
+    if (ice_status_t st = check_cross_count(c, a)) return st;
     if (ice_status_t st = set_attend(c, a, q, q_stride, out, out_type, lse, ws, ws_bytes, need)) return st;
     launch_cache_cross(a, static_cast<hipStream_t>(stream));
     return device_status("ice_cache_attend_cross");
@@ -683,20 +696,11 @@ static ice_status_t plan_shared(const ice_cache_t *c, int32_t G, int32_t n_reque
     if (n_tokens < 0 || n_tokens > (1 << 30)) return fail(ICE_ERR_SHAPE, "n_tokens %d is outside [0, 2^30]", n_tokens);
     if (ice_status_t st = plan_attend(c, G, n_requests, max_shared, max_source_keys, false, a, bytes)) return st;  // (its checks of these two)
     if (ice_status_t st = plan_attend(c, G, n_requests, max_query, max_keys, false, a, bytes)) return st;
-    if ((double)n_tokens * c->n_kv_heads >= 2147483648.0) return fail(ICE_ERR_UNSUPPORTED, "%d tokens for %d KV heads: too many for one call", n_tokens, c->n_kv_heads);
+    if ((double)n_tokens * c->n_kv_heads > 1e7) return fail(ICE_ERR_UNSUPPORTED, "%d tokens for %d KV heads: too many for one call", n_tokens, c->n_kv_heads);
     a.T = n_tokens;
     a.max_shared = max_shared;
     a.whole = false;
     *bytes = plan_cache_shared(a, max_source_keys);
-    return ICE_OK;
-}
-
-// (both sides' quanta are counted together, all requests in one launch)
-static ice_status_t check_shared_count(const ice_cache_t *c, const CacheAttend &a) {
-    const double keys = (double)a.max_blocks * c->block_size / 128 + 3, tile = 192 / a.G;
-    if (keys * (a.max_query / tile + a.max_shared / tile + 4) * 2 * a.S * c->n_kv_heads >= 2147483648.0)
-        return fail(ICE_ERR_UNSUPPORTED, "%d requests x %d KV heads x %d blocks x %d and %d queries: too many for one call", a.S, c->n_kv_heads, a.max_blocks,
-                    a.max_query, a.max_shared);
     return ICE_OK;
 }
 
@@ -749,7 +753,11 @@ ice_status_t ice_debug_shared_cut(const ice_cache_t *c, int32_t G, int32_t n_req
     a.query_start = query_start;
     set_list(a, plan);
     if (ice_status_t st = check_shared_count(c, a)) return st;
-    *n_parts = cut_cache_shared(a, parts, max_parts);
+    try {
+        *n_parts = cut_cache_shared(a, parts, max_parts);
+    } catch (...) {
+        return fail(ICE_ERR_CAPACITY, "no host memory for the sums of %d requests", n_requests);
+    }
     return ICE_OK;
 }
 
@@ -765,8 +773,12 @@ ice_status_t ice_debug_cross_cut(const ice_cache_t *c, int32_t G, int32_t n_rows
     if (ice_status_t st = plan_attend(c, G, n_rows, max_shared, max_keys, false, a, &need)) return st;
     a.T = n_tokens;
     a.max_blocks = max_blocks;
-    if (ice_status_t st = check_count(c, a, false)) return st;
-    *n_parts = cut_cache_cross(a, start, len, parts, max_parts);
+    if (ice_status_t st = check_cross_count(c, a)) return st;
+    try {
+        *n_parts = cut_cache_cross(a, start, len, parts, max_parts);
+    } catch (...) {
+        return fail(ICE_ERR_CAPACITY, "no host memory for the sums of %d rows", n_rows);
+    }
     return ICE_OK;
 }
 
@@ -784,7 +796,11 @@ ice_status_t ice_debug_cache_cut(const ice_cache_t *c, int32_t G, int32_t n_requ
     a.max_blocks = max_blocks;
     a.window = window;
     if (ice_status_t st = check_count(c, a, !query_start)) return st;
-    *n_parts = cut_cache_attend(a, !query_start, query_start, len, parts, max_parts);
+    try {
+        *n_parts = cut_cache_attend(a, !query_start, query_start, len, parts, max_parts);
+    } catch (...) {
+        return fail(ICE_ERR_CAPACITY, "no host memory for the sums of %d requests", n_requests);
+    }
     return ICE_OK;
 }
 

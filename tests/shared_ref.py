@@ -47,24 +47,19 @@ def source_of(source, s, rows, same):
 def sources(source, start, lens, n_rows, n_tokens):
     """The plan as the header states it; lens None: the sources are rows of another table."""
     n = len(source)
-    to = [source_of(source, s, n_rows, lens is not None) for s in range(n)]
-    begin, lowest, token, place = [], [], [], []
-    for r in list(range(n_rows)) + [-1]:
-        begin.append(len(token))
-        low = NONE
-        for s in range(n):
-            m = int(start[s + 1] - start[s])
-            if to[s] != r or m == 0:
-                continue
-            at = max(int(lens[s]), 0) - m if lens is not None else 0
-            low = min(low, at)
-            token += list(range(int(start[s]), int(start[s + 1])))
-            place += [at + j if lens is not None else 0 for j in range(m)]
-        if r >= 0:
-            lowest.append(low)
-    begin.append(len(token))
+    to = np.array([source_of(source, s, n_rows, lens is not None) for s in range(n)])
+    to = np.where(to < 0, n_rows, to)
+    many = np.diff(np.asarray(start))
+    at = np.maximum(np.asarray(lens), 0) - many if lens is not None else np.zeros(n, int)
+    begin, lowest = np.zeros(n_rows + 2, int), np.full(n_rows + 1, NONE)
+    np.add.at(begin, to + 1, many)
+    np.minimum.at(lowest, to[many > 0], at[many > 0])
+    token, place = [], []
+    for s in np.argsort(to, kind="stable"):
+        token += range(int(start[s]), int(start[s + 1]))
+        place += range(int(at[s]), int(at[s] + many[s])) if lens is not None else [0] * int(many[s])
     rest = [-1] * (n_tokens - len(token))
-    return np.array(begin + lowest + token + rest + place + rest)
+    return np.concatenate([np.cumsum(begin), lowest[:n_rows], token, rest, place, rest]).astype(np.int64)
 
 
 def append(data, k, v, q, start, lens, source, table, rope, neighbours, block):
@@ -110,7 +105,12 @@ def held_rows(data, table_row, length, block, h):
 
 def attention(q, data, table, lens, qlens, source, block, group, window, bf16_out, many, cross=False):
     """Query rows in order: (out, lse, tol, lse_tol), [tokens, heads, ...].  cross: table and lens are the sources'."""
-    heads, parts, at = data.shape[1], [], 0
+    heads, parts, at, kept = data.shape[1], [], 0, {}
+
+    def of_source(r, h):
+        if (r, h) not in kept:
+            kept[r, h] = held_rows(data, table[r], lens[r], block, h)
+        return kept[r, h]
     for s, m in enumerate(qlens):
         if m == 0:
             continue
@@ -118,7 +118,7 @@ def attention(q, data, table, lens, qlens, source, block, group, window, bf16_ou
         before = max(int(lens[r]), 0) if r >= 0 else 0
         res = []
         for h in range(heads):
-            rows = [held_rows(data, table[r], lens[r], block, h) + (0,)] if r >= 0 else []
+            rows = [of_source(r, h) + (0,)] if r >= 0 else []
             if not cross:
                 rows.append(held_rows(data, table[s], lens[s], block, h) + (before,))
             if rows:
@@ -132,8 +132,8 @@ def attention(q, data, table, lens, qlens, source, block, group, window, bf16_ou
                 seen &= pos[None] <= own
                 if window:
                     seen &= pos[None] > own - window
-            for j in range(group):
-                res.append(ref.softmax_rows(q[at: at + m, h * group + j], k, v, seen, bf16_out, many))
-        parts.append([np.stack([x[i] for x in res], 1) for i in range(4)])
+            rows = ref.softmax_rows(q[at: at + m, h * group: (h + 1) * group].reshape(m * group, D), k, v, np.repeat(seen, group, 0), bf16_out, many)
+            res.append([x.reshape(m, group, *x.shape[1:]) for x in rows])
+        parts.append([np.concatenate([x[i] for x in res], 1) for i in range(4)])
         at += m
     return [np.concatenate([p[i] for p in parts]) for i in range(4)]

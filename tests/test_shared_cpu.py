@@ -198,6 +198,7 @@ def test_attention_to_sources_refuses():
         assert go(wb=need[call] - 1) == b.ICE_ERR_CAPACITY and "workspace" in p.ice_last_error()
         assert go(**{count: 8192, "shared": 2 ** 24}) == b.ICE_ERR_UNSUPPORTED
         call(c, *{**good, "tokens": 0}.values())
+    assert status(p.ice_cache_attend_shared, c, *{**both, "tokens": 5 * 10 ** 6 + 1}.values()) == b.ICE_ERR_UNSUPPORTED
     for args in ((c, 17, 2, 1, 4096), (c, 4, 0, 1, 4096), (c, 4, 8193, 1, 4096), (c, 4, 2, 0, 4096)):
         assert p.ice_cache_attend_cross_bytes(*args) == 0
     assert p.ice_cache_attend_shared_bytes(c, 4, 2, -1, 1, 2, 64, 4096) == 0 and p.ice_cache_attend_shared_bytes(c, 4, 8193, 2, 1, 2, 64, 4096) == 0

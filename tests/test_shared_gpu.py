@@ -289,6 +289,90 @@ def test_blocks_that_do_not_exist_and_values_held_as_nan(queries, cross):
         run_shared(np.random.default_rng([queries, window]), 2, 4, 16, lens, qlens, source, window, torch.float32, cross=cross, edit=edit)
 
 
+@pytest.mark.parametrize("group", [1, 3, 5, 6, 7, 9, 11, 13, 14, 16])
+def test_row_tiles_of_whole_tokens(group):
+    """Groups that do not divide a tile's 192 rows: a token's rows stay in one tile; one tile of up to 128 rows, several of them, chunks of a request's own."""
+    rng = np.random.default_rng([group, 17])
+    run_shared(rng, 1, group, 16, [300, 40, 9], [0, 100 // group, 1], [-1, 0, 0], 0, torch.float32)
+    run_shared(rng, 2, group, 32, [450, 170, 60, 40], [0, 800 // group, 60 // group + 1, 2], [-1, 0, 0, -1], 0, torch.bfloat16)
+    run_shared(rng, 1, group, 16, [270, 30], [700 // group, 3, 0], [1, 0, 0], 0, torch.float32, cross=True)
+
+
+@pytest.mark.parametrize("longest,source", [(1, 1), (20, 200), (90000, 1), (1, 500000)])
+def test_any_hint_of_the_lengths_gives_the_result(longest, source):
+    rng = np.random.default_rng(longest)
+    heads, group, block, lens, qlens, named = 2, 4, 16, [1500, 300, 33, 700, 5], [0, 1, 30, 2, 1], [-1, 0, 0, 0, -1]
+    n_blocks, table = tables(rng, lens, block)
+    data = random_pool(rng, n_blocks, heads, block)
+    c, start = make(n_blocks, heads, block, data), np.concatenate([[0], np.cumsum(qlens)])
+    q = bits(rng, int(start[-1]), heads * group, D)
+    plan = i32(sh.sources(named, start, lens, 5, int(start[-1])))
+    want = sh.attention(ref.widen(q).astype(np.float64), data, table, lens, qlens, named, block, group, 0, False, True)
+    check(*c.attend_shared(up(q), i32(start), i32(named), plan, i32(lens), i32(table), max_len=longest, max_source=source, with_lse=True), want)
+    plan = i32(sh.sources(named, start, None, 5, int(start[-1])))
+    want = sh.attention(ref.widen(q).astype(np.float64), data, table, lens, qlens, named, block, group, 0, False, True, cross=True)
+    check(*c.attend_cross(up(q), plan, i32(lens), i32(table), max_len=source, with_lse=True), want)
+
+
+@pytest.mark.parametrize("max_query,max_shared", [(2, 9), (9, 4), (3, 5), (70, 40), (20, 90), (30, 30)])
+def test_queries_beyond_the_most_are_left_as_they_were(max_query, max_shared):
+    """Of a request those behind its first max_query, of a source those behind the first max_shared of its list; the others get their results."""
+    rng = np.random.default_rng([max_query, max_shared])
+    many = max(max_query, max_shared) > 12
+    heads, group, block, lens = 2, 4, 16, [400, 90, 120, 64]
+    qlens, named = ([0, 60, 40, 25] if many else [0, 3, 5, 4]), [-1, 0, 0, -1]
+    n_blocks, table = tables(rng, lens, block)
+    data = random_pool(rng, n_blocks, heads, block)
+    c, start = make(n_blocks, heads, block, data), np.concatenate([[0], np.cumsum(qlens)])
+    total = int(start[-1])
+    q = bits(rng, total, heads * group, D)
+    place = np.arange(total) - np.repeat(start[:-1], qlens)
+    in_list = np.where(np.arange(total) < start[3], np.arange(total), 0)  # (the two requests behind row 0 stand one after the other)
+    for cross in (False, True):
+        plan = i32(sh.sources(named, start, None if cross else lens, 4, total))
+        out, lse = torch.full((total, heads * group, D), 7.0, device="cuda"), torch.full((total, heads * group), 7.0, device="cuda")
+        if cross:
+            c.attend_cross(up(q), plan, i32(lens), i32(table), max_shared=max_shared, out=out, lse=lse)
+            there = in_list < max_shared
+        else:
+            c.attend_shared(up(q), i32(start), i32(named), plan, i32(lens), i32(table), max_query=max_query, max_shared=max_shared, out=out, lse=lse)
+            there = (place < max_query) & (in_list < max_shared)
+        want = sh.attention(ref.widen(q).astype(np.float64), data, table, lens, qlens, named, block, group, 0, False, True, cross)
+        want[2] = np.maximum(want[2], 1e-37)
+        assert there.any()
+        at = torch.from_numpy(there).cuda()
+        check(out[at], lse[at], [w[there] for w in want])
+        assert bool((out[~at] == 7).all()) and bool((lse[~at] == 7).all())
+
+
+def test_units_of_few_rows_beside_a_chunk_keep_two_terms():
+    """bf16 outputs of requests and sources with up to 16 rows in a call that has a chunk: their weights have 16 bits."""
+    rng = np.random.default_rng(18)
+    heads, group, block, lens, qlens, named = 2, 4, 16, [500, 700, 90, 300, 40, 200], [0, 0, 1, 2, 1, 60], [-1, -1, 0, 0, 0, 1]
+    n_blocks, table = tables(rng, lens, block)
+    data = random_pool(rng, n_blocks, heads, block)
+    c, start = make(n_blocks, heads, block, data), np.concatenate([[0], np.cumsum(qlens)])
+    q = bits(rng, 64, heads * group, D)
+    for cross in (False, True):
+        plan = i32(sh.sources(named, start, None if cross else lens, 6, 64))
+        got = c.attend_cross(up(q), plan, i32(lens), i32(table), out_dtype=torch.bfloat16, with_lse=True) if cross else \
+            c.attend_shared(up(q), i32(start), i32(named), plan, i32(lens), i32(table), out_dtype=torch.bfloat16, with_lse=True)
+        want = sh.attention(ref.widen(q).astype(np.float64), data, table, lens, qlens, named, block, group, 0, True, False, cross)
+        check(got[0][:4], got[1][:4], [w[:4] for w in want])
+
+
+@pytest.mark.parametrize("group,queries,requests,longest,dtype", [(16, 1, 6, 102000, torch.bfloat16), (1, 1, 3, 150000, torch.float32), (4, 40, 3, 35000, torch.bfloat16)])
+def test_a_long_source(group, queries, requests, longest, dtype):
+    """As many long pieces as there are workgroups, of the two lengths that two to a CU get, or the three of three."""
+    rng = np.random.default_rng([queries, requests])
+    heads, block = 8, 64
+    lens = [longest] + [int(x) for x in rng.integers(queries, 200, requests)]
+    n_blocks, table = tables(rng, lens, block)
+    data = rng.integers(0, 256, (n_blocks, heads, 4, 2176), dtype=np.uint8)
+    data[..., 2048:] = 124 + data[..., 2048:] % 3  # scales of 1 / 8 to 1 / 2
+    run_shared(rng, heads, group, block, lens, [0] + [queries] * requests, [-1] + [0] * requests, 0, dtype, data=data, table=table)
+
+
 def test_sources_that_are_longer_than_the_tables_row():
     """Queries stand behind the source's length all the same; its tokens behind the row do not exist."""
     rng = np.random.default_rng(13)
@@ -478,3 +562,65 @@ def test_the_same_call_gives_the_same_bits():
         for _ in range(5):
             again = c.attend_shared(q, start, source, plan, lens_t, table_t, out_dtype=dtype, with_lse=True)
             assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+# ------------------------------------------------------------------------------------------------------- what is refused
+def test_what_the_classes_refuse():
+    """Nothing is enqueued, outputs and cache stay as they are, and the good calls work afterwards."""
+    import paper_2604_10539_amd.binding as b
+    from paper_2604_10539_amd import IceBlocks, IceError
+    rng = np.random.default_rng(41)
+    heads, group, block, lens, qlens = 2, 4, 16, [20, 5, 40], [1, 1, 1]
+    n_blocks, table = tables(rng, lens, block)
+    data = random_pool(rng, n_blocks, heads, block)
+    c = make(n_blocks, heads, block, data)
+    rows = lambda h: up(bits(rng, 3, h, D))  # noqa: E731
+    plan = sh.sources([-1, 0, 0], [0, 1, 2, 3], lens, 3, 3)
+    g = dict(q=rows(heads * group), k=rows(heads), v=rows(heads), query_start=i32([0, 1, 2, 3]), seq_len=i32(lens), block_table=i32(table), source=i32([-1, 0, 0]),
+             plan=i32(plan), rope=up(angles(70, 64)), out=torch.full((3, heads * group, D), 7.0, device="cuda"), lse=torch.full((3, heads * group), 7.0, device="cuda"))
+    turned = torch.full((3, heads * group, D), 7, dtype=torch.int16, device="cuda")
+    calls = {"append": (c.append, ("k", "v", "query_start", "seq_len", "block_table", "q", "rope", "source"), dict(out=turned)),
+             "attend_cross": (c.attend_cross, ("q", "plan", "seq_len", "block_table", "out", "lse"), {}),
+             "attend_shared": (c.attend_shared, ("q", "query_start", "source", "plan", "seq_len", "block_table", "out", "lse"), {})}
+    row_kinds = {"float32": lambda t: t.float(), "cpu": lambda t: t.cpu(), "64 values": lambda t: t[..., :64], "two dimensions": lambda t: t.flatten(1), "a number": lambda t: 7,
+                 "heads apart": lambda t: t.transpose(0, 1).contiguous().transpose(0, 1), "the same row again": lambda t: t[:1].expand(t.shape)}
+    int_kinds = {"int64": lambda t: t.long(), "cpu": lambda t: t.cpu(), "longer": lambda t: torch.cat([t, t]), "apart": lambda t: t.repeat_interleave(2, -1)[..., ::2],
+                 "none": lambda t: None}
+    out_kinds = {"float16": lambda t: t.half(), "cpu": lambda t: t.cpu(), "longer": lambda t: torch.cat([t, t]), "apart": lambda t: t.repeat_interleave(2, -1)[..., ::2]}
+    rope_kinds = {"float64": lambda t: t.double(), "cpu": lambda t: t.cpu(), "apart": lambda t: t.repeat_interleave(2, -1)[..., ::2], "one dimension": lambda t: t.flatten(),
+                  "130 wide": lambda t: torch.zeros((70, 130), device="cuda")}
+
+    def refused(call, status, **k):
+        try:
+            call(**k)
+        except IceError as e:
+            assert e.status == status, (k.keys(), e)
+            return
+        raise AssertionError("taken")
+    for name, (call, names, more) in calls.items():
+        for n in names:
+            kinds = row_kinds if n in ("q", "k", "v") else out_kinds if n in ("out", "lse") else rope_kinds if n == "rope" else int_kinds
+            for kind, change in kinds.items():
+                if (n, kind) == ("source", "none") and name == "append":
+                    continue
+                refused(call, b.ICE_ERR_SHAPE, **{**{x: g[x] for x in names}, **more, n: change(g[n])})
+    good = {x: g[x] for x in calls["append"][1]}
+    for change, status in ((dict(rope=None), b.ICE_ERR_INVALID_ARG), (dict(q=None), b.ICE_ERR_SHAPE), (dict(rope=up(angles(70, 64))[:0]), b.ICE_ERR_SHAPE),
+                           (dict(rope=torch.zeros((70, 24), device="cuda")), b.ICE_ERR_UNSUPPORTED), (dict(q=g["q"][:2]), b.ICE_ERR_SHAPE), (dict(k=g["k"][:, :1], v=g["v"][:, :1]), b.ICE_ERR_SHAPE),
+                           (dict(out=turned[:2]), b.ICE_ERR_SHAPE), (dict(out=turned.float()), b.ICE_ERR_SHAPE)):
+        refused(c.append, status, **{**good, "out": turned, **change})
+    for name in ("attend_cross", "attend_shared"):
+        call, names, _ = calls[name]
+        good = {x: g[x] for x in names}
+        for change in (dict(max_shared=0), dict(max_len=0), dict(max_len=2 ** 30 + 1), dict(out_dtype=torch.float16), dict(plan=g["plan"][:-2].contiguous())):
+            refused(call, b.ICE_ERR_SHAPE, **{**good, **change})
+        refused(call, b.ICE_ERR_UNSUPPORTED, **{**good, "q": g["q"].repeat(1, 5, 1)[:, :34].contiguous(), "out": None, "lse": None})
+    good = {x: g[x] for x in calls["attend_shared"][1]}
+    for change in (dict(max_query=0), dict(max_source=0), dict(window=-1)):
+        refused(c.attend_shared, b.ICE_ERR_SHAPE, **{**good, **change})
+    blocks = IceBlocks(16, 16, 3, 64)
+    for bad in (dict(source=i32([0, 1])), dict(source=i32([0, 1, 2]).cpu()), dict(source=i32([0, 1, 2]).long()), dict(n_tokens=-1), dict(plan=i32([0] * 9))):
+        refused(blocks.plan_sources, b.ICE_ERR_SHAPE, **{**dict(source=i32([0, 1, 2]), n_tokens=3, plan=i32([0] * 14)), **bad})
+    assert bool((g["out"] == 7).all()) and bool((g["lse"] == 7).all()) and bool((turned == 7).all()) and np.array_equal(down(c.data), data)
+    c.attend_shared(**good)
+    check(g["out"], g["lse"], sh.attention(ref.widen(down(g["q"])).astype(np.float64), data, table, lens, qlens, [-1, 0, 0], block, group, 0, False, True))
