@@ -115,9 +115,10 @@ struct Unit {
 template <typename U> __host__ __device__ inline int quanta_of(const CacheAttend &a, const U &u, int t0, int t1, int quantum) {
     return max((u.high(t1) + quantum - 1) / quantum - u.low(a, t0) / quantum, 1);
 }
-// What a unit costs beside its keys, in quanta of the kernel for many queries: it is that much longer in the flat work, behind its keys.  (Of Causal
-// nothing: its units are long there.  Six chunks of 250 to 500 queries on 500 to 1500 keys of their own and 32 K of a source, us: 0 1990, 2 1340, 3 1260, 4 1270; 48 times
-// four drafted tokens on up to 2 K and 8 K: 98, 89, 100, 105.)
+// What a unit costs beside its keys (the trips in front of them, sums or a record behind them), in quanta of the kernel for many queries: it is that much longer in the
+// flat work, behind its keys.  Without it a workgroup whose piece is 64 requests' few own tokens takes several times as long as one in the middle of a source.  (Of Causal
+// nothing: its units are long there.)  Six chunks of 250 to 500 queries on 500 to 1500 tokens of their own and 32 K of a source, us: 0 1990, 2 1340, 3 1260, 4
+// 1270; 48 times four drafted tokens on up to 2 K and 8 K: 98, 89, 100, 105.  Units of few rows, whose quanta are longer: 2 65, 1 60.
 __host__ __device__ inline int chunk_setup(int form, int rows) { return form == kCross || form == kBoth ? (rows <= kRows ? 1 : 2) : 0; }
 // The quanta of a request in the kernel for few queries, if it takes that many rows.
 template <int FORM> __host__ __device__ inline int few_quanta(const CacheAttend &a, const Unit<FORM> &u, int most_rows, int quantum) {
@@ -186,7 +187,8 @@ template <int FORM> __device__ inline int source_at(const CacheAttend &a, int s)
 template <int FORM> __device__ inline bool is_alone(const CacheAttend &a, bool side, int s, int source) {
     return FORM == kBoth && !side && ((unsigned)source >= (unsigned)a.S || source == s);
 }
-// Of Both, by the workgroup that a unit ends in: where each query's sums are.  rows: of the unit, from the request's row `base` on.
+// Of Both, by the workgroup that a unit ends in: where each query's sums are.  A (token, KV head) gets one note for its own tokens' unit and one for its source's, whatever
+// workgroups they end in, so one launch can join both.  rows: of the unit, from the request's row `base` on.
 __device__ inline void put_notes(const CacheAttend &a, const Unit<kBoth> &u, int h, int base, int rows, int first, bool alone) {
     const int side = u.side ? 1 : 0, t0 = base / a.G, n = rows / a.G, all = u.queries(a);
     for (int i = threadIdx.x; i < n; i += (int)blockDim.x) {
@@ -381,6 +383,10 @@ __device__ inline void clear_unsourced(const CacheAttend &a) {
 // Bound by the vector unit (busy 61 %) and HBM together where there is much to read: one token of 16 requests of up to 32 K tokens, 8 KV heads,
 // 68 us with the merge, 5.3 TB/s; about 220 vector instructions beside 16 products for 32 keys.  Else by its trips: one request of
 // 4 K tokens 10 us.  Five drafted tokens of 32 requests, 40 rows, a window of 4096: 55 us, 23 of them products.  Lists of 1024 for 128 units 13.5.
+// Gathered queries (Cross, and the sources of Both) cost a trip more, the list's; the table's blocks are looked up beside it.  Five beams, ten rows, on each of 16
+// sources of 1500 tokens, 8 KV heads, float32 outputs: 18 us (16 rows: the sources with more than one answer have up to 20) and 4 for the merge; the steps, 3 of 128 keys
+// a workgroup, are 6 of them, the start 4.  Four requests of 130 tokens behind 2 K, 2 KV heads: 8 us, and 4 for the join.
+
 // LDS of a part: the waves' sums.  More than one tile of columns leaves no registers for a step on its way: three steps of a wave are copied to LDS by
 // direct loads (where the waves' sums meet later), [two tiles' key codes in operand order][their value codes][their scales].
 constexpr int kDepth = 3, kStage = 4352;
@@ -915,7 +921,7 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
         pair = single = per_head = 0;
         // (up to kRows rows are the few-query kernel's, which takes that many where there are requests with more than kFewRows)
         if (n_rows <= (FORM == kCausal ? kRows : 0)) return;
-        if constexpr (FORM != kCausal) {  // whole tokens, as evenly as they go; a quantum of few rows is longer, since its keys cost less
+        if constexpr (FORM != kCausal) {  // whole tokens (their notes are by token), as evenly as they go; a quantum of few rows is longer, since its keys cost less
             const int most = kChunkRows / a.G, n = n_rows / a.G;
             tiles = (n + most - 1) / most;
             step = (n + tiles - 1) / tiles * a.G;
@@ -952,7 +958,12 @@ struct Chunks {  // how a request's row tiles lie in the flat work of one KV hea
     }
 };
 
-// TILES: of rows that a wave has room for; kTiles, or 2 where no unit has more than kSmallRows rows (decode steps behind a source).
+// Cross and Both take all units here, those of few rows too (few_part), so that no other launch is needed beside this one.
+//
+// TILES: of rows that a wave has room for; kTiles, or 2 where no unit has more than kSmallRows rows (decode steps behind a source).  The smaller kernel keeps its
+// registers: one token of 32 requests behind 32 K tokens, 128 rows, 8 KV heads, bf16, 40 us and the join 7, 58 in all with three tiles' code in the kernel.  A round of two tiles takes
+// 2 us there beside another workgroup (conversion 0.6, scores 0.4, their maxima 0.3, weights and value products 0.6); start and lengths 2.3, the part's own
+// trips 5, its record 4 to 5.  Chunks of up to 500 queries behind 32 K tokens run at 1.05 PFLOP/s, a long source alone at 1.2.
 constexpr int kSmallRows = 2 * kWaves * kRows;
 template <int SETS, int FORM, int TILES>
 __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend a) {
@@ -1169,7 +1180,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 if constexpr (decltype(count)::value == 0) continue;  // (no rows: this wave only converts)
                 // scores of the round's 64 keys (those behind the last one are masked)
                 constexpr int NX = decltype(count)::value ? decltype(count)::value : 1, NB = kRound / 16;
-                // of one or two tiles of rows, where a product is soon done: operands read side by side, while those before them are used
+                // of one or two tiles of rows, where a product is soon done: operands read side by side, while those before them are used.  (Left to the compiler,
+                // and with the order below, every read was waited for: drafts of 64 rows a source 78 us, 67 so; groups of 4 and 2 here, 8 and 4 2 us more.)
                 constexpr int GROUP = FORM == kCausal || NX > 2 ? 0 : NX == 1 ? 4 : 2;
                 const int key0 = key_at + n * kRound;
                 f32x4 d[NX][NB];

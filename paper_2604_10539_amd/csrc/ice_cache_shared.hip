@@ -12,6 +12,7 @@ namespace {
 // Every workgroup counts all requests' queries by row of the table in LDS (whole numbers: the order of the additions does not matter), those of the requests
 // before its own share apart, and sums them up; so it knows where the queries of its requests stand, no workgroup waits for another, and the order is always the
 // same.  Bound by latency: a trip for the requests' words, the counts (a lane at a time where requests share a row), the sums, the stores.
+// 34 rows 4.4 us, 2000 requests with 217 K queries 7.1, 8000 requests of 40 sources 14 (a wave that counted the requests in front of each: 13.2 and 84).
 constexpr int kSourceThreads = 1024, kSourceShare = 64;  // of a workgroup, and requests of one, at most
 __global__ __launch_bounds__(kSourceThreads) void plan_sources_kernel(CacheSources p, int share, int row_share) {
     extern __shared__ unsigned sources_lds[];
