@@ -399,7 +399,7 @@ ice_status_t ice_cache_attend_tokens(const ice_cache_t *cache, const void *q, in
  *     `rotated` dimensions, (i, i + rotated / 2), or (2i, 2i + 1) with neighbours = 1, becomes (x cos - y sin, x sin + y cos): products and sums each rounded to
  *     fp32; a query is then rounded to bf16, a key is held from fp32.  A token whose position has no row in it is left out, its row of q_out too.
  *     NULL: keys enter as they are and positions are not looked at.
- * Rows behind query_start[n_requests] are left as they were. */
+ * query_start ascends; rows in front of query_start[0] and behind query_start[n_requests] belong to no request: they are left as they were. */
 ice_status_t ice_cache_append(const ice_cache_t *cache, const void *q_or_null, int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride,
                               const void *k, const void *v, int64_t k_stride, int64_t v_stride, int32_t n_tokens, int32_t n_requests,
                               const int32_t *query_start, const int32_t *seq_len, const int32_t *source_or_null, const int32_t *block_table,

@@ -785,7 +785,7 @@ class IceBlocks:
         if stream is not None or _current_device() != self._index:
             return _elsewhere(IceBlocks.plan_sources, self, stream, source, n_tokens, plan)
         if plan is None:
-            plan = torch.empty(2 * self.max_requests + 2 + 2 * n_tokens, dtype=torch.int32, device=self.device)
+            plan = torch.empty(2 * self.max_requests + 2 + 2 * max(n_tokens, 0), dtype=torch.int32, device=self.device)
         ice_plan_sources(source, self.query_start, self.seq_len, plan, self.max_requests, n_tokens)
         return plan
 

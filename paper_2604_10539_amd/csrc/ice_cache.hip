@@ -289,6 +289,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int ch
     // The request of each of the four tokens: the number of requests that end at or before it.  Up to 64 requests lie on the lanes, their lengths and
     // sources beside them; else 64 starts are looked at in a trip.
     int s, end, len, source, source_len;
+    const int front = a.query_start[0];  // (tokens in front of the first request are nobody's)
     if (n <= 64) {
         const int at = min(lane, n - 1), start = a.query_start[at + 1], length = a.seq_len[at], named = a.source ? a.source[at] : -1;
         int owner[4];
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int ch
         source = a.source ? a.source[safe] : -1;
         source_len = a.seq_len[(unsigned)source < (unsigned)n ? source : 0];
     }
-    const bool real = t0 + r < a.n_tokens && s < n;
+    const bool real = t0 + r < a.n_tokens && t >= front && s < n;
     const long long place = (long long)max(len, 0) - min(max(end, 0), a.n_tokens) + t;
     const long long position = place + ((unsigned)source < (unsigned)n && source != s ? max(source_len, 0) : 0);
     const bool known = real && (!a.half || (position >= 0 && position < a.n_positions));

@@ -1450,9 +1450,9 @@ __global__ __launch_bounds__(kMergeThreads) void cache_join_kernel(CacheAttend a
     __shared__ float s_sum[kMergeThreads / 32][kRecord];
     constexpr int kAtOnceRows = kMergeThreads / 32 / GROUPS, kAtOnce = 4;
     const int t = (int)(blockIdx.x / (unsigned)a.c.H), h = (int)(blockIdx.x % (unsigned)a.c.H);
-    const int all_tokens = a.query_start[a.S];
+    const int front = a.query_start[0], all_tokens = a.query_start[a.S];
     const TokenNote note[2] = {a.token_notes[(size_t)t * a.c.H + h], a.token_notes[((size_t)a.T + t) * a.c.H + h]};
-    if (t >= all_tokens || (note[0].flags & (kNoteLeft | kNoteDone))) return;
+    if (t < front || t >= all_tokens || (note[0].flags & (kNoteLeft | kNoteDone))) return;
     const bool alone = note[0].flags & kNoteAlone;
     if (!alone && (note[1].flags & kNoteLeft)) return;
     int n[2];

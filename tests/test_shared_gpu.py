@@ -345,6 +345,46 @@ def test_queries_beyond_the_most_are_left_as_they_were(max_query, max_shared):
         assert bool((out[~at] == 7).all()) and bool((lse[~at] == 7).all())
 
 
+@pytest.mark.parametrize("requests", [3, 70])
+def test_rows_in_front_of_the_first_request_are_nobodys(requests):
+    """A step whose first rows belong to other work: the rest is as if they were not there, and they stay as they were."""
+    rng = np.random.default_rng(requests)
+    heads, group, block, front, behind = 2, 4, 16, 5, 3
+    lens, qlens, named = [100] + [20] * (requests - 1), [0] + [2] * (requests - 1), [-1] + [0, -1] * requests
+    named = named[:requests]
+    n_blocks, table = tables(rng, lens, block)
+    data = random_pool(rng, n_blocks, heads, block)
+    start = np.concatenate([[0], np.cumsum(qlens)]) + front
+    total = int(start[-1]) + behind
+    k, v, q = bits(rng, total, heads, D), bits(rng, total, heads, D), bits(rng, total, heads * group, D)
+    rope = up(angles(200, 128))
+
+    def step(rows, start, out, lse):
+        c = make(n_blocks, heads, block, data)
+        args = i32(start), i32(lens), i32(table)
+        turned = up(q[rows])
+        c.append(up(k[rows]), up(v[rows]), *args, q=turned, out=turned, rope=rope, source=i32(named))
+        plan = i32(sh.sources(named, start, lens, requests, len(turned)))
+        c.attend_shared(turned, args[0], i32(named), plan, *args[1:], max_query=2, max_shared=2 * requests, out=out, lse=lse)
+        return c.data, turned
+
+    full = [torch.full((total, heads * group, *d), 7.0, device="cuda") for d in ((D,), ())]
+    less = [x[front:].clone() for x in full]
+    data0, q0 = step(slice(None), start, *full)
+    data1, q1 = step(slice(front, None), start - front, *less)
+    assert torch.equal(data0, data1) and torch.equal(q0[front:], q1) and np.array_equal(down(q0[:front].contiguous()), q[:front])
+    for x, y in zip(full, less):
+        assert torch.equal(x[front:].view(torch.int32), y.view(torch.int32)) and bool((x[:front] == 7).all()) and bool((x[-behind:] == 7).all())
+
+
+def test_a_negative_number_of_rows_is_refused():
+    from paper_2604_10539_amd import IceBlocks, IceError
+    b = IceBlocks(8, 16, 2, 64)
+    for n in (-1, -100):
+        with pytest.raises(IceError):
+            b.plan_sources(i32([-1, 0]), n)
+
+
 def test_units_of_few_rows_beside_a_chunk_keep_two_terms():
     """bf16 outputs of requests and sources with up to 16 rows in a call that has a chunk: their weights have 16 bits."""
     rng = np.random.default_rng(18)
