@@ -1615,14 +1615,17 @@ inline void launch_few(const CacheAttend &a, hipStream_t stream) {
         else cache_attend_kernel<W, 1, 3, 3, FORM><<<grid, block, 0, stream>>>(a);
     }
 }
+// threads for four records of a unit at a time, of which there are about per_unit: one trip for most
+template <int FORM>
+inline void launch_merge(const CacheAttend &a, int groups, int rows, int per_unit, hipStream_t stream) {
+    if (per_unit <= 4) cache_merge_kernel<1, FORM><<<dim3(groups, (rows + 7) / 8), kMergeThreads, 0, stream>>>(a);
+    else if (per_unit <= 8) cache_merge_kernel<2, FORM><<<dim3(groups, (rows + 3) / 4), kMergeThreads, 0, stream>>>(a);
+    else cache_merge_kernel<8, FORM><<<dim3(groups, rows), kMergeThreads, 0, stream>>>(a);
+}
 template <int FORM>
 inline void launch_few_merge(const CacheAttend &a, hipStream_t stream) {
     if (a.whole) return;
-    // threads for four records of a unit at a time: one trip for most
-    const int rows = std::min(a.rows, a.max_query * a.G), per_unit = a.few_groups / std::max(1, a.n_here * a.c.H) + 2;
-    if (per_unit <= 4) cache_merge_kernel<1, FORM><<<dim3(a.few_groups, (rows + 7) / 8), kMergeThreads, 0, stream>>>(a);
-    else if (per_unit <= 8) cache_merge_kernel<2, FORM><<<dim3(a.few_groups, (rows + 3) / 4), kMergeThreads, 0, stream>>>(a);
-    else cache_merge_kernel<8, FORM><<<dim3(a.few_groups, rows), kMergeThreads, 0, stream>>>(a);
+    launch_merge<FORM>(a, a.few_groups, std::min(a.rows, a.max_query * a.G), a.few_groups / std::max(1, a.n_here * a.c.H) + 2, stream);
 }
 
 template <int FORM>
@@ -1654,7 +1657,12 @@ inline void launch_attend(CacheAttend a, hipStream_t stream) {
             a.notes = (MergeNote *)part;
             a.part = (float *)(a.notes + a.many_groups);
             launch_chunks<FORM>(a, a.many_groups, stream);
-            cache_merge_kernel<1, FORM><<<dim3(a.many_groups, (a.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32)), kMergeThreads, 0, stream>>>(a);
+            if constexpr (FORM == kCross) {  // (16 answers, 64 rows, to one source of 32 K tokens, float32: 43 us, 57 by single threads)
+                const long long units = (long long)a.n_here * a.c.H * (((long long)a.max_query * a.G + kChunkRows - 1) / kChunkRows);
+                launch_merge<FORM>(a, a.many_groups, a.rows, (int)(a.many_groups / std::max(1ll, units)) + 2, stream);
+            } else {
+                launch_merge<FORM>(a, a.many_groups, a.rows, 0, stream);
+            }
         }
     }
 }

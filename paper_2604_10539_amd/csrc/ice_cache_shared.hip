@@ -116,15 +116,21 @@ void launch_plan_sources(const CacheSources &p, hipStream_t stream) {
 static size_t note_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H * sizeof(TokenNote); }
 static size_t state_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H * a.G * kRecord * sizeof(float); }
 
+// Rows from which a call that is not small goes to the kernel for many queries: it does the few rows of a request's own as they are, the one for few
+// queries with as many tiles as the sources' take.  Four drafted tokens of 24 requests, four sources of 8 K, 32 rows, float32: 65 us there and 40 here; eight requests
+// behind 32 K, 32 rows, bf16, 35.4 and 28.8; twelve, 48 rows, 42.7 and 31.9.  But eight requests behind 2 K, 64 quanta: 15.0 and 18.5; behind 4 K, 768 of them, 17.7 and 18.0.
+static bool for_many(long long rows, double quanta) { return rows > kFewRows || (rows > kRows && quanta > 512); }
+
 size_t plan_cache_shared(CacheAttend &a, int max_source) {
     const long long most = std::max(a.max_query, a.max_shared), tile = kChunkRows / a.G;
-    a.many = most * a.G > kFewRows;
+    const auto quanta = [&](int keys, long long queries) { return ((long long)keys + kQuantum - 1) / kQuantum * (a.many ? (queries + tile - 1) / tile : 1); };
+    const auto all = [&]() { return (double)a.c.H * ((double)a.S * quanta(a.max_keys, a.max_query) + quanta(max_source, a.max_shared)); };
+    a.many = false;  // (quanta without their row tiles)
+    a.many = for_many(most * a.G, all());
     CacheAttend rows = a;
     rows.max_query = (int)most;
     a.rows = a.many ? (int)std::min<long long>(tile, most) * a.G : few_rows(rows);
-    const auto quanta = [&](int keys, long long queries) { return ((long long)keys + kQuantum - 1) / kQuantum * (a.many ? (queries + tile - 1) / tile : 1); };
-    const double all = (double)a.c.H * ((double)a.S * quanta(a.max_keys, a.max_query) + quanta(max_source, a.max_shared));
-    a.groups = (int)std::min<double>(a.rows > kRows ? 512 : 768, all);
+    a.groups = (int)std::min<double>(a.rows > kRows ? 512 : 768, all());
     return note_bytes(a) + state_bytes(a) + (size_t)a.groups * 2 * a.rows * kRecord * sizeof(float);
 }
 

@@ -48,7 +48,8 @@ def check_shared(heads, group, lens, qlens, source, window=0, max_query=None, ma
     keys = [max(1, max(lens)) if k is None else k for k in (max_keys, max_source)]
     parts = b.ice_debug_shared_cut(c, group, n, start, plan, tokens, *most, lens, *keys, width, window)
     nbytes = p.ice_cache_attend_shared_bytes(c, group, n, tokens, *most, *keys) - tokens * heads * (32 + 1056 * group)
-    many, capacity = max(most) * group > FEW, width * block
+    quanta, capacity = heads * (n * -(-keys[0] // 128) + -(-keys[1] // 128)), width * block
+    many = max(most) * group > (16 if quanta > 512 else FEW)
     expected = {}
     for e in range(2 * n):
         s = e % n

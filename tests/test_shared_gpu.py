@@ -345,6 +345,15 @@ def test_queries_beyond_the_most_are_left_as_they_were(max_query, max_shared):
         assert bool((out[~at] == 7).all()) and bool((lse[~at] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("group,queries,window", [(4, 1, 0), (2, 2, 700), (4, 1, 4500), (1, 3, 0), (3, 1, 5000), (2, 1, 4999)])
+def test_few_rows_of_a_source_in_a_call_that_is_not_small(group, queries, window, dtype):
+    """Two sources of 17 to 48 rows, requests of up to six; eight KV heads."""
+    n = 12
+    lens = [5000, 4700] + [40 + 53 * i % 300 for i in range(n)]
+    run_shared(np.random.default_rng([group, queries, window]), 8, group, 16, lens, [0, 0] + [queries] * n, [-1, -1] + [0] * 7 + [1] * 5, window, dtype)
+
+
 @pytest.mark.parametrize("requests", [3, 70])
 def test_rows_in_front_of_the_first_request_are_nobodys(requests):
     """A step whose first rows belong to other work: the rest is as if they were not there, and they stay as they were."""
