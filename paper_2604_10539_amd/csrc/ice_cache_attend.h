@@ -168,10 +168,10 @@ template <int FORM> __device__ inline const bf16_t *query_at(const CacheAttend &
     if (FORM == kCross || FORM == kBoth) token = max(token, 0);
     return a.q + (long long)token * a.q_stride + (long long)(h * a.G + row % a.G) * kD;
 }
-// A whole unit's row.  alone: of Both, the request has no source, its sums are its output; else they wait for the others in their side's state.
+// A whole unit's row, whose query is `token` (looked up before any store: the compiler would do it again behind each).  alone: of Both, the request has no source,
+// its sums are its output; else they wait for the others in their side's state.
 template <int FORM>
-__device__ inline void put_query(const CacheAttend &a, bool side, int row0, int h, int row, int d0, const f32x4 &sum, float top, float total, bool alone) {
-    const int token = token_of<FORM>(a, side, row0, row);
+__device__ inline void put_query(const CacheAttend &a, bool side, int token, int h, int row, int d0, const f32x4 &sum, float top, float total, bool alone) {
     if ((FORM == kCross || FORM == kBoth) && token < 0) return;
     const size_t at = (size_t)token * a.c.H * a.G + h * a.G + row % a.G;
     if (FORM == kBoth && !alone) {
@@ -740,9 +740,11 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
         for (int in0 = tid >> 5; in0 < (NT == 1 ? 2 * W : min(R, n_rows - R * x)); in0 += 2 * W * kPasses) {
             f32x4 sum[kPasses];
             float top[kPasses], all[kPasses];
+            int token[kPasses];
 #pragma unroll
             for (int pass = 0; pass < kPasses; ++pass) {
                 const int in = min(in0 + 2 * W * pass, R - 1);
+                token[pass] = whole ? token_of<FORM>(a, unit.side, unit.row0, min(R * x + in, n_rows - 1)) : 0;
                 float2 ml[W];
 #pragma unroll
                 for (int w = 0; w < W; ++w) ml[w] = *(const float2 *)&s_acc[w][in][kD];
@@ -766,7 +768,7 @@ __device__ __attribute__((always_inline)) inline void few_part(const CacheAttend
                 const int in = in0 + 2 * W * pass, row = R * x + in;
                 if (in >= R || row >= n_rows) continue;
                 if (whole) {
-                    put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum[pass], top[pass], all[pass], alone);
+                    put_query<FORM>(a, unit.side, token[pass], h, row, d0, sum[pass], top[pass], all[pass], alone);
                 } else {
                     float *r = record + (size_t)row * kRecord;
                     *(f32x4 *)(r + d0) = sum[pass];
@@ -1372,6 +1374,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
         lds_barrier();  // (the last operands have been used: the next part writes others)
         const bool whole = now == u0 && stop == u1, alone = is_alone<FORM>(a, unit.side, s, source);
         float *record = a.part + (size_t)record_of(blockIdx.x, now > u0) * a.rows * kRecord;
+        int token[TILES];
+#pragma unroll
+        for (int x = 0; x < TILES; ++x)
+            token[x] = whole ? token_of<FORM>(a, unit.side, unit.row0, base + min(kRows * (kWaves * x + wave) + c, n_rows - 1)) : 0;
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
             const int in = kRows * (kWaves * x + wave) + c, row = base + in;
@@ -1384,7 +1390,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
                 for (int half = 0; half < 2; ++half) {
                     const int d0 = 32 * g + 8 * i + 4 * half;
                     const f32x4 sum = {acc[x][4 * half][i], acc[x][4 * half + 1][i], acc[x][4 * half + 2][i], acc[x][4 * half + 3][i]};
-                    if (whole) put_query<FORM>(a, unit.side, unit.row0, h, row, d0, sum, m[x], l[x], alone);
+                    if (whole) put_query<FORM>(a, unit.side, token[x], h, row, d0, sum, m[x], l[x], alone);
                     else *(f32x4 *)(record + (size_t)in * kRecord + d0) = sum;
                 }
             if (!whole && g == 0) {
@@ -1448,7 +1454,7 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(CacheAttend 
 #pragma unroll
         for (int w = 1; w < GROUPS; ++w) join(s_sum[all + w][kD], s_sum[all + w][kD + 1], *(const f32x4 *)(s_sum[all + w] + d0));
     }
-    if (mine) put_query<FORM>(a, false, note.row0, note.h, row, d0, sum, top, total, false);
+    if (mine) put_query<FORM>(a, false, token_of<FORM>(a, false, note.row0, row), note.h, row, d0, sum, top, total, false);
 }
 
 // Of Both: a (token, KV head)'s sums over its own tokens and over its source's, records or a whole unit's state each, become its output.  Groups of 32 threads
