@@ -117,7 +117,7 @@ static size_t note_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H 
 static size_t state_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H * a.G * kRecord * sizeof(float); }
 
 // Rows from which a call that is not small goes to the kernel for many queries: it does the few rows of a request's own as they are, the one for few
-// queries with as many tiles as the sources' take.  Four drafted tokens of 24 requests, four sources of 8 K, 32 rows, float32: 65 us there and 40 here; eight requests
+// queries with as many tiles as the sources' take.  Four drafted tokens of 24 requests, six sources of 8 K, 32 rows, float32: 65 us there and 40 here; eight requests
 // behind 32 K, 32 rows, bf16, 35.4 and 28.8; twelve, 48 rows, 42.7 and 31.9.  But eight requests behind 2 K, 64 quanta: 15.0 and 18.5; behind 4 K, 768 of them, 17.7 and 18.0.
 static bool for_many(long long rows, double quanta) { return rows > kFewRows || (rows > kRows && quanta > 512); }
 
