@@ -223,6 +223,9 @@ template <int FORM> struct Entries {
     __host__ __device__ Entries(const CacheAttend &a) : n(FORM == kBoth ? 2 * a.S : a.n_here), each(FORM == kBoth ? (n + kEntries - 1) / kEntries : 1),
                                                         slots(FORM == kBoth ? (n + each - 1) / each : n) {}
 };
+// Units of the kernel for few queries that are of equal nominal length, so that it need not look at the lengths.  Both sides of Both are counted by theirs: a source
+// is long where its requests' own texts are short.
+template <int FORM> __host__ __device__ inline bool even_units(const CacheAttend &a) { return FORM == kListed || (FORM != kBoth && a.per_unit > 0); }
 // Of Both: the entry that the flat work's quantum `now` lies in, from its place of the table; quanta(e): those of an entry.  first: where the entry begins.
 template <typename F> __host__ __device__ inline int entry_at(const Entries<kBoth> &x, int slot, unsigned now, unsigned &first, unsigned &n, F quanta) {
     int e = slot * x.each;
@@ -799,7 +802,7 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
         const Unit<FORM> u(a, a.first + e, 0, uniform);
         return (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
     };
-    const bool even = FORM != kBoth && (LIST || a.per_unit > 0);  // units of equal nominal length: no need to look at the lengths
+    const bool even = even_units<FORM>(a);
     if (even) {
         total = (unsigned)a.n_here * a.c.H * (unsigned)a.per_unit;
     } else {
@@ -1539,7 +1542,7 @@ template <int FORM> inline Unit<FORM> host_unit(const CacheAttend &a, int entry,
 template <int FORM, typename F> inline void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
     constexpr bool LIST = FORM == kListed;
     const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = FORM == kBoth ? a.rows : few_rows(a);
-    const bool even = LIST || a.per_unit > 0;
+    const bool even = even_units<FORM>(a);
     const int n = Entries<FORM>(a).n;
     std::vector<unsigned> before(n + 1, 0);  // quanta before each request
     for (int e = 0; e < n; ++e)
