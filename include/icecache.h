@@ -429,8 +429,9 @@ ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_toke
  *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with max_shared in the place of max_query and a source's queries in the place of a
  *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
  *   workspace: ice_cache_attend_cross_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
- * SHAPE for n_rows > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * (max_shared / (192 / group_size) + 2) * rows (at most 1024 of them) *
- * n_kv_heads reaches 2^31. */
+ * SHAPE for n_rows > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * n_kv_heads * row tiles reaches 2^31.  A tile is 192 / group_size tokens; of
+ * rows (at most 1024 of them) with up to max_shared queries each and n_tokens together there are at most rows * ceil(max_shared / tile), and
+ * n_tokens / tile + rows where max_shared is not larger than n_tokens.  The plan's starts ascend: if they do not, listed rows may be left as they were. */
 size_t ice_cache_attend_cross_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_rows, int32_t max_shared, int32_t max_keys);
 ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_rows, const int32_t *plan,
                                     int32_t n_tokens, int32_t max_shared, const int32_t *seq_len, int32_t max_keys, const int32_t *block_table,
@@ -447,8 +448,9 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int
  *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with the larger of max_query and max_shared in the place
  *     of max_query; a source's queries and a request's own each for themselves.
  *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 1056 for every row of out, and scratch.
- * SHAPE for n_requests > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * ((max_query + max_shared) / (192 / group_size) + 2) * 2 * n_requests *
- * n_kv_heads reaches 2^31, or n_tokens * n_kv_heads passes 10^7. */
+ * SHAPE for n_requests > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * n_kv_heads * row tiles reaches 2^31 (those of n_requests rows by max_query and
+ * those by max_shared, each counted as for ice_cache_attend_cross), or n_tokens * n_kv_heads passes 10^7.  query_start and the plan's starts ascend: if one does
+ * not, all rows of out and lse are left as they were. */
 size_t ice_cache_attend_shared_bytes(const ice_cache_t *cache, int32_t group_size, int32_t n_requests, int32_t n_tokens, int32_t max_query,
                                      int32_t max_shared, int32_t max_keys, int32_t max_source_keys);
 ice_status_t ice_cache_attend_shared(const ice_cache_t *cache, const void *q, int64_t q_stride, int32_t group_size, int32_t n_requests,

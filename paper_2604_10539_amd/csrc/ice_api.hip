@@ -518,7 +518,8 @@ static ice_status_t set_attend(const ice_cache_t *c, CacheAttend &a, const void 
     if (!q || !aligned16(q)) return fail(ICE_ERR_INVALID_ARG, "q is null or misaligned");
     // (positions are rounded up to steps in 32 bits)
     if ((long long)a.max_blocks * c->block_size > (1 << 30)) return fail(ICE_ERR_SHAPE, "max_blocks %d: more than 2^30 tokens", a.max_blocks);
-    if (ice_status_t st = check_count(c, a, a.pos != nullptr)) return st;
+    if (!a.list_start)  // (else the call has counted its work)
+        if (ice_status_t st = check_count(c, a, a.pos != nullptr)) return st;
     if ((q_stride & 7) || (a.T > 1 && q_stride < (int64_t)c->n_kv_heads * a.G * kD))
         return fail(ICE_ERR_SHAPE, "q's stride must be a multiple of 8 and at least n_kv_heads * group_size * 128");
     if (!out || !aligned16(out)) return fail(ICE_ERR_INVALID_ARG, "out is null or misaligned");
@@ -639,17 +640,26 @@ static ice_status_t check_rows(int32_t n_rows) {
     return n_rows < 1 || n_rows > kSourceRows ? fail(ICE_ERR_SHAPE, "%d rows of the table: outside [1, %d]", n_rows, kSourceRows) : ICE_OK;
 }
 
-// (the quanta of a launch's entries are counted in 31 bits; row tiles of sources are whole tokens, those of both sides lie in one launch)
-static ice_status_t check_sources_count(const ice_cache_t *c, const CacheAttend &a, double queries, double entries) {
-    const double keys = (double)a.max_blocks * c->block_size / 128 + 4, tile = 192 / a.G;
-    if (keys * (queries / tile + 2) * entries * c->n_kv_heads >= 2147483648.0)
-        return fail(ICE_ERR_UNSUPPORTED, "%d rows x %d KV heads x %d blocks x %.0f queries: too many for one call", a.S, c->n_kv_heads, a.max_blocks, queries);
+// The row tiles that `rows` requests or sources can have between them: each those of its most queries, and all together those of n_tokens, the last ones of
+// each not full.  (A most beyond n_tokens, that no step can have, counts as it is given.)  The kernels take arrays of starts that do not ascend, where
+// queries would count several times, for a step without queries.
+static double row_tiles(const CacheAttend &a, int most, int rows) {
+    const int tile = 192 / a.G;
+    const double each = rows * (double)((most + (long long)tile - 1) / tile);
+    return most > a.T ? each : std::min(each, (double)(a.T / tile) + std::min(rows, a.T));
+}
+// (the quanta of a launch's entries are counted in 31 bits; both sides of attention behind a source lie in one launch)
+static ice_status_t check_sources_count(const ice_cache_t *c, const CacheAttend &a, double tiles) {
+    if (((double)a.max_blocks * c->block_size / 128 + 4) * tiles * c->n_kv_heads >= 2147483648.0)
+        return fail(ICE_ERR_UNSUPPORTED, "%d rows, %d tokens x %d KV heads x %d blocks: too many for one call", a.S, a.T, c->n_kv_heads, a.max_blocks);
     return ICE_OK;
 }
 static ice_status_t check_shared_count(const ice_cache_t *c, const CacheAttend &a) {
-    return check_sources_count(c, a, (double)a.max_query + a.max_shared, 2.0 * a.S);
+    return check_sources_count(c, a, row_tiles(a, a.max_query, a.S) + row_tiles(a, a.max_shared, a.S));
 }
-static ice_status_t check_cross_count(const ice_cache_t *c, const CacheAttend &a) { return check_sources_count(c, a, a.max_query, std::min(a.S, 1024)); }
+static ice_status_t check_cross_count(const ice_cache_t *c, const CacheAttend &a) {
+    return check_sources_count(c, a, row_tiles(a, a.max_query, std::min(a.S, 1024)));
+}
 
 // where a list's parts lie (ice_plan_sources)
 static void set_list(CacheAttend &a, const int32_t *plan) {

@@ -58,6 +58,7 @@ struct Unit {
                              // position behind the lowest one's own)
     int tokens;              // the length, or what the table has room for if that is less: the queries' positions follow the length all the same
     bool side;               // of Both: gathered
+    bool falls;              // the next entry of query_start is less than this one
     // t: the request's length; x, y: its entry of query_start and the next one, or x the length of its list.
     __host__ __device__ Unit(const CacheAttend &a, int s, int t, int x, int y, int lowest = 0) : side(FORM == kBoth && s < a.S) { set(a, s, t, x, y, lowest); }
     // UNIFORM: the same on all lanes.  A request's words are asked for before one is looked at: left to the compiler, the length was asked for
@@ -89,6 +90,7 @@ struct Unit {
     }
     __host__ __device__ void set(const CacheAttend &a, int s, int t, int x, int y, int lowest = 0) {
         tokens = (int)min((long long)max(t, 0), (long long)a.max_blocks << (a.c.tile_shift + 4));
+        falls = !LIST && y < x;
         if constexpr (LIST) {
             row0 = s;
             n_query = 1;
@@ -363,6 +365,22 @@ __device__ inline void clear_unsourced(const CacheAttend &a) {
             put_row(a, row, d0, f32x4{0.f, 0.f, 0.f, 0.f}, kNoMax, 0.f);
         }
     }
+}
+
+// Of gathered forms the host counts a call's work by n_tokens, whatever each request may have; so queries that several entries of arrays which do not ascend
+// would count must not enter the sums of 32 bits.  A wave that has seen such entries says so in the place of its sum, which is less than 2^31 otherwise; every
+// workgroup then takes the step for one without queries, and of Both the join is told to leave all rows.  (The other forms are counted by requests.)
+constexpr unsigned kFell = ~0u;
+template <int FORM> __device__ inline void put_wave(unsigned *s_wave, int wave, int lane, unsigned incl, bool falls) {
+    if constexpr (FORM == kCross || FORM == kBoth)
+        if (__any(falls)) incl = kFell;
+    if (lane == 63) s_wave[wave] = incl;
+}
+template <int FORM> __device__ inline bool fell(unsigned sum) { return (FORM == kCross || FORM == kBoth) && sum == kFell; }
+template <int FORM> __device__ inline void leave_all(const CacheAttend &a) {
+    if constexpr (FORM == kBoth)
+        for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)a.T * a.c.H; i += (long long)gridDim.x * blockDim.x)
+            a.token_notes[i] = TokenNote{-1, 1, 0, kNoteLeft};
 }
 
 // Attention of few query rows (queries times heads of a group: at most 16 NT) of every request over its keys.
@@ -798,8 +816,10 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
 
     unsigned total = 0;
     const Entries<FORM> entries(a);
+    bool falls = false, unordered = false;
     auto quanta_at = [&](int e, auto uniform) -> unsigned {
         const Unit<FORM> u(a, a.first + e, 0, uniform);
+        falls |= u.falls;
         return (unsigned)few_quanta(a, u, NT * R, Q) * (unsigned)a.c.H;
     };
     const bool even = even_units<FORM>(a);
@@ -815,19 +835,24 @@ __global__ __launch_bounds__(W * 64, NT > 1 || W > 4 ? 2 : 3) void cache_attend_
                 n = quanta_at(e, std::false_type());
             }
             const unsigned incl = (unsigned)wave_scan_add((int)n);
-            if (lane == 63) s_wave[wave] = incl;
+            put_wave<FORM>(s_wave, wave, lane, incl, falls);
             __syncthreads();
             unsigned before = total;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 if (w < wave) before += s_wave[w];
                 total += s_wave[w];
+                unordered |= fell<FORM>(s_wave[w]);
             }
             if (e < entries.slots) s_before[e] = before + incl - n;
             __syncthreads();
         }
         if (tid == 0) s_before[entries.slots] = total;
         __syncthreads();
+    }
+    if (unordered) {
+        total = 0;
+        leave_all<FORM>(a);
     }
     if constexpr (FORM == kCross)
         if (a.first == 0) clear_unsourced(a);
@@ -984,7 +1009,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
     unsigned total = 0;
     const Entries<FORM> entries(a);
-    auto quanta_at = [&](int e, auto uniform) -> unsigned { return Chunks(a, Unit<FORM>(a, a.first + e, 0, uniform)).per_head * (unsigned)a.c.H; };
+    bool falls = false, unordered = false;
+    auto quanta_at = [&](int e, auto uniform) -> unsigned {
+        const Unit<FORM> u(a, a.first + e, 0, uniform);
+        falls |= u.falls;
+        return Chunks(a, u).per_head * (unsigned)a.c.H;
+    };
     for (int e0 = 0; e0 < entries.slots; e0 += kWaves * 64) {
         const int e = e0 + tid;
         unsigned n = 0;
@@ -994,19 +1024,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void cache_chunk_kernel(CacheAttend
             n = e < a.n_here ? quanta_at(e, std::false_type()) : 0u;
         }
         const unsigned incl = (unsigned)wave_scan_add((int)n);
-        if (lane == 63) s_wave[wave] = incl;
+        put_wave<FORM>(s_wave, wave, lane, incl, falls);
         __syncthreads();
         unsigned before = total;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             if (w < wave) before += s_wave[w];
             total += s_wave[w];
+            unordered |= fell<FORM>(s_wave[w]);
         }
         if (e < entries.slots) s_before[e] = before + incl - n;
         __syncthreads();
     }
     if (tid == 0) s_before[entries.slots] = total;
     __syncthreads();
+    if (unordered) {
+        total = 0;
+        leave_all<FORM>(a);
+    }
     if constexpr (FORM == kCross)
         if (a.first == 0) clear_unsourced(a);
     const Pieces pieces(__builtin_amdgcn_readfirstlane(total), gridDim.x, false);
