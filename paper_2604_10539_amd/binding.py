@@ -418,6 +418,8 @@ def ice_plan_sources(source, query_start, seq_len, plan, n_rows, n_tokens, strea
 def ice_cache_append(cache: IceCacheDesc, q, q_stride, n_q_heads, q_out, q_out_stride, k, v, k_stride, v_stride, n_tokens, n_requests, query_start, seq_len,
                      source, block_table, max_blocks, rope, n_positions, rotated, neighbours, stream=None) -> None:
     """q, q_out, k, v: addresses (rows need not be contiguous with each other)."""
+    if isinstance(rope, torch.Tensor) and rope.numel() == 0:
+        raise IceError(ICE_ERR_SHAPE, "rope: an empty table")  # (it may have no address, which is how none is handed over)
     _check(lib().ice_cache_append(C.byref(cache), q, q_stride, n_q_heads, q_out, q_out_stride, k, v, k_stride, v_stride, n_tokens, n_requests, _ptr(query_start),
                                   _ptr(seq_len), _ptr(source), _ptr(block_table), max_blocks, _ptr(rope), n_positions, rotated, neighbours, _stream(stream)))
 

@@ -354,6 +354,7 @@ PyObject *call_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
             const Tensor &r = tensor(a[10], "rope");
             if (!(r.scalar_type() == at::kFloat && r.dim() == 2 && r.is_contiguous() && c.here(r) && r.size(0) <= INT32_MAX && r.size(1) <= 128))
                 refuse_shape("rope: contiguous float32 [positions, up to 128] on the cache's device");
+            if (r.numel() == 0) refuse_shape("rope: an empty table");  // (it may have no address, which is how none is handed over)
             rope = r.const_data_ptr<float>();
             positions = (int)r.size(0);
             rotated = (int)r.size(1);

@@ -174,6 +174,16 @@ def test_appending_refuses():
     assert b.lib().ice_cache_append(None, *good.values(), None) == b.ICE_ERR_INVALID_ARG
 
 
+def test_an_empty_table_of_rotations_is_not_none():
+    """(A fresh tensor of no values has no address, which would read as no rotations.)"""
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    c = p.make_cache_desc(FAKE, 10, 2, 16)
+    for q, out in ((FAKE, FAKE), (None, None)):
+        for shape in ((0, 128), (0, 0), (5, 0)):
+            assert status(p.ice_cache_append, c, q, 1024, 8, out, 1024, FAKE, FAKE, 256, 256, 4, 2, FAKE, FAKE, FAKE, FAKE, 4, torch.empty(shape), *shape, 0) == b.ICE_ERR_SHAPE
+
+
 def test_attention_to_sources_refuses():
     import paper_2604_10539_amd as p
     from paper_2604_10539_amd import binding as b

@@ -473,6 +473,22 @@ def test_a_pool_beyond_32_bit_offsets():
     check(out, lse, want)
 
 
+@pytest.mark.parametrize("shape", [(0, 128), (0, 0), (5, 0)])
+def test_an_empty_table_of_rotations_is_refused(shape):
+    """Nothing is held: without the refusal keys would enter as they are."""
+    import paper_2604_10539_amd.binding as b
+    from paper_2604_10539_amd import IceError
+    rng = np.random.default_rng(52)
+    c = make(4, 2, 16)
+    c.data.fill_(9)
+    k, v, q = up(bits(rng, 3, 2, D)), up(bits(rng, 3, 2, D)), up(bits(rng, 3, 4, D))
+    for queries in (None, q):
+        with pytest.raises(IceError) as e:
+            c.append(k, v, i32([0, 3]), i32([3]), i32([[1]]), q=queries, rope=torch.empty(shape, device="cuda"))
+        assert e.value.status == b.ICE_ERR_SHAPE
+    assert bool((c.data == 9).all())
+
+
 # ---------------------------------------------------------------------------------------------------------- as they are used
 class Server:
     """Two layers' caches, a shared prompt in row 0, requests behind it, and the same in numpy."""
