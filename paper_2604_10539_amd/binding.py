@@ -411,7 +411,11 @@ def ice_cache_attend_tokens(cache: IceCacheDesc, q, q_stride, group_size, n_requ
 
 
 def ice_plan_sources(source, query_start, seq_len, plan, n_rows, n_tokens, stream=None) -> None:
-    """int32 device tensors as in the header; seq_len None where the sources are rows of another table."""
+    """int32 device tensors as in the header; seq_len None where the sources are rows of another table.  Runs on their device: on `stream`, or the one that is
+    current there."""
+    if isinstance(source, torch.Tensor) and source.is_cuda and source.get_device() != _current_device():
+        with torch.cuda.device(source.get_device()):
+            return ice_plan_sources(source, query_start, seq_len, plan, n_rows, n_tokens, stream)
     _extension().plan_sources(_stream(stream) or 0, source, query_start, seq_len, plan, n_rows, n_tokens)
 
 

@@ -223,3 +223,38 @@ def test_sorting_takes_arrays_on_a_gpu_only():
     assert status(p.ice_plan_sources, *args) == b.ICE_ERR_INVALID_ARG
     for i, bad in ((0, e(3)), (1, e(2)), (2, e(1)), (3, e(15)), (0, torch.zeros(2)), (1, None), (3, torch.zeros(32, dtype=torch.int32)[::2])):
         assert status(p.ice_plan_sources, *[bad if j == i else x for j, x in enumerate(args)]) == b.ICE_ERR_SHAPE, i
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_sorting_goes_to_the_device_of_its_arrays(monkeypatch, current):
+    """Rows of another table are sorted by ice_plan_sources itself: on the arrays' device and its current stream, whatever the current device is."""
+    from paper_2604_10539_amd import binding as b
+    state, calls = {"device": current}, []
+
+    class Under:
+        def __init__(self, device):
+            self.device = getattr(device, "index", device)
+
+        def __enter__(self):
+            self.before, state["device"] = state["device"], self.device
+
+        def __exit__(self, *_):
+            state["device"] = self.before
+
+    class OnSecond(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 1
+
+    class Native:
+        def plan_sources(self, stream, *args):
+            calls.append((state["device"], stream, args))
+    monkeypatch.setattr(torch.cuda, "device", Under)
+    monkeypatch.setattr(b, "_current_device", lambda: state["device"])
+    monkeypatch.setattr(b, "_extension", lambda: Native())
+    monkeypatch.setattr(b, "_stream", lambda stream: 100 + state["device"] if stream is None else stream)
+    arrays = [torch.zeros(n, dtype=torch.int32).as_subclass(OnSecond) for n in (2, 3, 2, 16)]
+    b.ice_plan_sources(*arrays, 2, 5)
+    b.ice_plan_sources(*arrays, 2, 5, stream=7)
+    assert [x[:2] for x in calls] == [(1, 101), (1, 7)] and all(x[2][0] is arrays[0] and x[2][4:] == (2, 5) for x in calls) and state["device"] == current
