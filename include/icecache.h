@@ -427,7 +427,8 @@ ice_status_t ice_plan_sources(int32_t n_requests, int32_t n_rows, int32_t n_toke
  *   seq_len [n_rows], block_table [n_rows][max_blocks]: those of the sources.  max_keys: about the longest of them, a hint.
  *   max_shared: no source has more queries (tokens; those beyond are left out), in [1, 2^24].
  *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with max_shared in the place of max_query and a source's queries in the place of a
- *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.
+ *     request's.  Queries of requests without a source, or whose source has no token, get 0 and -inf.  Rows that are not listed are left as they were.  (The workgroups that
+ *     attend write those of no source first, so thousands of them beside one short source take longer than the attention.)
  *   workspace: ice_cache_attend_cross_bytes() bytes, 16-byte aligned, for this call alone (NULL where that is 0).
  * SHAPE for n_rows > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * n_kv_heads * row tiles reaches 2^31.  A tile is 192 / group_size tokens; of
  * rows (at most 1024 of them) with up to max_shared queries each and n_tokens together there are at most rows * ceil(max_shared / tile), and
@@ -446,8 +447,11 @@ ice_status_t ice_cache_attend_cross(const ice_cache_t *cache, const void *q, int
  *   max_query, max_keys: of the requests' own queries and tokens, as for ice_cache_attend; max_shared: no source has more queries (tokens of all its requests;
  *     those beyond are left out, their outputs as they were), in [1, 2^24]; max_source_keys: about the longest source, a hint.
  *   q, out, out_type, lse: as for ice_cache_attend.  Precision: as there, with the larger of max_query and max_shared in the place
- *     of max_query; a source's queries and a request's own each for themselves.
- *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 1056 for every row of out, and scratch.
+ *     of max_query; a source's queries and a request's own each for themselves.  But where that larger one times group_size is 17 to 48, requests and sources with at
+ *     most 16 query rows keep 16 bits only in a call that is not small: n_kv_heads * (n_requests * ceil(max_keys / 128) + ceil(max_source_keys / 128)) > 512.  So how a
+ *     bf16 output is rounded depends on how many share its source and on these hints; the precision of fp32 outputs does not.
+ *   workspace: ice_cache_attend_shared_bytes() bytes, 16-byte aligned, for this call alone: 1056 for every row of out (a token's query head), 32 for every token and
+ *     KV head, and scratch of up to 104 MB: 1.2 GB for 32 K tokens of 32 query heads.  Give long prompts in chunks.
  * SHAPE for n_requests > 8192; UNSUPPORTED where (tokens of a table row / 128 + 4) * n_kv_heads * row tiles reaches 2^31 (those of n_requests rows by max_query and
  * those by max_shared, each counted as for ice_cache_attend_cross), or n_tokens * n_kv_heads passes 10^7.  query_start and the plan's starts ascend: if one does
  * not, all rows of out and lse are left as they were. */

@@ -874,7 +874,8 @@ class IceCache:
         """attend where requests' texts begin with the tokens of a source, a row of the same table: causal attention over that row and the request's own as
         one text; a source is read once for all queries that share it.  source and plan: as given to and returned by IceBlocks.plan_sources for this
         step.  max_query, max_len: as for attend, of the requests' own; max_shared: the most queries (tokens) of all requests that share a source (none has
-        more); max_source: about the longest source (a hint).  Give them wherever they are known.  -> out, or (out, lse), as attend."""
+        more); max_source: about the longest source (a hint).  Give them wherever they are known.  Scratch: about 1 KB for every row of q and head, so give long
+        prompts in chunks.  -> out, or (out, lse), as attend."""
         if stream is not None or _current_device() != self._index:
             return _elsewhere(IceCache.attend_shared, self, stream, q, query_start, source, plan, seq_len, block_table, max_query, max_shared, max_len,
                               max_source, window, out, out_dtype, lse, with_lse)

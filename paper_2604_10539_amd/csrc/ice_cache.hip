@@ -256,7 +256,7 @@ __device__ inline uint32_t round2(float a, float b) {
 // A wave takes four consecutive tokens, 16 lanes of 8 dims to a row, and `span` heads of them, PER at a time: of the queries, then the keys, then the
 // values.  Pair i of a row's rotated dims (half apart, or neighbours) becomes (x cos - y sin, x sin + y cos), products and sums each rounded to
 // 32 bits; a query is then rounded to bf16 and a key held, so either is rounded to fewer bits once.  The angles' cos and sin are read once for all of a wave's
-// heads.  Bound by the rows' bytes where there are many (two prompts of 16 K tokens: 706 MB at 4.9 TB/s, what a copy reaches), else by three trips: the requests'
+// heads.  Bound by the rows' bytes where there are many (two prompts of 16 K tokens: 723 MB in 134 us, 5.4 TB/s; a copy reaches 4.9), else by three trips: the requests'
 // words beside the rows, the block and the angles, the stores (16 tokens 4.1 us, the write without rotation 2.8).
 template <int PER>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, int chunks, int span) {

@@ -353,7 +353,9 @@ __device__ inline void find_nan(const CacheAttend &a, const int *table, int h, i
     }
 }
 
-// Queries whose requests have no source see nothing: 0 and -inf.
+// Queries whose requests have no source see nothing: 0 and -inf.  The workgroups of the call share them, before their own work; these are as many as the sources' keys
+// are worth, so one short source leaves the rows to few.  One source of 100 tokens, four queries of its own, float32: 1 KV head of 4 query heads 6.2 us, with 100 rows of no source
+// 29, with 1000 246; 8 KV heads 6.4, 12.8 and 67.
 __device__ inline void clear_unsourced(const CacheAttend &a) {
     const int from = min(max(a.query_start[a.S], 0), a.T), to = min(max(a.query_start[a.S + 1], 0), a.T), heads = a.c.H * a.G;
     for (int e = from + (int)blockIdx.x; e < to; e += (int)gridDim.x) {

@@ -118,9 +118,12 @@ static size_t state_bytes(const CacheAttend &a) { return 2 * (size_t)a.T * a.c.H
 
 // Rows from which a call that is not small goes to the kernel for many queries: it does the few rows of a request's own as they are, the one for few
 // queries with as many tiles as the sources' take.  Four drafted tokens of 24 requests, six sources of 8 K, 32 rows, float32: 65 us there and 40 here; eight requests
-// behind 32 K, 32 rows, bf16, 35.4 and 28.8; twelve, 48 rows, 42.7 and 31.9.  But eight requests behind 2 K, 64 quanta: 15.0 and 18.5; behind 4 K, 768 of them, 17.7 and 18.0.
+// behind 32 K, 32 rows, bf16, 35.4 and 28.8; twelve, 48 rows, 42.7 and 31.9.  But eight requests behind 2 K, 64 quanta: 15.0 and 18.5; behind 4 K, 768 of them, the two are even,
+// 17.7 and 18.0.
 static bool for_many(long long rows, double quanta) { return rows > kFewRows || (rows > kRows && quanta > 512); }
 
+// (How many sources a step has is not known here: quanta are those of the requests and of one source.  Of several a piece is longer than it need be: one token each of
+// eight requests, 1 KV head of 8, behind four sources of 8 K 20.3 us, behind one 18.9; 2 KV heads, behind eight of 4 K 18.2, behind one 18.9.)
 size_t plan_cache_shared(CacheAttend &a, int max_source) {
     const long long most = std::max(a.max_query, a.max_shared), tile = kChunkRows / a.G;
     const auto quanta = [&](int keys, long long queries) { return ((long long)keys + kQuantum - 1) / kQuantum * (a.many ? (queries + tile - 1) / tile : 1); };
