@@ -1576,14 +1576,19 @@ template <int FORM> inline Unit<FORM> host_unit(const CacheAttend &a, int entry,
     if constexpr (FORM == kListed) return Unit<FORM>(a, entry, 1 << 30, len[entry * a.c.H + h], 0);
     else return Unit<FORM>(a, entry, len[entry], start[entry], start[entry + 1]);
 }
+// (gathered forms take arrays that do not ascend for a step without queries)
+template <int FORM> inline bool fell_at(const Unit<FORM> &u) { return (FORM == kCross || FORM == kBoth) && u.falls; }
 template <int FORM, typename F> inline void cut_few(const CacheAttend &a, const int *start, const int *len, F put) {
     constexpr bool LIST = FORM == kListed;
     const int quantum = (LIST ? kListWaves : kWaves) * kStep, rows = FORM == kBoth ? a.rows : few_rows(a);
     const bool even = even_units<FORM>(a);
     const int n = Entries<FORM>(a).n;
     std::vector<unsigned> before(n + 1, 0);  // quanta before each request
-    for (int e = 0; e < n; ++e)
-        before[e + 1] = before[e] + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, host_unit<FORM>(a, a.first + e, 0, start, len), rows, quantum));
+    for (int e = 0; e < n; ++e) {
+        const auto u = host_unit<FORM>(a, a.first + e, 0, start, len);
+        if (!even && fell_at(u)) return;
+        before[e + 1] = before[e] + (unsigned)a.c.H * (unsigned)(even ? a.per_unit : few_quanta(a, u, rows, quantum));
+    }
     const unsigned total = before[n];
     const unsigned launched = a.whole ? a.n_here * a.c.H : FORM == kBoth ? a.groups : a.few_groups;
     const Pieces pieces(total, launched, a.whole);
@@ -1607,7 +1612,11 @@ template <int FORM, typename F> inline void cut_many(const CacheAttend &a, const
     const int n = Entries<FORM>(a).n;
     const unsigned launched = FORM == kBoth ? a.groups : a.many_groups;
     std::vector<unsigned> before(n + 1, 0);
-    for (int e = 0; e < n; ++e) before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, host_unit<FORM>(a, a.first + e, 0, start, len)).per_head;
+    for (int e = 0; e < n; ++e) {
+        const auto u = host_unit<FORM>(a, a.first + e, 0, start, len);
+        if (fell_at(u)) return;
+        before[e + 1] = before[e] + (unsigned)a.c.H * Chunks(a, u).per_head;
+    }
     const Pieces pieces(before[n], launched, false);
     if (before[n] == 0) return;
     for (unsigned i = 0; i < pieces.groups && i < launched; ++i)

@@ -70,6 +70,26 @@ def test_the_edge_of_what_can_be_counted():
         assert status(p.ice_cache_attend_cross, c, FAKE, 1 << 20, 4, 1, FAKE, tokens, tokens, FAKE, 1 << 30, FAKE, width, FAKE, 0, None, FAKE, need - 1) == want
 
 
+@pytest.mark.parametrize("queries", [1, 60])
+def test_starts_that_do_not_ascend_have_no_parts(queries):
+    """As in the kernels.  Every second request with all of the step's queries would be more quanta than 32 bits count (300 of 2^24 tokens, 32 heads, two tiles)."""
+    import paper_2604_10539_amd as p
+    from paper_2604_10539_amd import binding as b
+    n = 600
+    c = p.make_cache_desc(FAKE, 8192, 32, 64)
+    width, lens = 1 << 18, [1 << 24] * n
+    good = np.minimum(np.arange(n + 1), queries)
+    bad = np.arange(n + 1) % 2 * queries
+    plan = {name: np.concatenate([start, [queries], np.zeros(n, int), np.arange(queries), np.zeros(queries, int)]) for name, start in (("good", good), ("bad", bad))}
+    cut = lambda start, listed: b.ice_debug_shared_cut(c, 4, n, start, plan[listed], queries, queries, queries, lens, 1 << 24, 1 << 24, width)  # noqa: E731
+    assert len(cut(good, "good")) > 0
+    for start, listed in ((good, "bad"), (bad, "good"), (bad, "bad")):
+        assert len(cut(start, listed)) == 0
+    for start in (good, bad):
+        parts = b.ice_debug_cross_cut(c, 4, n, np.concatenate([start, [queries]]), queries, queries, lens, 1 << 24, width)
+        assert (len(parts) > 0) == (start is good)
+
+
 def test_a_most_that_a_step_cannot_have_counts_as_it_is_given():
     import paper_2604_10539_amd as p
     from paper_2604_10539_amd import binding as b
